@@ -76,13 +76,15 @@ typedef struct {
   int32_t dtype;        /* moe_dtype */
 } moe_desc;
 
-/* moe_workspace_size(which) selectors */
+/* moe_workspace_size(which) selectors (the last two belong to calls of pcmoe_ext.h) */
 enum {
   MOE_WS_PERMUTE = 0,     /* scratch of moe_permute */
   MOE_WS_FFN_SAVED = 1,   /* activations saved by moe_expert_ffn_fwd for the backward */
   MOE_WS_FFN_FWD = 2,     /* scratch of moe_expert_ffn_fwd */
   MOE_WS_FFN_BWD = 3,     /* scratch of moe_expert_ffn_bwd */
-  MOE_WS_ROUTE_BWD = 4    /* scratch of moe_route_bwd */
+  MOE_WS_ROUTE_BWD = 4,   /* scratch of moe_route_bwd and moe_route_gated_bwd */
+  MOE_WS_FFN_Q4 = 5,      /* scratch of moe_expert_ffn_q4 */
+  MOE_WS_FFN_CKPT = 6     /* the 8-bit checkpoint that moe_ffn_checkpoint writes */
 };
 
 /* Bytes of device memory the selected buffer needs for this shape (0 if none). */

@@ -1,6 +1,6 @@
 // C ABI of the pcmoe library: argument validation (before any HIP call), workspace sizing,
 // error reporting and the optional per-kernel event timing. Kernels live in the other files.
-#include "pcmoe_internal.h"
+#include "expert_ops.h"
 
 #include <atomic>
 #include <mutex>
@@ -78,6 +78,39 @@ moe_status check_desc(const moe_desc* d) {
   if ((wmax + 256) * wmax * es >= ((int64_t)1 << 31))
     return fail(MOE_ERR_UNSUPPORTED, "one expert's %d x %d weight matrix (+ 256 rows) exceeds 2 GiB", d->d_ff,
                 d->d_model);
+  return MOE_OK;
+}
+
+moe_status check_gate(const moe_desc& d, const moe_gate* g) {
+  if (!g) return fail(MOE_ERR_INVALID_ARGUMENT, "gate is NULL");
+  if (g->score != MOE_SCORE_SOFTMAX && g->score != MOE_SCORE_SIGMOID)
+    return fail(MOE_ERR_INVALID_ARGUMENT, "score kind %d", g->score);
+  if (g->n_groups < 1 || d.n_experts % g->n_groups)
+    return fail(MOE_ERR_INVALID_ARGUMENT, "n_groups=%d must divide E=%d", g->n_groups, d.n_experts);
+  if (g->topk_groups < 1 || g->topk_groups > g->n_groups)
+    return fail(MOE_ERR_INVALID_ARGUMENT, "topk_groups=%d outside [1, n_groups=%d]", g->topk_groups, g->n_groups);
+  const int size = d.n_experts / g->n_groups;
+  if (g->group_top != 1 && g->group_top != 2) return fail(MOE_ERR_INVALID_ARGUMENT, "group_top must be 1 or 2");
+  if (g->n_groups > 1 && g->group_top > size)
+    return fail(MOE_ERR_INVALID_ARGUMENT, "group_top=2 with groups of one expert");
+  if (d.top_k > g->topk_groups * size)
+    return fail(MOE_ERR_INVALID_ARGUMENT, "top_k=%d > %d experts of the open groups", d.top_k, g->topk_groups * size);
+  if (!(g->scale > 0.f) || !std::isfinite(g->scale))
+    return fail(MOE_ERR_INVALID_ARGUMENT, "scale must be > 0 and finite");
+  if (g->n_groups > 64) return fail(MOE_ERR_UNSUPPORTED, "n_groups=%d > 64", g->n_groups);
+  return MOE_OK;
+}
+
+moe_status check_q4(int32_t n, int32_t rows, int32_t cols, int32_t group, int32_t dtype) {
+  if (dtype != MOE_F32 && dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARGUMENT, "dtype %d", dtype);
+  if (n < 1 || rows < 1 || cols < 1)
+    return fail(MOE_ERR_INVALID_ARGUMENT, "non-positive shape n=%d rows=%d cols=%d", n, rows, cols);
+  if (group != 32 && group != 64 && group != 128)
+    return fail(MOE_ERR_INVALID_ARGUMENT, "group=%d is not 32, 64 or 128", group);
+  if (rows % 16 || cols % 128)
+    return fail(MOE_ERR_UNSUPPORTED, "rows=%d must be a multiple of 16 and cols=%d of 128", rows, cols);
+  if ((double)n * rows * cols >= (double)((int64_t)1 << 40))
+    return fail(MOE_ERR_UNSUPPORTED, "%d matrices of %d x %d are too many weights", n, rows, cols);
   return MOE_OK;
 }
 
@@ -172,6 +205,8 @@ size_t moe_workspace_size(const moe_desc* d, int which) {
     case MOE_WS_FFN_FWD: return ffn_fwd_ws_bytes(*d);
     case MOE_WS_FFN_BWD: return ffn_bwd_ws_bytes(*d);
     case MOE_WS_ROUTE_BWD: return route_bwd_ws_bytes(*d);
+    case MOE_WS_FFN_Q4: return ffn_q4_ws_bytes(*d);
+    case MOE_WS_FFN_CKPT: return ffn_ckpt_bytes(*d);
   }
   return 0;
 }
@@ -187,6 +222,21 @@ moe_status moe_route(const moe_desc* d, const void* x, const void* w_router, con
   return hip_status(launch_route_fwd(*d, x, w_router, logit_bias, logit_bias ? bias_groups : 1, logits, topk_idx,
                                      topk_w, stream),
                     "moe_route");
+}
+
+moe_status moe_route_gated(const moe_desc* d, const moe_gate* gate, const void* x, const void* w_router,
+                           const float* logit_bias, int32_t bias_groups, const float* select_bias, float* logits,
+                           int32_t* topk_idx, float* topk_w, hipStream_t stream) {
+  moe_status st = check_desc(d);
+  if (st || (st = check_gate(*d, gate))) return st;
+  NEED(x); NEED(w_router); NEED(logits); NEED(topk_idx); NEED(topk_w);
+  if (((uintptr_t)logit_bias | (uintptr_t)select_bias) & 3)
+    return fail(MOE_ERR_INVALID_ARGUMENT, "logit_bias or select_bias misaligned");
+  if (logit_bias && (bias_groups < 1 || d->T % bias_groups))
+    return fail(MOE_ERR_INVALID_ARGUMENT, "bias_groups=%d must divide T=%d", bias_groups, d->T);
+  return hip_status(launch_route_gated(*d, *gate, x, w_router, logit_bias, logit_bias ? bias_groups : 1, select_bias,
+                                       logits, topk_idx, topk_w, stream),
+                    "moe_route_gated");
 }
 
 moe_status moe_permute(const moe_desc* d, const int32_t* topk_idx, const void* x, int32_t* counts, int32_t* offsets,
@@ -261,20 +311,85 @@ moe_status moe_expert_ffn_bwd(const moe_desc* d, const void* x, const void* x_pe
                     "moe_expert_ffn_bwd");
 }
 
+#define NEED_ALL_EXPERTS(fn)                                                                                    \
+  if (d->local_begin != 0 || d->local_count != d->n_experts)                                                    \
+  return fail(MOE_ERR_INVALID_ARGUMENT,                                                                         \
+              fn " needs every expert's dgate (local range must be [0, E)); a party shard leaves the "          \
+                 "router gradient to the data owner")
+
 moe_status moe_route_bwd(const moe_desc* d, const void* x, const float* logits, const int32_t* topk_idx,
                          const float* topk_w, const float* dgate, float* dlogits, float* dw_router, void* ws,
                          size_t ws_bytes, hipStream_t stream) {
   moe_status st = check_desc(d);
   if (st) return st;
-  if (d->local_begin != 0 || d->local_count != d->n_experts)
-    return fail(MOE_ERR_INVALID_ARGUMENT,
-                "moe_route_bwd needs every expert's dgate (local range must be [0, E)); a party shard leaves the "
-                "router gradient to the data owner");
+  NEED_ALL_EXPERTS("moe_route_bwd");
   NEED(x); NEED(topk_idx); NEED(topk_w); NEED(dgate); NEED(dlogits); NEED(dw_router);
   if (!d->renormalize) NEED(logits);
   NEED_WS(ws_bytes, route_bwd_ws_bytes(*d));
   return hip_status(launch_route_bwd(*d, x, logits, topk_idx, topk_w, dgate, dlogits, dw_router, ws, stream),
                     "moe_route_bwd");
+}
+
+moe_status moe_route_gated_bwd(const moe_desc* d, const moe_gate* gate, const void* x, const float* logits,
+                               const int32_t* topk_idx, const float* topk_w, const float* dgate, float* dlogits,
+                               float* dw_router, void* ws, size_t ws_bytes, hipStream_t stream) {
+  moe_status st = check_desc(d);
+  if (st || (st = check_gate(*d, gate))) return st;
+  NEED_ALL_EXPERTS("moe_route_gated_bwd");
+  NEED(x); NEED(logits); NEED(topk_idx); NEED(topk_w); NEED(dgate); NEED(dlogits); NEED(dw_router);
+  NEED_WS(ws_bytes, route_bwd_ws_bytes(*d));
+  return hip_status(launch_route_gated_bwd(*d, *gate, x, logits, topk_idx, topk_w, dgate, dlogits, dw_router, ws,
+                                           stream),
+                    "moe_route_gated_bwd");
+}
+
+moe_status moe_ffn_checkpoint(const moe_desc* d, const int32_t* offsets, const void* saved, void* ckpt,
+                              size_t ckpt_bytes, hipStream_t stream) {
+  moe_status st = check_desc(d);
+  if (st) return st;
+  NEED(offsets); NEED(saved);
+  void* const ws = ckpt;
+  NEED_WS(ckpt_bytes, ffn_ckpt_bytes(*d));
+  return hip_status(launch_ffn_checkpoint(*d, offsets, saved, ckpt, stream), "moe_ffn_checkpoint");
+}
+
+moe_status moe_ffn_restore(const moe_desc* d, const int32_t* offsets, const void* ckpt, size_t ckpt_bytes, void* saved,
+                           hipStream_t stream) {
+  moe_status st = check_desc(d);
+  if (st) return st;
+  NEED(offsets); NEED(saved);
+  const void* const ws = ckpt;
+  NEED_WS(ckpt_bytes, ffn_ckpt_bytes(*d));
+  return hip_status(launch_ffn_restore(*d, offsets, ckpt, saved, stream), "moe_ffn_restore");
+}
+
+moe_status moe_q4_pack(int32_t n, int32_t rows, int32_t cols, int32_t group, int32_t dtype, const void* w, void* codes,
+                       void* scales, hipStream_t stream) {
+  if (moe_status st = check_q4(n, rows, cols, group, dtype)) return st;
+  NEED(w); NEED(codes); NEED(scales);
+  return hip_status(launch_q4_pack(n, rows, cols, group, dtype, w, codes, scales, stream), "moe_q4_pack");
+}
+
+moe_status moe_q4_unpack(int32_t n, int32_t rows, int32_t cols, int32_t group, int32_t dtype, const void* codes,
+                         const void* scales, void* w, hipStream_t stream) {
+  if (moe_status st = check_q4(n, rows, cols, group, dtype)) return st;
+  NEED(codes); NEED(scales); NEED(w);
+  return hip_status(launch_q4_unpack(n, rows, cols, group, dtype, codes, scales, w, stream), "moe_q4_unpack");
+}
+
+moe_status moe_expert_ffn_q4(const moe_desc* d, int32_t group, const void* x, const void* x_perm,
+                             const int32_t* offsets, const void* gate_codes, const void* gate_scales,
+                             const void* up_codes, const void* up_scales, const void* down_codes,
+                             const void* down_scales, void* y_perm, void* ws, size_t ws_bytes, hipStream_t stream) {
+  moe_status st = check_desc(d);
+  if (st || (st = check_q4(d->local_count + d->n_shared, d->d_ff, d->d_model, group, d->dtype))) return st;
+  if (d->n_shared > 0) NEED(x);
+  NEED(x_perm); NEED(offsets); NEED(gate_codes); NEED(gate_scales); NEED(up_codes); NEED(up_scales);
+  NEED(down_codes); NEED(down_scales); NEED(y_perm);
+  NEED_WS(ws_bytes, ffn_q4_ws_bytes(*d));
+  return hip_status(launch_ffn_q4(*d, group, x, x_perm, offsets, {gate_codes, gate_scales}, {up_codes, up_scales},
+                                  {down_codes, down_scales}, y_perm, ws, stream),
+                    "moe_expert_ffn_q4");
 }
 
 moe_status moe_permute_bwd(const moe_desc* d, const void* dx_perm, const int32_t* slot_to_row, const float* dlogits,

@@ -6,7 +6,7 @@
 // 2^-37 of the sum) so do other batches; else a score can differ in its last fp32 bit, in about one of 10^8, and a
 // selection that hangs on that bit with it. Selection happens at wavefront level: k rounds of a 64-lane maximum over
 // order-preserving keys, ties to the lowest expert index.
-#include "pcmoe_internal.h"
+#include "expert_ops.h"
 #include <math.h>
 #include <algorithm>
 
@@ -40,6 +40,146 @@ __device__ __forceinline__ float key_score(uint32_t k) {
   return k == 0u ? -INFINITY : __uint_as_float((k >> 31) ? (k & 0x7fffffffu) : ~k);
 }
 
+// ------------------------------------------------------------------------- gated selection
+// Selection by scores with a balance bias within limited expert groups. An expert's score s is softmax(l) or sigmoid(l) of
+// its fp32 score l above, its choice value s + bias; both are formed in fp64, so that which of two close experts is chosen
+// does not hang on the last bits of an exponential. (Without a bias the experts rank by l itself, the same order.)
+constexpr int NO_EXPERT = 0x7fffffff;  // index of a slot that no expert fills
+
+struct GateArgs {
+  const float* bias;  // [E] or null
+  float scale;
+  int sigmoid, groups, keep, top, group_size;
+  int group_mul;      // e / group_size = e * group_mul >> 16 for e < 256
+};
+
+// Order-preserving key of a choice value: 0 for what is never chosen (NaN, -inf), -0 and +0 alike.
+__device__ __forceinline__ uint64_t choice_key(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v + 0.0);
+  if (!(v > -INFINITY)) return 0ull;
+  return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
+}
+__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
+  const uint32_t hi = wave_max_u32((uint32_t)(v >> 32));
+  const uint32_t lo = wave_max_u32((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
+  return ((uint64_t)hi << 32) | lo;
+}
+__device__ __forceinline__ double wave_sum_f64(double v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+
+// One token: v[qq] is the score of expert lane + 64 qq (-inf past E). `row` is LDS that only this wavefront uses, E
+// doubles of it.
+template <int QE>
+__device__ __forceinline__ void gated_select(const float (&v)[QE], int E, int k, int renorm, const GateArgs& ga,
+                                             double* row, int32_t* __restrict__ idx, float* __restrict__ gw) {
+  const int lane = threadIdx.x & 63;
+  const bool need = ga.bias || (ga.groups > 1 && ga.top == 2);  // are scores of all the experts needed?
+  double z = 1.0;                                                // softmax: the largest logit and the sum over E
+  float m = 0.f;
+  double sc[QE];
+  if (!ga.sigmoid && (need || !renorm)) {
+    float mm = v[0];
+#pragma unroll
+    for (int qq = 1; qq < QE; ++qq) mm = fmaxf(mm, v[qq]);
+    m = wave_max(mm);
+    double zz = 0.0;
+#pragma unroll
+    for (int qq = 0; qq < QE; ++qq) {
+      sc[qq] = v[qq] > -INFINITY ? exp((double)v[qq] - (double)m) : 0.0;  // nothing of a masked or NaN expert
+      zz += sc[qq];
+    }
+    z = wave_sum_f64(zz);
+  }
+  uint64_t key[QE];
+  double worth[QE];  // what a group's value is made of
+#pragma unroll
+  for (int qq = 0; qq < QE; ++qq) {
+    const int e = lane + 64 * qq;
+    double c = (double)v[qq];
+    worth[qq] = c;
+    if (need) {
+      worth[qq] = ga.sigmoid ? 1.0 / (1.0 + exp(-c)) : sc[qq] / z;
+      if (ga.bias) {
+        worth[qq] += (double)(e < E ? ga.bias[e] : 0.f);
+        c = worth[qq];
+      }
+    }
+    key[qq] = e < E && v[qq] > -INFINITY ? choice_key(c) : 0ull;
+  }
+  if (ga.groups > 1) {
+    // lane g finds the largest and the second largest value of group g; the lanes start at different experts of theirs,
+    // on different LDS banks
+#pragma unroll
+    for (int qq = 0; qq < QE; ++qq)
+      if (lane + 64 * qq < E) row[lane + 64 * qq] = key[qq] ? worth[qq] : -INFINITY;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    double a = -INFINITY, b = -INFINITY;
+    if (lane < ga.groups) {
+      int o = lane % ga.group_size;
+      for (int n = 0; n < ga.group_size; ++n) {
+        const double w = row[lane * ga.group_size + o];
+        b = fmax(b, fmin(a, w));
+        a = fmax(a, w);
+        if (++o == ga.group_size) o = 0;
+      }
+      if (ga.top == 2 && b > -INFINITY) a += b;
+    }
+    const uint64_t mine = choice_key(a);
+    int ahead = 0;  // groups that come before this one: of equals, the lower index first
+    for (int g = 0; g < ga.groups; ++g) {
+      const uint64_t o = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), g) << 32) |
+                         (uint32_t)__builtin_amdgcn_readlane((int)mine, g);
+      ahead += o > mine || (o == mine && g < lane);
+    }
+    const uint64_t open = __ballot(lane < ga.groups && ahead < ga.keep);
+#pragma unroll
+    for (int qq = 0; qq < QE; ++qq)
+      if (!((open >> (((lane + 64 * qq) * ga.group_mul) >> 16 & 63)) & 1)) key[qq] = 0ull;
+  }
+  int myi = NO_EXPERT;
+  float myl = -INFINITY;
+  for (int j = 0; j < k; ++j) {
+    uint64_t mx = key[0];
+#pragma unroll
+    for (int qq = 1; qq < QE; ++qq) mx = key[qq] > mx ? key[qq] : mx;
+    mx = wave_max_u64(mx);
+    if (mx == 0ull) break;  // nothing is left to choose from
+    int best = NO_EXPERT;
+    float l = 0.f;
+#pragma unroll
+    for (int qq = QE - 1; qq >= 0; --qq) {
+      const uint64_t bl = __ballot(key[qq] == mx);
+      if (bl) {
+        const int ln = __builtin_ctzll(bl);
+        best = 64 * qq + ln;
+        l = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v[qq]), ln));
+      }
+    }
+#pragma unroll
+    for (int qq = 0; qq < QE; ++qq)
+      if (lane + 64 * qq == best) key[qq] = 0ull;
+    if (lane == j) {
+      myi = best;
+      myl = l;
+    }
+  }
+  const bool filled = lane < k && myi != NO_EXPERT;
+  if (!ga.sigmoid && renorm) m = wave_max(myl);  // any shift will do: the largest of the chosen
+  double s = 0.0;
+  if (filled) s = ga.sigmoid ? 1.0 / (1.0 + exp(-(double)myl)) : exp((double)myl - (double)m) / z;
+  if (renorm) {
+    const double t = wave_sum_f64(s);
+    s = t == 0.0 ? 0.0 : s / t;  // every chosen score underflows (or nothing is chosen): no weight
+  }
+  if (lane < k) {
+    idx[lane] = myi;
+    gw[lane] = (float)(s * (double)ga.scale);
+  }
+}
+
 // Scores of NTOK = TB * TT tokens against all E experts on the fp64 matrix cores, then top-k and gate weights.
 // The WE x WK wavefronts split the experts into WE runs of 16 * NET and d into WK ranges of column steps (4 chunks
 // each); the WK fp64 partial sums of a score are added in a fixed order, the bias is added in fp64 and the result is
@@ -56,12 +196,12 @@ __device__ __forceinline__ float key_score(uint32_t k) {
 // are 14 us of a CU's fp64 rate, whatever the token count. Long batches take TT token tiles per wavefront: an expert
 // chunk is then converted once for TT products, a token chunk once for NET.
 // PF column steps of loads are in flight per wavefront.
-template <typename T, int TB, int TT, int NET, int WE, int WK, int PF>
+template <typename T, bool GATED, int TB, int TT, int NET, int WE, int WK, int PF>
 __global__ __launch_bounds__(64 * WE * WK) void route_fwd_kernel(const T* __restrict__ x, const T* __restrict__ wr,
                                                               const float* __restrict__ bias, int bias_div, int Tn,
                                                               int d, int E, int k, int renorm,
                                                               float* __restrict__ logits, int32_t* __restrict__ idx,
-                                                              float* __restrict__ gw) {
+                                                              float* __restrict__ gw, GateArgs ga) {
   constexpr int EP = EPC<T>::value;        // elements per 16-byte chunk
   constexpr int EW = 16 * NET * WE + 1;    // padded expert stride of the partial-sum table
   constexpr int NTOK = TB * TT;
@@ -192,6 +332,10 @@ __global__ __launch_bounds__(64 * WE * WK) void route_fwd_kernel(const T* __rest
         key[qq] = score_key(L);
       }
     }
+    if constexpr (GATED) {
+      gated_select<QE>(v, E, k, renorm, ga, part + row * EW, idx + (size_t)tt * k, gw + (size_t)tt * k);
+      continue;
+    }
     float myv = -INFINITY;
     int myi = 0;
     for (int j = 0; j < k; ++j) {
@@ -232,26 +376,26 @@ __global__ __launch_bounds__(64 * WE * WK) void route_fwd_kernel(const T* __rest
   }
 }
 
-template <typename T, int TB, int TT, int NET, int WE, int WK, int PF>
+template <typename T, bool GATED, int TB, int TT, int NET, int WE, int WK, int PF>
 static hipError_t route_fwd_run(const moe_desc& d, const void* x, const void* wr, const float* bias, int div,
-                                float* logits, int32_t* idx, float* w, hipStream_t s) {
+                                float* logits, int32_t* idx, float* w, const GateArgs& ga, hipStream_t s) {
   constexpr int NTOK = TB * TT;
   constexpr size_t LDS = (size_t)WK * NTOK * (16 * NET * WE + 1) * sizeof(double);
   static_assert(LDS <= 160 * 1024, "partial-sum table");
-  auto kern = route_fwd_kernel<T, TB, TT, NET, WE, WK, PF>;
+  auto kern = route_fwd_kernel<T, GATED, TB, TT, NET, WE, WK, PF>;
   if (LDS > 65536) {
     static std::atomic<uint64_t> lds_set{0};
     if (hipError_t e = lds_limit_once((const void*)kern, (int)LDS, lds_set); e != hipSuccess) return e;
   }
-  KernelTimer kt("route_fwd", s);
+  KernelTimer kt(GATED ? "route_gated" : "route_fwd", s);
   hipLaunchKernelGGL(kern, dim3((d.T + NTOK - 1) / NTOK), dim3(64 * WE * WK), LDS, s, (const T*)x, (const T*)wr, bias,
-                     div, d.T, d.d_model, d.n_experts, d.top_k, d.renormalize, logits, idx, w);
+                     div, d.T, d.d_model, d.n_experts, d.top_k, d.renormalize, logits, idx, w, ga);
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, bool GATED>
 static hipError_t route_fwd_t(const moe_desc& d, const void* x, const void* wr, const float* bias, int bg,
-                              float* logits, int32_t* idx, float* w, hipStream_t s) {
+                              float* logits, int32_t* idx, float* w, const GateArgs& ga, hipStream_t s) {
   const int E = d.n_experts;
   const int div = d.T / (bg > 0 ? bg : 1);
   // Tokens per workgroup: the fewest (1, 4, 16 or 32) whose workgroups are at most one per CU, since a workgroup costs
@@ -266,7 +410,7 @@ static hipError_t route_fwd_t(const moe_desc& d, const void* x, const void* wr, 
   // Wavefronts: as many as fit the LDS table and, at 16 of them, 128 VGPRs without spills; 4 to a workgroup of 16 tokens
   // in long batches, where several workgroups share a CU.
 #define RT(TB, TT, NET, WE, WK, PF) \
-  return route_fwd_run<T, TB, TT, NET, WE, WK, PF>(d, x, wr, bias, div, logits, idx, w, s)
+  return route_fwd_run<T, GATED, TB, TT, NET, WE, WK, PF>(d, x, wr, bias, div, logits, idx, w, ga, s)
   const int cus = device_cus();
   const int r16 = (d.T + 16 * cus - 1) / (16 * cus), r32 = (r16 + 1) / 2;  // rounds of 16 and of 32 tokens per CU
   const bool by32 = r32 == 1 || ((E > 32 || d.dtype == MOE_F32) && 20 * r32 <= 11 * r16);
@@ -304,8 +448,18 @@ static hipError_t route_fwd_t(const moe_desc& d, const void* x, const void* wr, 
 
 hipError_t launch_route_fwd(const moe_desc& d, const void* x, const void* wr, const float* bias, int bg,
                             float* logits, int32_t* idx, float* w, hipStream_t s) {
-  if (d.dtype == MOE_BF16) return route_fwd_t<bf16>(d, x, wr, bias, bg, logits, idx, w, s);
-  return route_fwd_t<float>(d, x, wr, bias, bg, logits, idx, w, s);
+  const GateArgs none{};
+  if (d.dtype == MOE_BF16) return route_fwd_t<bf16, false>(d, x, wr, bias, bg, logits, idx, w, none, s);
+  return route_fwd_t<float, false>(d, x, wr, bias, bg, logits, idx, w, none, s);
+}
+
+hipError_t launch_route_gated(const moe_desc& d, const moe_gate& g, const void* x, const void* wr, const float* bias,
+                              int bg, const float* select_bias, float* logits, int32_t* idx, float* w, hipStream_t s) {
+  const int size = d.n_experts / g.n_groups;
+  const GateArgs ga{select_bias, g.scale, g.score == MOE_SCORE_SIGMOID, g.n_groups, g.topk_groups, g.group_top, size,
+                    (65536 + size - 1) / size};
+  if (d.dtype == MOE_BF16) return route_fwd_t<bf16, true>(d, x, wr, bias, bg, logits, idx, w, ga, s);
+  return route_fwd_t<float, true>(d, x, wr, bias, bg, logits, idx, w, ga, s);
 }
 
 // ------------------------------------------------------------------------------ backward
@@ -375,6 +529,73 @@ __global__ __launch_bounds__(256) void route_dlogits_kernel(int Tn, int E, int k
       for (int n = 0; n < NQ; ++n)
         if (lane + 64 * n < E) dl[(size_t)t * E + lane + 64 * n] = p[n] * (g[n] - S);
     }
+  }
+}
+
+// ... of the gated routing (one wavefront per token). With w_j the returned weight of slot j, g_j its gradient, c the scale:
+//   renormalised: dl_j = w_j (g_j - sum_i w_i g_i / c), for sigmoid scores times (1 - s_j);
+//   sigmoid:      dl_j = w_j (1 - s_j) g_j;       softmax: dl_e = p_e (c g_e - sum_i c p_i g_i) over all the experts.
+// 1 - s is formed as sigmoid(-l), which does not cancel. Slots that no expert fills give nothing.
+__global__ __launch_bounds__(256) void gate_dlogits_kernel(int Tn, int E, int k, int renorm, int sigmoid, float scale,
+                                                           const float* __restrict__ logits,
+                                                           const int32_t* __restrict__ idx,
+                                                           const float* __restrict__ gw,
+                                                           const float* __restrict__ dgate, float* __restrict__ dl) {
+  constexpr int NQ = 4;  // E <= 256
+  const int lane = threadIdx.x & 63;
+  const int wave = (blockIdx.x * blockDim.x + threadIdx.x) >> 6;
+  const int nwaves = (gridDim.x * blockDim.x) >> 6;
+  for (int t = wave; t < Tn; t += nwaves) {
+    float wj = 0.f, gj = 0.f;
+    int ij = NO_EXPERT;
+    if (lane < k) {
+      ij = idx[(size_t)t * k + lane];
+      if ((unsigned)ij < (unsigned)E) {
+        wj = gw[(size_t)t * k + lane];
+        gj = dgate[(size_t)t * k + lane];
+      }
+    }
+    float out[NQ] = {0.f, 0.f, 0.f, 0.f};
+    const bool dense = !renorm && !sigmoid;
+    float val = dense ? scale * gj : gj;  // what slot `lane` adds to its expert
+    if (!dense) {
+      if (renorm) val -= wave_sum(wj * gj) / scale;
+      val *= wj;
+      if (sigmoid && (unsigned)ij < (unsigned)E) val /= 1.f + expf(logits[(size_t)t * E + ij]);
+    }
+    for (int jj = 0; jj < k; ++jj) {
+      const int i2 = __builtin_amdgcn_readlane(ij, jj);
+      const float g2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(val), jj));
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+        if (lane + 64 * n == i2) out[n] = g2;
+    }
+    if (dense) {
+      float p[NQ], m = -INFINITY, zp = 0.f, spg = 0.f;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        p[n] = lane + 64 * n < E ? logits[(size_t)t * E + lane + 64 * n] : -INFINITY;
+        m = fmaxf(m, p[n]);
+      }
+      m = wave_max(m);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        p[n] = p[n] > -INFINITY ? expf(p[n] - m) : 0.f;
+        zp += p[n];
+      }
+      const float z = wave_sum(zp);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        p[n] = z == 0.f ? 0.f : p[n] / z;  // z = 0: every expert is masked
+        spg += p[n] * out[n];
+      }
+      spg = wave_sum(spg);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) out[n] = p[n] * (out[n] - spg);
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+      if (lane + 64 * n < E) dl[(size_t)t * E + lane + 64 * n] = out[n];
   }
 }
 
@@ -601,18 +822,12 @@ size_t route_bwd_ws_bytes(const moe_desc& d) {
   return align256((size_t)nch * d.n_experts * d.d_model * sizeof(float));
 }
 
+static unsigned token_blocks(const moe_desc& d) { return std::min((d.T + 3) / 4, 4096); }
+
+// dW_router from the gradients of the scores.
 template <typename T>
-static hipError_t route_bwd_t(const moe_desc& d, const void* x, const float* logits, const int32_t* idx,
-                              const float* w, const float* dgate, float* dl, float* dwr, void* ws,
-                              hipStream_t s) {
+static hipError_t route_dw_t(const moe_desc& d, const void* x, const float* dl, float* dwr, void* ws, hipStream_t s) {
   const int E = d.n_experts;
-  {
-    KernelTimer kt("route_dlogits", s);
-    int blocks = (d.T + 3) / 4;
-    if (blocks > 4096) blocks = 4096;
-    hipLaunchKernelGGL(route_dlogits_kernel, dim3(blocks), dim3(256), 0, s, d.T, E, d.top_k, d.renormalize,
-                       logits, idx, w, dgate, dl);
-  }
   int nch, tpc;
   bool wide;
   route_bwd_chunks(d, &nch, &tpc, &wide);
@@ -654,10 +869,30 @@ static hipError_t route_bwd_t(const moe_desc& d, const void* x, const float* log
   return hipGetLastError();
 }
 
+static hipError_t route_dw(const moe_desc& d, const void* x, const float* dl, float* dwr, void* ws, hipStream_t s) {
+  if (d.dtype == MOE_BF16) return route_dw_t<bf16>(d, x, dl, dwr, ws, s);
+  return route_dw_t<float>(d, x, dl, dwr, ws, s);
+}
+
 hipError_t launch_route_bwd(const moe_desc& d, const void* x, const float* logits, const int32_t* idx,
                             const float* w, const float* dgate, float* dl, float* dwr, void* ws, hipStream_t s) {
-  if (d.dtype == MOE_BF16) return route_bwd_t<bf16>(d, x, logits, idx, w, dgate, dl, dwr, ws, s);
-  return route_bwd_t<float>(d, x, logits, idx, w, dgate, dl, dwr, ws, s);
+  {
+    KernelTimer kt("route_dlogits", s);
+    hipLaunchKernelGGL(route_dlogits_kernel, dim3(token_blocks(d)), dim3(256), 0, s, d.T, d.n_experts, d.top_k,
+                       d.renormalize, logits, idx, w, dgate, dl);
+  }
+  return route_dw(d, x, dl, dwr, ws, s);
+}
+
+hipError_t launch_route_gated_bwd(const moe_desc& d, const moe_gate& g, const void* x, const float* logits,
+                                  const int32_t* idx, const float* w, const float* dgate, float* dl, float* dwr,
+                                  void* ws, hipStream_t s) {
+  {
+    KernelTimer kt("gate_dlogits", s);
+    hipLaunchKernelGGL(gate_dlogits_kernel, dim3(token_blocks(d)), dim3(256), 0, s, d.T, d.n_experts, d.top_k,
+                       d.renormalize, (int)(g.score == MOE_SCORE_SIGMOID), g.scale, logits, idx, w, dgate, dl);
+  }
+  return route_dw(d, x, dl, dwr, ws, s);
 }
 
 }  // namespace pcmoe

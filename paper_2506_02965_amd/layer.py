@@ -4,6 +4,8 @@ Forward (Alg. 3 with the gating of Alg. 7 and the experts of Alg. 6):
     moe_route -> moe_permute -> moe_expert_ffn_fwd -> moe_combine
 Backward (Alg. 5 / Alg. 6 and the owner-side router adjoint):
     moe_combine_bwd -> moe_expert_ffn_bwd -> moe_route_bwd (full layer only) -> moe_permute_bwd
+With a gate, moe_route_gated and moe_route_gated_bwd take the place of the routing calls. With checkpoint=True the forward
+ends in moe_ffn_checkpoint and the backward begins with moe_ffn_restore. forward_q4 runs the experts from 4-bit weights.
 Expert update (the last step of Alg. 6): moe_expert_update over the hosted experts' weights.
 All calls are enqueued on one stream; no per-expert count ever returns to the host.
 """
@@ -28,6 +30,7 @@ class LayerWeights:
     w_up: torch.Tensor
     w_down: torch.Tensor
     dy: Optional[torch.Tensor] = None
+    select_bias: Optional[torch.Tensor] = None   # [E] fp32, gated routing only
 
 
 def torch_dtype(dtype: str):
@@ -46,9 +49,33 @@ def upload(inp, device="cuda") -> LayerWeights:
                         to(inp.w_down), None if inp.dy is None else to(inp.dy))
 
 
+@dataclass
+class Q4Experts:
+    """4-bit codes and group scales of the experts' gate, up and down projections."""
+    group: int
+    gate: tuple
+    up: tuple
+    down: tuple
+
+    @staticmethod
+    def pack(w: LayerWeights, group: int = 64) -> "Q4Experts":
+        def one(t):
+            n, rows, cols = t.shape
+            codes = torch.empty(n, rows // 16, cols // 128, 4, 16, 4, 4, dtype=torch.uint8, device=t.device)
+            scales = torch.empty(n, rows // 16, cols // group, 16, dtype=torch.bfloat16, device=t.device)
+            P.moe_q4_pack(n, rows, cols, group, "bf16" if t.dtype == torch.bfloat16 else "f32", t, codes, scales)
+            return codes, scales
+        return Q4Experts(group, one(w.w_gate), one(w.w_up), one(w.w_down))
+
+
 class MoELayer:
-    def __init__(self, cfg, device="cuda", backward=None, router_backward=None):
+    """gate: a pcmoe.make_gate(...) for gated routing. checkpoint: keep the activations of the backward in 8 bits;
+    `saved`, the buffer of their full form, may then be shared by layers that run one after the other."""
+
+    def __init__(self, cfg, device="cuda", backward=None, router_backward=None, gate=None, checkpoint=False, saved=None):
         self.cfg = cfg
+        self.gate = gate
+        self.checkpoint = checkpoint
         self.device = device
         self.backward_enabled = cfg.backward if backward is None else backward
         self.router_backward = cfg.router_backward if router_backward is None else router_backward
@@ -70,7 +97,12 @@ class MoELayer:
         self.y = torch.empty(T, d, dtype=dt, **kw)
         ws = lambda which: torch.empty(max(P.moe_workspace_size(self.desc, which), 1), dtype=torch.uint8, **kw)
         self.ws_permute = ws(P.MOE_WS_PERMUTE)
-        self.saved = ws(P.MOE_WS_FFN_SAVED)
+        self.saved = ws(P.MOE_WS_FFN_SAVED) if saved is None else saved
+        if checkpoint:
+            self.ckpt = ws(P.MOE_WS_FFN_CKPT)
+        elif saved is not None:
+            raise ValueError("a shared saved buffer needs checkpoint=True: it does not outlive the next layer's forward")
+        self.ws_q4 = None   # of forward_q4, allocated by its first call
         self.ws_ffn_fwd = ws(P.MOE_WS_FFN_FWD)
         if self.backward_enabled:
             G = Eloc + S
@@ -89,6 +121,10 @@ class MoELayer:
 
     # ------------------------------------------------------------------ forward
     def route(self, w: LayerWeights):
+        if self.gate is not None:
+            P.moe_route_gated(self.desc, self.gate, w.x, w.w_router, w.logit_bias, w.bias_groups, w.select_bias,
+                              self.logits, self.topk_idx, self.topk_w)
+            return
         P.moe_route(self.desc, w.x, w.w_router, w.logit_bias, w.bias_groups, self.logits, self.topk_idx, self.topk_w)
 
     def permute(self, w: LayerWeights):
@@ -98,6 +134,8 @@ class MoELayer:
     def ffn_fwd(self, w: LayerWeights):
         P.moe_expert_ffn_fwd(self.desc, w.x, self.x_perm, self.offsets, w.w_gate, w.w_up, w.w_down, self.y_perm,
                              self.saved, self.ws_ffn_fwd, self.ws_ffn_fwd.numel())
+        if self.checkpoint:
+            P.moe_ffn_checkpoint(self.desc, self.offsets, self.saved, self.ckpt, self.ckpt.numel())
 
     def combine(self):
         P.moe_combine(self.desc, self.y_perm, self.slot_to_row, self.topk_w, self.y)
@@ -109,16 +147,34 @@ class MoELayer:
         self.combine()
         return self.y
 
+    def forward_q4(self, w: LayerWeights, q: Q4Experts):
+        """The forward with the experts' 4-bit weights (inference: nothing is saved; w's expert weights are not read)."""
+        if self.ws_q4 is None:
+            self.ws_q4 = torch.empty(P.moe_workspace_size(self.desc, P.MOE_WS_FFN_Q4), dtype=torch.uint8,
+                                     device=self.device)
+        self.route(w)
+        self.permute(w)
+        P.moe_expert_ffn_q4(self.desc, q.group, w.x, self.x_perm, self.offsets, *q.gate, *q.up, *q.down, self.y_perm,
+                            self.ws_q4, self.ws_q4.numel())
+        self.combine()
+        return self.y
+
     # ----------------------------------------------------------------- backward
     def combine_bwd(self, dy):
         P.moe_combine_bwd(self.desc, dy, self.y_perm, self.slot_to_row, self.topk_w, self.dy_perm, self.dgate)
 
     def ffn_bwd(self, w: LayerWeights, dy):
+        if self.checkpoint:
+            P.moe_ffn_restore(self.desc, self.offsets, self.ckpt, self.ckpt.numel(), self.saved)
         P.moe_expert_ffn_bwd(self.desc, w.x, self.x_perm, dy, self.dy_perm, self.offsets, w.w_gate, w.w_up, w.w_down,
                              self.saved, self.dx_perm, self.dw_gate, self.dw_up, self.dw_down, self.ws_ffn_bwd,
                              self.ws_ffn_bwd.numel())
 
     def route_bwd(self, w: LayerWeights):
+        if self.gate is not None:
+            P.moe_route_gated_bwd(self.desc, self.gate, w.x, self.logits, self.topk_idx, self.topk_w, self.dgate,
+                                  self.dlogits, self.dw_router, self.ws_route_bwd, self.ws_route_bwd.numel())
+            return
         P.moe_route_bwd(self.desc, w.x, self.logits, self.topk_idx, self.topk_w, self.dgate, self.dlogits,
                         self.dw_router, self.ws_route_bwd, self.ws_route_bwd.numel())
 

@@ -15,12 +15,18 @@ LIB_PATH = os.path.join(HERE, "libpcmoe.so")
 
 MOE_OK, MOE_ERR_INVALID_ARGUMENT, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE_TOO_SMALL, MOE_ERR_HIP = range(5)
 MOE_F32, MOE_BF16 = 0, 1
-MOE_WS_PERMUTE, MOE_WS_FFN_SAVED, MOE_WS_FFN_FWD, MOE_WS_FFN_BWD, MOE_WS_ROUTE_BWD = range(5)
+(MOE_WS_PERMUTE, MOE_WS_FFN_SAVED, MOE_WS_FFN_FWD, MOE_WS_FFN_BWD, MOE_WS_ROUTE_BWD, MOE_WS_FFN_Q4,
+ MOE_WS_FFN_CKPT) = range(7)
+MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID = 0, 1
+MOE_NO_EXPERT = 0x7fffffff
 
 # every symbol include/pcmoe.h declares
 EXPORTS = ("moe_workspace_size", "moe_route", "moe_permute", "moe_permute_noalloc", "moe_expert_ffn_fwd", "moe_combine", "moe_combine_bwd",
            "moe_expert_ffn_bwd", "moe_route_bwd", "moe_permute_bwd", "moe_expert_update", "moe_kernel_timing",
            "moe_kernel_timing_select", "moe_kernel_timing_report", "moe_status_string", "moe_last_error")
+# ... and include/pcmoe_ext.h
+EXPORTS_EXT = ("moe_route_gated", "moe_route_gated_bwd", "moe_ffn_checkpoint", "moe_ffn_restore", "moe_q4_pack",
+               "moe_q4_unpack", "moe_expert_ffn_q4")
 MOE_OPT_SGD, MOE_OPT_ADAMW = 0, 1
 
 
@@ -35,6 +41,18 @@ class moe_opt(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("lr", ctypes.c_float), ("beta1", ctypes.c_float),
                 ("beta2", ctypes.c_float), ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float),
                 ("step", ctypes.c_int32)]
+
+
+class moe_gate(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("topk_groups", ctypes.c_int32),
+                ("group_top", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+def make_gate(score="softmax", n_groups=1, topk_groups=1, group_top=1, scale=1.0) -> moe_gate:
+    kinds = {"softmax": MOE_SCORE_SOFTMAX, "sigmoid": MOE_SCORE_SIGMOID}
+    if score not in kinds:
+        raise ValueError(f"score {score!r} is not one of {sorted(kinds)}")
+    return moe_gate(kinds[score], n_groups, topk_groups, group_top, scale)
 
 
 def make_opt(kind="adamw", lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, step=1) -> moe_opt:
@@ -71,6 +89,13 @@ def lib():
             "moe_route_bwd": (_INT, [D, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _SZ, _VP]),
             "moe_permute_bwd": (_INT, [D, _VP, _VP, _VP, _VP, _VP, _VP]),
             "moe_expert_update": (_INT, [D, ctypes.POINTER(moe_opt)] + [_VP] * 9 + [_VP]),
+            "moe_route_gated": (_INT, [D, ctypes.POINTER(moe_gate), _VP, _VP, _VP, _I32] + [_VP] * 5),
+            "moe_route_gated_bwd": (_INT, [D, ctypes.POINTER(moe_gate)] + [_VP] * 8 + [_SZ, _VP]),
+            "moe_ffn_checkpoint": (_INT, [D, _VP, _VP, _VP, _SZ, _VP]),
+            "moe_ffn_restore": (_INT, [D, _VP, _VP, _SZ, _VP, _VP]),
+            "moe_q4_pack": (_INT, [_I32] * 5 + [_VP] * 4),
+            "moe_q4_unpack": (_INT, [_I32] * 5 + [_VP] * 4),
+            "moe_expert_ffn_q4": (_INT, [D, _I32] + [_VP] * 11 + [_SZ, _VP]),
             "moe_kernel_timing": (_INT, [_INT]),
             "moe_kernel_timing_select": (_INT, [ctypes.c_char_p]),
             "moe_kernel_timing_report": (_SZ, [ctypes.c_char_p, _SZ]),
@@ -186,6 +211,51 @@ def moe_expert_update(desc, opt, w_gate, w_up, w_down, dw_gate, dw_up, dw_down, 
     _check("moe_expert_update", lib().moe_expert_update(
         ctypes.byref(desc), ctypes.byref(opt), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(dw_gate), _ptr(dw_up),
         _ptr(dw_down), _ptr(master), _ptr(m), _ptr(v), _stream(stream)))
+
+
+def moe_route_gated(desc, gate, x, w_router, logit_bias, bias_groups, select_bias, logits, topk_idx, topk_w,
+                    stream=None):
+    _check("moe_route_gated", lib().moe_route_gated(
+        ctypes.byref(desc), ctypes.byref(gate), _ptr(x), _ptr(w_router), _ptr(logit_bias), bias_groups,
+        _ptr(select_bias), _ptr(logits), _ptr(topk_idx), _ptr(topk_w), _stream(stream)))
+
+
+def moe_route_gated_bwd(desc, gate, x, logits, topk_idx, topk_w, dgate, dlogits, dw_router, ws, ws_bytes, stream=None):
+    _check("moe_route_gated_bwd", lib().moe_route_gated_bwd(
+        ctypes.byref(desc), ctypes.byref(gate), _ptr(x), _ptr(logits), _ptr(topk_idx), _ptr(topk_w), _ptr(dgate),
+        _ptr(dlogits), _ptr(dw_router), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_ffn_checkpoint(desc, offsets, saved, ckpt, ckpt_bytes, stream=None):
+    _check("moe_ffn_checkpoint", lib().moe_ffn_checkpoint(ctypes.byref(desc), _ptr(offsets), _ptr(saved), _ptr(ckpt),
+                                                          ckpt_bytes, _stream(stream)))
+
+
+def moe_ffn_restore(desc, offsets, ckpt, ckpt_bytes, saved, stream=None):
+    _check("moe_ffn_restore", lib().moe_ffn_restore(ctypes.byref(desc), _ptr(offsets), _ptr(ckpt), ckpt_bytes,
+                                                    _ptr(saved), _stream(stream)))
+
+
+def _dtype(dtype) -> int:
+    return MOE_BF16 if dtype == "bf16" else MOE_F32
+
+
+def moe_q4_pack(n, rows, cols, group, dtype, w, codes, scales, stream=None):
+    _check("moe_q4_pack", lib().moe_q4_pack(n, rows, cols, group, _dtype(dtype), _ptr(w), _ptr(codes), _ptr(scales),
+                                            _stream(stream)))
+
+
+def moe_q4_unpack(n, rows, cols, group, dtype, codes, scales, w, stream=None):
+    _check("moe_q4_unpack", lib().moe_q4_unpack(n, rows, cols, group, _dtype(dtype), _ptr(codes), _ptr(scales), _ptr(w),
+                                                _stream(stream)))
+
+
+def moe_expert_ffn_q4(desc, group, x, x_perm, offsets, gate_codes, gate_scales, up_codes, up_scales, down_codes,
+                      down_scales, y_perm, ws, ws_bytes, stream=None):
+    _check("moe_expert_ffn_q4", lib().moe_expert_ffn_q4(
+        ctypes.byref(desc), group, _ptr(x), _ptr(x_perm), _ptr(offsets), _ptr(gate_codes), _ptr(gate_scales),
+        _ptr(up_codes), _ptr(up_scales), _ptr(down_codes), _ptr(down_scales), _ptr(y_perm), _ptr(ws), ws_bytes,
+        _stream(stream)))
 
 
 def moe_kernel_timing(enable: bool):
