@@ -11,6 +11,7 @@
 #include "expert_ops.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace pcmoe {
 
@@ -20,22 +21,46 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // ----------------------------------------------------------------------------------------------- packing
 
-// Code of a value with |value| = a in units of its scale s: nearest of the eight magnitudes, ties to the even code. The
-// midpoints times s are exact in fp32, so the comparisons decide on the quotient itself.
-__device__ __forceinline__ uint32_t e2m1(float v, float s) {
-  const float a = fabsf(v);
-  uint32_t c = (a > 0.25f * s) + (a >= 0.75f * s && a > 0.f) + (a > 1.25f * s) + (a >= 1.75f * s && a > 0.f) +
-               (a > 2.5f * s) + (a >= 3.5f * s && a > 0.f) + (a > 5.f * s);
-  return c | (v < 0.f ? 8u : 0u);
+// Codes of eight values in units of their scale s: the nearest of the magnitudes, ties to the even code.
+//   fp32: by comparisons with the midpoints times s, which are exact, so they decide on the quotient itself.
+//   bf16: two 8-bit significands' quotient is a midpoint exactly or at least 2^-17 away from it, so the fp32 quotient (one
+//   correction of v * rcp(s): exact where the quotient has few bits) decides, in the hardware's conversion. A third of the
+//   instructions: the comparisons bound the packing (344 us for 470 M weights, 3.4 TB/s).
+__device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float s, float) {
+  uint32_t d = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float a = fabsf(v[e]);
+    const uint32_t c = (a > 0.25f * s) + (a >= 0.75f * s && a > 0.f) + (a > 1.25f * s) + (a >= 1.75f * s && a > 0.f) +
+                       (a > 2.5f * s) + (a >= 3.5f * s && a > 0.f) + (a > 5.f * s);
+    d |= (c | (v[e] < 0.f ? 8u : 0u)) << (4 * e);
+  }
+  return d;
+}
+__device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float s, bf16) {
+  const float up = s < 0x1p-60f ? 0x1p64f : 1.f;  // keeps the reciprocal of a tiny scale finite
+  const float su = s * up, r = s > 0.f ? __builtin_amdgcn_rcpf(su) : 0.f;
+  float t[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float vu = v[e] * up, t0 = vu * r;
+    t[e] = fmaf(fmaf(-t0, su, vu), r, t0);
+  }
+  uint32_t d = 0;
+  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, t[0], t[1], 1.0f, 0);
+  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, t[2], t[3], 1.0f, 1);
+  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, t[4], t[5], 1.0f, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, t[6], t[7], 1.0f, 3);
 }
 
-// One wavefront per 16 x 128 block: lane (q, i) reads the eight k of each dword, the four lanes of a row share each
-// group's largest value.
+// One 16 x 128 block per wavefront and turn: lane (q, i) reads the eight k of each dword, the four lanes of a row share each
+// group's largest value. Magnitudes are compared as integers, which orders infinities and NaN above every number.
 template <typename T>
 __global__ __launch_bounds__(256) void q4_pack_kernel(int64_t blocks, int kb, int group, const T* __restrict__ w,
                                                       char* __restrict__ codes, bf16* __restrict__ scales) {
-  const int lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
-  const int64_t b = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int XC = 8 / EPC<T>::value;
+  const int lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15, per = group / 32;  // dwords of a group
+  const int64_t b = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (b >= blocks) return;
   const int64_t nb = b / kb;
   const int k0 = (int)(b - nb * kb);
@@ -44,38 +69,28 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(int64_t blocks, int kb, in
 #pragma unroll
   for (int s = 0; s < 4; ++s)
 #pragma unroll
-    for (int c = 0; c < 8 / EPC<T>::value; ++c)
-      chunk_to_f<T>(ld_chunk(src + 32 * s + c * EPC<T>::value), v[s] + c * EPC<T>::value);
-  float top[4];
+    for (int c = 0; c < XC; ++c)
+      chunk_to_f<T>(ld_chunk_nt(src + 32 * s + c * EPC<T>::value), v[s] + c * EPC<T>::value);
+  uint32_t top[4];
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
-    float t = 0.f;
-    bool bad = false;
+    uint32_t t = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      t = fmaxf(t, fabsf(v[s][e]));
-      bad |= !(fabsf(v[s][e]) < INFINITY);
-    }
-    if (bad) t = INFINITY;
-    t = fmaxf(t, __shfl_xor(t, 16, 64));
-    top[s] = fmaxf(t, __shfl_xor(t, 32, 64));
+    for (int e = 0; e < 8; ++e) t = max(t, __float_as_uint(v[s][e]) & 0x7fffffffu);
+    t = max(t, (uint32_t)__shfl_xor((int)t, 16, 64));
+    top[s] = max(t, (uint32_t)__shfl_xor((int)t, 32, 64));
   }
-  const int per = group / 32;  // dwords of a group
   if (per >= 2) {
-    top[0] = top[1] = fmaxf(top[0], top[1]);
-    top[2] = top[3] = fmaxf(top[2], top[3]);
+    top[0] = top[1] = max(top[0], top[1]);
+    top[2] = top[3] = max(top[2], top[3]);
   }
-  if (per == 4) top[0] = top[1] = top[2] = top[3] = fmaxf(top[0], top[2]);
+  if (per == 4) top[0] = top[1] = top[2] = top[3] = max(top[0], top[2]);
   Chunk out;
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
     // a group with a NaN or an infinity: its scale, and with it every product, is NaN
-    const bf16 sb = top[s] < INFINITY ? f2bf(top[s] / 6.f) : (bf16)0x7fc0;
-    const float sc = bf2f(sb);
-    uint32_t d = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) d |= e2m1(v[s][e], sc) << (4 * e);
-    out.w[s] = d;
+    const bf16 sb = top[s] < 0x7f800000u ? f2bf(__uint_as_float(top[s]) / 6.f) : (bf16)0x7fc0;
+    out.w[s] = codes_of(v[s], bf2f(sb), T{});
     if (q == 0 && s % per == 0) scales[((nb * kb + k0) * (4 / per) + s / per) * 16 + i] = sb;
   }
   st_chunk(codes + b * 1024 + lane * 16, out);
@@ -132,6 +147,19 @@ struct Q4Args {
   const bf16* scales[2];
 };
 
+// Inclusive sum over the lanes (DPP: shifts within rows of 16, then row broadcasts).
+__device__ __forceinline__ int wave_scan(int v) {
+#define PCMOE_DPP_ADD(ctrl, rows) v += __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false)
+  PCMOE_DPP_ADD(0x111, 0xf);  // row_shr 1, 2, 4, 8
+  PCMOE_DPP_ADD(0x112, 0xf);
+  PCMOE_DPP_ADD(0x114, 0xf);
+  PCMOE_DPP_ADD(0x118, 0xf);
+  PCMOE_DPP_ADD(0x142, 0xa);  // row_bcast 15 into rows 1 and 3, row_bcast 31 into rows 2 and 3
+  PCMOE_DPP_ADD(0x143, 0xc);
+#undef PCMOE_DPP_ADD
+  return v;
+}
+
 // Workgroup -> (group, chunk of its rows, column block), from the offsets alone. Lane l counts the chunks of groups l,
 // l + 64, ... Consecutive tiles, the row chunks of one column block first, stay on one XCD, whose L2 serves a block's
 // repeated reads.
@@ -155,13 +183,7 @@ __device__ __forceinline__ bool q4_tile(const Q4Args& p, int bid, int chunk, Q4T
   for (int s = 0; s < NS; ++s) {
     incl[s] = 0;
     if (s < ns) {
-      int v = (n[s] + chunk - 1) / chunk;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(v, o, 64);
-        if (lane >= o) v += u;
-      }
-      incl[s] = v + total;
+      incl[s] = wave_scan((n[s] + chunk - 1) / chunk) + total;
       total = __builtin_amdgcn_readlane(incl[s], 63);
     }
   }
@@ -221,149 +243,320 @@ __device__ __forceinline__ void split(const XChunk<float>& x, Chunk (&out)[3]) {
   }
 }
 
+// 16 or 2 bytes at byte voff + soff of a buffer, soff wave-uniform; zeros where voff is past the end.
+__device__ __forceinline__ Chunk buf_ld16_at(__amdgpu_buffer_rsrc_t r, int voff, int soff) {
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(Chunk, __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 0)));
+}
+__device__ __forceinline__ uint32_t buf_ld2_at(__amdgpu_buffer_rsrc_t r, int voff, int soff) {
+  return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, voff, soff, 0);
+}
+
+// The scales of a block's 16 weight rows for the SG groups of a step. Lane (q, i) has read row i's scale of group q % SG;
+// out[z] is row i's scale of group z in every lane.
+template <int SG>
+__device__ __forceinline__ void spread_scales(uint32_t v, float (&out)[SG]) {
+  if constexpr (SG == 1) {
+    out[0] = __uint_as_float(v << 16);
+  } else {
+    uint32_t lo = v << 16, hi = lo;  // rows of 16 lanes hold groups 0 1 0 1 or 0 1 2 3
+    if constexpr (SG == 4) {
+      const auto h = __builtin_amdgcn_permlane32_swap(lo, lo, false, false);  // 0 1 0 1 and 2 3 2 3
+      lo = h[0];
+      hi = h[1];
+    }
+    const auto a = __builtin_amdgcn_permlane16_swap(lo, lo, false, false);  // 0 0 0 0 and 1 1 1 1
+    out[0] = __uint_as_float(a[0]);
+    out[1] = __uint_as_float(a[1]);
+    if constexpr (SG == 4) {
+      const auto b = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+      out[2] = __uint_as_float(b[0]);
+      out[3] = __uint_as_float(b[1]);
+    }
+  }
+}
+
 __device__ __forceinline__ float silu_of(float g, bf16) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
 __device__ __forceinline__ float silu_of(float g, float) { return g / (1.f + expf(-g)); }
 
-template <typename T>
-__device__ __forceinline__ void store4(T* p, const floatx4& v) {
-  if constexpr (std::is_same<T, bf16>::value)
-    *reinterpret_cast<uint2*>(p) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-  else
-    *reinterpret_cast<floatx4*>(p) = v;
-}
-
-// Up to 16 MT rows of a group against 16 NB columns of the output (GU: of gate and of up). The four wavefronts take a
-// quarter of K each, 128 k at a time with D steps of loads in flight; their sums meet in LDS and are added in wavefront
-// order. SG = 128 / group.
-constexpr int Q4_W = 4;
-template <typename T, bool GU, int MT, int NB, int SG, int D>
-__global__ __launch_bounds__(64 * Q4_W) void q4_split_kernel(Q4Args p) {
+// Up to 16 rows of a group against 16 NB columns of the output (GU: of gate and of up): the Q4_KS wavefronts take a part of K
+// each, 128 k at a time, read rows and weights straight into MFMA operands and share nothing until their sums meet in LDS
+// and are added in wavefront order. SG = 128 / group. Bound by the round trips of the loads: a wavefront's steps are few, so
+// the next one's loads, issued behind a step's products, are all that is in flight.
+constexpr int Q4_KS = 8;
+template <typename T, bool GU, int NB, int SG>
+__global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
   constexpr int NM = GU ? 2 : 1, NP = Parts<T>::N, XC = 8 / EPC<T>::value;
-  __shared__ __align__(16) floatx4 red[Q4_W][NM * NB * MT][64];
+  __shared__ __align__(16) floatx4 red[Q4_KS][NM * NB][64];
   Q4Tile t;
-  if (!q4_tile(p, blockIdx.x, 16 * MT, t)) return;
+  if (!q4_tile(p, blockIdx.x, 16, t)) return;
   const int lane = threadIdx.x & 63, q = lane >> 4, li = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int K = GU ? p.d : p.f, N = GU ? p.f : p.d, units = K / 128, KB = K * (int)sizeof(T);
   const bool routed = t.g < p.Eloc;
   const int64_t rs = routed ? (int64_t)t.row0 : p.shared0 + (int64_t)(t.g - p.Eloc) * p.T;
   const char* xb = GU ? (routed ? (const char*)p.xp + (int64_t)t.row0 * KB : (const char*)p.x) : (const char*)p.h + rs * KB;
-  const int m0 = t.ch * 16 * MT, m_rows = min(t.rows - m0, 16 * MT);
-  const auto xr = buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB);
-  const int u0 = (int)((int64_t)units * w / Q4_W), u1 = (int)((int64_t)units * (w + 1) / Q4_W);
+  const int m0 = t.ch * 16, m_rows = min(t.rows - m0, 16);
+  const auto xr = buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB);  // rows past the last read as zeros
+  const int u0 = (int)((int64_t)units * w / Q4_KS), u1 = (int)((int64_t)units * (w + 1) / Q4_KS);
   const int nb0 = t.nb * NB;  // first 16-column block
-  const char* cb[NM];
-  const char* sb[NM];
+  __amdgpu_buffer_rsrc_t cr[NM], sr[NM];
 #pragma unroll
   for (int a = 0; a < NM; ++a) {
     const int64_t blk = ((int64_t)t.g * (N / 16) + nb0) * units;
-    cb[a] = p.codes[a] + blk * 1024 + lane * 16;
-    sb[a] = (const char*)p.scales[a] + blk * SG * 32 + q * 8;
+    cr[a] = buf_rsrc(p.codes[a] + blk * 1024, (size_t)NB * units * 1024);
+    sr[a] = buf_rsrc((const char*)p.scales[a] + blk * SG * 32, (size_t)NB * units * SG * 32);
   }
   struct Stage {
     Chunk c[NM][NB];
-    uint2 s[NM][NB][SG];
-    XChunk<T> x[4][MT];
-  };
-  auto load = [&](int u, Stage& st) {
-    if (u >= u1) return;
+    uint32_t s[NM][NB];
+    XChunk<T> x[4];
+  } st;
+  auto load = [&](int u) {
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int c = 0; c < XC; ++c)
-          st.x[s][m].c[c] = buf_ld16(xr, (16 * m + li) * KB + (u * 128 + 32 * s + 8 * q) * (int)sizeof(T) + 16 * c);
+      for (int c = 0; c < XC; ++c)
+        st.x[s].c[c] = buf_ld16_at(xr, li * KB + (32 * s + 8 * q) * (int)sizeof(T) + 16 * c, u * 128 * (int)sizeof(T));
 #pragma unroll
     for (int a = 0; a < NM; ++a)
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        const int64_t o = (int64_t)i * units + u;
-        st.c[a][i] = ld_chunk(cb[a] + o * 1024);
-#pragma unroll
-        for (int z = 0; z < SG; ++z) st.s[a][i][z] = *reinterpret_cast<const uint2*>(sb[a] + (o * SG + z) * 32);
+        const int o = i * units + u;
+        st.c[a][i] = buf_ld16_at(cr[a], lane * 16, o * 1024);
+        st.s[a][i] = buf_ld2_at(sr[a], (q % SG) * 32 + 2 * li, o * SG * 32);
       }
   };
-  floatx4 acc[NM][NB][MT];
+  floatx4 acc[NM][NB];
 #pragma unroll
   for (int a = 0; a < NM; ++a)
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+    for (int i = 0; i < NB; ++i) acc[a][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+  if (u0 < u1) load(u0);
+  for (int u = u0; u < u1; ++u) {
+    Chunk xs[4][NP];
 #pragma unroll
-      for (int m = 0; m < MT; ++m) acc[a][i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
-  auto mul = [&](const Stage& st) {
-    Chunk xs[4][MT][NP];
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int m = 0; m < MT; ++m) split(st.x[s][m], xs[s][m]);
+    for (int s = 0; s < 4; ++s) split(st.x[s], xs[s]);
 #pragma unroll
     for (int a = 0; a < NM; ++a)
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
+      for (int i = 0; i < NB; ++i) {
+        float sc[SG];
+        spread_scales<SG>(st.s[a][i], sc);
 #pragma unroll
         for (int z = 0; z < SG; ++z) {
-          floatx4 sum[MT];
-#pragma unroll
-          for (int m = 0; m < MT; ++m) sum[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+          floatx4 sum = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int s = z * 4 / SG; s < (z + 1) * 4 / SG; ++s) {
             const Chunk wv = codes8(st.c[a][i].w[s]);
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-              for (int n = 0; n < NP; ++n)
-                sum[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv),
-                                                                 __builtin_bit_cast(bf16x8, xs[s][m][n]), sum[m], 0, 0, 0);
+            for (int n = 0; n < NP; ++n)
+              sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xs[s][n]),
+                                                            __builtin_bit_cast(bf16x8, wv), sum, 0, 0, 0);
           }
-          const uint2 sv = st.s[a][i][z];
-          const floatx4 sc = {__uint_as_float(sv.x << 16), __uint_as_float(sv.x & 0xffff0000u),
-                              __uint_as_float(sv.y << 16), __uint_as_float(sv.y & 0xffff0000u)};
 #pragma unroll
-          for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[a][i][m][r] = fmaf(sc[r], sum[m][r], acc[a][i][m][r]);
+          for (int r = 0; r < 4; ++r) acc[a][i][r] = fmaf(sc[z], sum[r], acc[a][i][r]);
         }
-  };
-  Stage st[D];
-#pragma unroll
-  for (int j = 0; j < D; ++j) load(u0 + j, st[j]);
-  for (int u = u0; u < u1; u += D) {
-#pragma unroll
-    for (int j = 0; j < D; ++j)
-      if (u + j < u1) {
-        mul(st[j]);
-        load(u + j + D, st[j]);
+        asm volatile("" : "+v"(acc[a][i]));  // due here, as in q4_rows_kernel
       }
+    __builtin_amdgcn_sched_barrier(0);
+    if (u + 1 < u1) load(u + 1);
+    __builtin_amdgcn_sched_barrier(0);
   }
 #pragma unroll
   for (int a = 0; a < NM; ++a)
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-      for (int m = 0; m < MT; ++m) red[w][(a * NB + i) * MT + m][lane] = acc[a][i][m];
+    for (int i = 0; i < NB; ++i) red[w][a * NB + i][lane] = acc[a][i];
   __syncthreads();
-  for (int it = w; it < NB * MT; it += Q4_W) {
-    const int i = it / MT, m = it - i * MT;
-    if (16 * m + li >= m_rows) continue;
-    floatx4 v[NM];
+  if (w >= NB) return;
+  floatx4 v[NM];  // rows 4 q .. 4 q + 3, column li of block w
 #pragma unroll
-    for (int a = 0; a < NM; ++a) {
-      v[a] = red[0][a * NB * MT + it][lane];
+  for (int a = 0; a < NM; ++a) {
+    v[a] = red[0][a * NB + w][lane];
 #pragma unroll
-      for (int k = 1; k < Q4_W; ++k) v[a] += red[k][a * NB * MT + it][lane];
-    }
-    const int64_t row = rs + m0 + 16 * m + li;
-    const int col = (nb0 + i) * 16 + 4 * q;
-    if constexpr (GU) {
-      floatx4 h;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) h[r] = silu_of(v[0][r], T{}) * v[NM - 1][r];
-      store4((T*)p.h + row * p.f + col, h);
-    } else {
-      store4((T*)p.y + row * p.d + col, v[0]);
-    }
+    for (int k = 1; k < Q4_KS; ++k) v[a] += red[k][a * NB + w][lane];
   }
+  const int col = (nb0 + w) * 16 + li;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    if (4 * q + r >= m_rows) break;
+    const int64_t row = rs + m0 + 4 * q + r;
+    if constexpr (GU) ((T*)p.h)[row * p.f + col] = from_f<T>(silu_of(v[0][r], T{}) * v[NM - 1][r]);
+    else ((T*)p.y)[row * p.d + col] = from_f<T>(v[0][r]);
+  }
+}
+
+// Up to 16 MT rows of a group against 64 NF columns of the output: the four wavefronts split the columns (16 NF each; GU: of
+// gate and of up) and share the rows, which pass through LDS 128 k at a time in two stages, as the bf16 parts that the MFMAs
+// take. One barrier per step; the next step's rows and codes are loaded while this one is multiplied.
+// LDS rows: 256 bytes of one part, 16-byte chunk c of row r at c ^ (r & 15): the 16 rows of an operand read fall on
+// different banks.
+template <typename T, bool GU, int MT, int NF, int SG, int D>
+__global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
+  static_assert(D % 2 == 0, "the steps of a round alternate between two LDS stages");
+  constexpr int NM = GU ? 2 : 1, NP = Parts<T>::N, XC = 8 / EPC<T>::value, ROWS = 16 * MT;
+  constexpr int PLANE = ROWS * 256;
+  __shared__ __align__(16) char xs[2][NP * PLANE];
+  Q4Tile t;
+  if (!q4_tile(p, blockIdx.x, ROWS, t)) return;
+  const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, li = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int K = GU ? p.d : p.f, N = GU ? p.f : p.d, units = K / 128, KB = K * (int)sizeof(T);
+  const bool routed = t.g < p.Eloc;
+  const int64_t rs = routed ? (int64_t)t.row0 : p.shared0 + (int64_t)(t.g - p.Eloc) * p.T;
+  const char* xb = GU ? (routed ? (const char*)p.xp + (int64_t)t.row0 * KB : (const char*)p.x) : (const char*)p.h + rs * KB;
+  const int m0 = t.ch * ROWS, m_rows = min(t.rows - m0, ROWS);
+  const auto xr = buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB);
+  const int nb0 = (t.nb * 4 + w) * NF;  // the wavefront's first 16-column block
+  __amdgpu_buffer_rsrc_t cr[NM], sr[NM];
+#pragma unroll
+  for (int a = 0; a < NM; ++a) {
+    const int64_t blk = ((int64_t)t.g * (N / 16) + nb0) * units;
+    cr[a] = buf_rsrc(p.codes[a] + blk * 1024, (size_t)NF * units * 1024);
+    sr[a] = buf_rsrc((const char*)p.scales[a] + blk * SG * 32, (size_t)NF * units * SG * 32);
+  }
+  struct Weights {
+    Chunk c[NM][NF];
+    uint32_t s[NM][NF];
+  };
+  // steps past the end read zeros
+  auto load_w = [&](int u, Weights& st) {
+    const int past = u < units ? 0 : kBufPast;
+#pragma unroll
+    for (int a = 0; a < NM; ++a)
+#pragma unroll
+      for (int i = 0; i < NF; ++i) {
+        const int o = u < units ? i * units + u : 0;
+        st.c[a][i] = buf_ld16_at(cr[a], lane * 16 | past, o * 1024);
+        st.s[a][i] = buf_ld2_at(sr[a], ((q % SG) * 32 + 2 * li) | past, o * SG * 32);
+      }
+  };
+  // eight activations of row r, columns 8 c .. 8 c + 7 of the step: thread tid takes (r, c) = item tid + 256 j
+  auto load_x = [&](int u, XChunk<T> (&x)[MT]) {
+    const int so = u < units ? u * 128 * (int)sizeof(T) : 0;
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+      const int it = tid + 256 * j;
+#pragma unroll
+      for (int c = 0; c < XC; ++c)
+        x[j].c[c] = buf_ld16_at(xr, u < units ? (it >> 4) * KB + 8 * (it & 15) * (int)sizeof(T) + 16 * c : kBufPast, so);
+    }
+  };
+  auto put_x = [&](int stage, const XChunk<T> (&x)[MT]) {
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+      const int it = tid + 256 * j, r = it >> 4;
+      Chunk part[NP];
+      split(x[j], part);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) st_chunk(xs[stage] + n * PLANE + r * 256 + (((it & 15) ^ (r & 15)) << 4), part[n]);
+    }
+  };
+  floatx4 acc[NM][NF][MT];
+#pragma unroll
+  for (int a = 0; a < NM; ++a)
+#pragma unroll
+    for (int i = 0; i < NF; ++i)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) acc[a][i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
+  // One step of 128 k on the first ML row blocks (those past the chunk's rows are left out, in halves of the chunk): an
+  // operand of the rows is read from LDS while the products of the one before run.
+  auto mul = [&](int stage, const Weights& st, auto ml) {
+    constexpr int ML = decltype(ml)::value;
+    Chunk xf[2][ML][NP];
+    auto read = [&](int s, Chunk (&f)[ML][NP]) {
+#pragma unroll
+      for (int m = 0; m < ML; ++m)
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+          f[m][n] = ld_chunk(xs[stage] + n * PLANE + (16 * m + li) * 256 + (((4 * s + q) ^ li) << 4));
+    };
+    read(0, xf[0]);
+    float sc[NM][NF][SG];
+#pragma unroll
+    for (int a = 0; a < NM; ++a)
+#pragma unroll
+      for (int i = 0; i < NF; ++i) spread_scales<SG>(st.s[a][i], sc[a][i]);
+    floatx4 sum[NM][NF][ML];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (s < 3) read(s + 1, xf[(s + 1) & 1]);
+      const int z = s * SG / 4;
+#pragma unroll
+      for (int a = 0; a < NM; ++a)
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+          const Chunk wv = codes8(st.c[a][i].w[s]);
+#pragma unroll
+          for (int m = 0; m < ML; ++m) {
+            if (s % (4 / SG) == 0) sum[a][i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int n = 0; n < NP; ++n)
+              sum[a][i][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xf[s & 1][m][n]),
+                                                                     __builtin_bit_cast(bf16x8, wv), sum[a][i][m], 0, 0, 0);
+          }
+        }
+      if ((s + 1) % (4 / SG) == 0) {
+#pragma unroll
+        for (int a = 0; a < NM; ++a)
+#pragma unroll
+          for (int i = 0; i < NF; ++i)
+#pragma unroll
+            for (int m = 0; m < ML; ++m)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[a][i][m][r] = fmaf(sc[a][i][z], sum[a][i][m][r], acc[a][i][m][r]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the sums are due here: left alone, the compiler moves the scaling past the next branch, with every product live
+#pragma unroll
+    for (int a = 0; a < NM; ++a)
+#pragma unroll
+      for (int i = 0; i < NF; ++i)
+#pragma unroll
+        for (int m = 0; m < ML; ++m) asm volatile("" : "+v"(acc[a][i][m]));
+  };
+  Weights wt[D];
+  XChunk<T> xv[D][MT];
+#pragma unroll
+  for (int j = 0; j < D - 1; ++j) {
+    load_x(j, xv[j]);
+    load_w(j, wt[j]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  put_x(0, xv[0]);
+  auto loop = [&](auto ml) {
+    for (int u0 = 0; u0 < units; u0 += D) {
+#pragma unroll
+      for (int j = 0; j < D; ++j) {
+        if (u0 + j >= units) break;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // stage j is filled, the other one was left
+        load_x(u0 + j + D - 1, xv[(j + D - 1) % D]);
+        load_w(u0 + j + D - 1, wt[(j + D - 1) % D]);
+        __builtin_amdgcn_sched_barrier(0);
+        mul(j & 1, wt[j], ml);
+        put_x((j + 1) & 1, xv[(j + 1) % D]);
+      }
+    }
+  };
+  // a loop of its own for half a chunk of rows (a branch inside one loop has its sides' conversions hoisted, and spills)
+  if (MT >= 2 && m_rows <= 8 * MT) loop(std::integral_constant<int, (MT + 1) / 2>{});
+  else loop(std::integral_constant<int, MT>{});
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (16 * m + 4 * q + r >= m_rows) break;
+      const int64_t row = rs + m0 + 16 * m + 4 * q + r;
+#pragma unroll
+      for (int i = 0; i < NF; ++i) {
+        const int col = (nb0 + i) * 16 + li;
+        if constexpr (GU)
+          ((T*)p.h)[row * p.f + col] = from_f<T>(silu_of(acc[0][i][m][r], T{}) * acc[NM - 1][i][m][r]);
+        else
+          ((T*)p.y)[row * p.d + col] = from_f<T>(acc[0][i][m][r]);
+      }
+    }
 }
 
 // ------------------------------------------------------------------------- host side
@@ -375,21 +568,53 @@ int64_t chunks_of(const moe_desc& d, int chunk) {
          (int64_t)d.n_shared * ((d.T + chunk - 1) / chunk);
 }
 
-template <typename T, bool GU, int MT, int NB, int SG, int D>
-hipError_t q4_run(const moe_desc& d, Q4Args a, hipStream_t s) {
+template <typename T, bool GU, int NB, int SG>
+hipError_t q4_run_split(const moe_desc& d, Q4Args a, hipStream_t s) {
   a.n_blocks = (GU ? d.d_ff : d.d_model) / (16 * NB);
-  const unsigned grid = (unsigned)((chunks_of(d, 16 * MT) * a.n_blocks + 7) / 8 * 8);
+  const unsigned grid = (unsigned)((chunks_of(d, 16) * a.n_blocks + 7) / 8 * 8);
   KernelTimer kt(GU ? "q4_gate_up" : "q4_down", s);
-  hipLaunchKernelGGL((q4_split_kernel<T, GU, MT, NB, SG, D>), dim3(grid), dim3(64 * Q4_W), 0, s, a);
+  hipLaunchKernelGGL((q4_split_kernel<T, GU, NB, SG>), dim3(grid), dim3(64 * Q4_KS), 0, s, a);
   return hipGetLastError();
 }
 
+template <typename T, bool GU, int MT, int NF, int SG, int D>
+hipError_t q4_run_rows(const moe_desc& d, Q4Args a, hipStream_t s) {
+  a.n_blocks = (GU ? d.d_ff : d.d_model) / (64 * NF);
+  const unsigned grid = (unsigned)((chunks_of(d, 16 * MT) * a.n_blocks + 7) / 8 * 8);
+  KernelTimer kt(GU ? "q4_gate_up" : "q4_down", s);
+  hipLaunchKernelGGL((q4_rows_kernel<T, GU, MT, NF, SG, D>), dim3(grid), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+// Which kernel a projection takes, by the rows that an active expert can expect (the counts stay on the device; a shard's
+// share of the slots, experts equally likely) and by whether the shared-rows kernel would be bound by the chain of its steps
+// (0.45 and 0.36 us each, gate/up and down, and 2 us around them) rather than by reading the weights (5.5 TB/s):
+//   * chain-bound and up to 12 rows: K split over 8 wavefronts, 32 columns each up to 2 rows, 64 above;
+//   * else shared rows. Gate/up: 16-row chunks up to 8 rows, 32-row chunks above. Down, whose K is the long one: 16-row
+//     chunks with four steps in flight up to 40 rows, 32-row chunks and 128 columns above.
+// us of split 32 / split 64 / rows 16 / rows 32 (down: rows 16 / rows 32 x 128), group 64, at T, d, f, E, k, shared:
+//   gate/up:  1, 2048, 1408, 64, 6, 2   10.1 /  9.9 / 11.2 / 12.6     down:  7.3 /  7.4 /  8.2 /  9.5
+//             1, 4096, 14336, 8, 2      27.0 / 26.8 / 25.5 / 28.5           17.6 / 21.0 / 38.9 / 66.8
+//             8, 1024, 2816, 16, 2      11.5 / 11.2 / 10.3 / 10.1            7.9 /  8.2 / 10.6 / 13.7
+//             16, 2048, 1408, 64, 6, 2  39.5 / 38.0 / 33.0 / 40.0           31.7 / 25.7 / 20.1 / 20.2
+//             16, 4096, 1408, 8, 2      15.6 / 13.6 / 18.1 / 19.2           11.9 / 10.0 /  9.0 / 10.0
+//             24, 4096, 14336, 8, 2     96.3 / 89.5 / 84.8 / 85.7           60.4 / 50.8 / 49.5 / 75.3
+//             64, 1024, 2816, 16, 2     19.2 / 16.1 / 14.0 / 12.5           11.2 /  9.4 / 11.0 / 13.9
+//             128, 4096, 14336, 8, 2   219.3 / 163  / 136  / 124           167   / 107  / 91.2 / 85.3
+//             777, 1024, 2816, 16, 2    95.2 / 67.4 / 38.2 / 30.7           56.9 / 37.0 / 23.2 / 20.2
+// Measured and not kept: 64- and 128-row chunks (777 rows: 36.8 and 49 us of gate/up), four and sixteen wavefronts of a
+// split, deeper prefetch in the split, non-temporal loads of the codes (equal, and worse where calls follow each other).
 template <typename T, bool GU, int SG>
 hipError_t q4_pick(const moe_desc& d, const Q4Args& a, hipStream_t s) {
-  const int64_t groups = std::min<int64_t>((int64_t)d.T * d.top_k, d.local_count) + d.n_shared;
-  const int64_t rows = rows_total(d) / std::max<int64_t>(1, groups);
-  if (rows <= 16) return q4_run<T, GU, 1, 2, SG, 2>(d, a, s);
-  return q4_run<T, GU, 2, 2, SG, 1>(d, a, s);
+  const double share = (double)d.top_k / d.n_experts;
+  const double active = d.local_count * (1 - std::pow(1 - share, d.T)) + d.n_shared;
+  const double rows = d.T * (share * d.local_count + d.n_shared) / active;
+  const double bytes = active * (GU ? 2 : 1) * d.d_ff * d.d_model * (0.5 + SG / 64.0);
+  const double chain = 2 + (GU ? 0.45 : 0.36) * ((GU ? d.d_model : d.d_ff) / 128);
+  if (rows <= 12 && chain > bytes / 5.5e6)
+    return rows <= 2 ? q4_run_split<T, GU, 2, SG>(d, a, s) : q4_run_split<T, GU, 4, SG>(d, a, s);
+  if constexpr (GU) return rows <= 8 ? q4_run_rows<T, GU, 1, 1, SG, 2>(d, a, s) : q4_run_rows<T, GU, 2, 1, SG, 2>(d, a, s);
+  else return rows <= 40 ? q4_run_rows<T, GU, 1, 1, SG, 4>(d, a, s) : q4_run_rows<T, GU, 2, 2, SG, 2>(d, a, s);
 }
 
 template <typename T, int SG>
