@@ -51,6 +51,7 @@ struct GateArgs {
   float scale;
   int sigmoid, groups, keep, top, group_size;
   int group_mul;      // e / group_size = e * group_mul >> 16 for e < 256
+  int lane_shift;     // 2^lane_shift = lanes of a wavefront per group, the largest power of two up to 64 / groups
 };
 
 // Order-preserving key of a choice value: 0 for what is never chosen (NaN, -inf), -0 and +0 alike.
@@ -59,15 +60,46 @@ __device__ __forceinline__ uint64_t choice_key(double v) {
   if (!(v > -INFINITY)) return 0ull;
   return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
-__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
-  const uint32_t hi = wave_max_u32((uint32_t)(v >> 32));
-  const uint32_t lo = wave_max_u32((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
-  return ((uint64_t)hi << 32) | lo;
+// The value of another lane, by the vector ALU's lane shifts (a shuffle through LDS costs ten times as long).
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double dpp_f64(double v, double otherwise = 0.0) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v), w = (uint64_t)__double_as_longlong(otherwise);
+  const uint32_t lo = __builtin_amdgcn_update_dpp((int)w, (int)u, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp((int)(w >> 32), (int)(u >> 32), CTRL, ROWS, 0xf, false);
+  return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+__device__ __forceinline__ double readlane_f64(double v, int lane) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  return __longlong_as_double((long long)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), lane) << 32) |
+                                          (uint32_t)__builtin_amdgcn_readlane((int)u, lane)));
 }
 __device__ __forceinline__ double wave_sum_f64(double v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
+  v += dpp_f64<0x111>(v);  // row_shr 1, 2, 4, 8: lane 15 of each row of 16 holds the row's sum
+  v += dpp_f64<0x112>(v);
+  v += dpp_f64<0x114>(v);
+  v += dpp_f64<0x118>(v);
+  v += dpp_f64<0x142, 0xa>(v);  // row_bcast 15 into rows 1 and 3, row_bcast 31 into rows 2 and 3
+  v += dpp_f64<0x143, 0xc>(v);
+  return readlane_f64(v, 63);
+}
+__device__ __forceinline__ double sum8_f64(double v) {  // of lanes 0 .. 7
+  v += dpp_f64<0x111>(v);
+  v += dpp_f64<0x112>(v);
+  v += dpp_f64<0x114>(v);
+  return readlane_f64(v, 7);
+}
+// The largest of fp32 numbers (NaN passed over; -inf where there is none), in every lane.
+__device__ __forceinline__ float wave_max_dpp(float v) {
+#define PCMOE_DPP_FMAX(ctrl, rows) \
+  v = fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp((int)0xff800000, (int)__float_as_uint(v), ctrl, rows, 0xf, false)))
+  PCMOE_DPP_FMAX(0x111, 0xf);
+  PCMOE_DPP_FMAX(0x112, 0xf);
+  PCMOE_DPP_FMAX(0x114, 0xf);
+  PCMOE_DPP_FMAX(0x118, 0xf);
+  PCMOE_DPP_FMAX(0x142, 0xa);
+  PCMOE_DPP_FMAX(0x143, 0xc);
+#undef PCMOE_DPP_FMAX
+  return __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
 }
 
 // One token: v[qq] is the score of expert lane + 64 qq (-inf past E). `row` is LDS that only this wavefront uses, E
@@ -84,7 +116,7 @@ __device__ __forceinline__ void gated_select(const float (&v)[QE], int E, int k,
     float mm = v[0];
 #pragma unroll
     for (int qq = 1; qq < QE; ++qq) mm = fmaxf(mm, v[qq]);
-    m = wave_max(mm);
+    m = wave_max_dpp(mm);
     double zz = 0.0;
 #pragma unroll
     for (int qq = 0; qq < QE; ++qq) {
@@ -110,48 +142,67 @@ __device__ __forceinline__ void gated_select(const float (&v)[QE], int E, int k,
     key[qq] = e < E && v[qq] > -INFINITY ? choice_key(c) : 0ull;
   }
   if (ga.groups > 1) {
-    // lane g finds the largest and the second largest value of group g; the lanes start at different experts of theirs,
-    // on different LDS banks
+    // 2^lane_shift lanes find the largest and the second largest value of a group
 #pragma unroll
     for (int qq = 0; qq < QE; ++qq)
       if (lane + 64 * qq < E) row[lane + 64 * qq] = key[qq] ? worth[qq] : -INFINITY;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     double a = -INFINITY, b = -INFINITY;
-    if (lane < ga.groups) {
-      int o = lane % ga.group_size;
-      for (int n = 0; n < ga.group_size; ++n) {
-        const double w = row[lane * ga.group_size + o];
+    const int g = lane >> ga.lane_shift, lanes = 1 << ga.lane_shift;
+    if (g < ga.groups)
+      for (int o = lane & (lanes - 1); o < ga.group_size; o += lanes) {
+        const double w = row[g * ga.group_size + o];
         b = fmax(b, fmin(a, w));
         a = fmax(a, w);
-        if (++o == ga.group_size) o = 0;
       }
-      if (ga.top == 2 && b > -INFINITY) a += b;
-    }
+    auto merge = [&](double a2, double b2) {
+      b = fmax(fmax(b, b2), fmin(a, a2));
+      a = fmax(a, a2);
+    };
+    // lane pairs, quads (quad_perm), halves of 8 and 16 lanes (mirrors: the lanes merged so far are equal)
+    if (ga.lane_shift >= 1) merge(dpp_f64<0xb1>(a), dpp_f64<0xb1>(b));
+    if (ga.lane_shift >= 2) merge(dpp_f64<0x4e>(a), dpp_f64<0x4e>(b));
+    if (ga.lane_shift >= 3) merge(dpp_f64<0x141>(a), dpp_f64<0x141>(b));
+    if (ga.lane_shift >= 4) merge(dpp_f64<0x140>(a), dpp_f64<0x140>(b));
+    if (ga.lane_shift >= 5) merge(__shfl_xor(a, 16, 64), __shfl_xor(b, 16, 64));
+    if (ga.top == 2 && b > -INFINITY) a += b;
     const uint64_t mine = choice_key(a);
     int ahead = 0;  // groups that come before this one: of equals, the lower index first
-    for (int g = 0; g < ga.groups; ++g) {
-      const uint64_t o = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), g) << 32) |
-                         (uint32_t)__builtin_amdgcn_readlane((int)mine, g);
-      ahead += o > mine || (o == mine && g < lane);
+    for (int h = 0; h < ga.groups; ++h) {
+      const int l = h << ga.lane_shift;
+      const uint64_t o = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), l) << 32) |
+                         (uint32_t)__builtin_amdgcn_readlane((int)mine, l);
+      ahead += o > mine || (o == mine && h < g);
     }
-    const uint64_t open = __ballot(lane < ga.groups && ahead < ga.keep);
+    const uint64_t open = __ballot(g < ga.groups && ahead < ga.keep);
 #pragma unroll
     for (int qq = 0; qq < QE; ++qq)
-      if (!((open >> (((lane + 64 * qq) * ga.group_mul) >> 16 & 63)) & 1)) key[qq] = 0ull;
+      if (!((open >> (((((lane + 64 * qq) * ga.group_mul) >> 16) << ga.lane_shift) & 63)) & 1)) key[qq] = 0ull;
   }
   int myi = NO_EXPERT;
   float myl = -INFINITY;
   for (int j = 0; j < k; ++j) {
-    uint64_t mx = key[0];
+    // the largest upper word; the lower words are compared only where several lanes hold it
+    uint32_t hi = (uint32_t)(key[0] >> 32);
 #pragma unroll
-    for (int qq = 1; qq < QE; ++qq) mx = key[qq] > mx ? key[qq] : mx;
-    mx = wave_max_u64(mx);
-    if (mx == 0ull) break;  // nothing is left to choose from
+    for (int qq = 1; qq < QE; ++qq) hi = max(hi, (uint32_t)(key[qq] >> 32));
+    hi = wave_max_u32(hi);
+    if (hi == 0u) break;  // nothing is left to choose from (a key above 0 has bits in its upper word)
+    int holders = 0;
+    uint32_t low = 0u;
+#pragma unroll
+    for (int qq = 0; qq < QE; ++qq) {
+      const bool is = (uint32_t)(key[qq] >> 32) == hi;
+      holders += __popcll(__ballot(is));
+      low = is ? max(low, (uint32_t)key[qq]) : low;
+    }
+    const bool one = holders == 1;
+    if (!one) low = wave_max_u32(low);
     int best = NO_EXPERT;
     float l = 0.f;
 #pragma unroll
     for (int qq = QE - 1; qq >= 0; --qq) {
-      const uint64_t bl = __ballot(key[qq] == mx);
+      const uint64_t bl = __ballot((uint32_t)(key[qq] >> 32) == hi && (one || (uint32_t)key[qq] == low));
       if (bl) {
         const int ln = __builtin_ctzll(bl);
         best = 64 * qq + ln;
@@ -167,11 +218,11 @@ __device__ __forceinline__ void gated_select(const float (&v)[QE], int E, int k,
     }
   }
   const bool filled = lane < k && myi != NO_EXPERT;
-  if (!ga.sigmoid && renorm) m = wave_max(myl);  // any shift will do: the largest of the chosen
+  if (!ga.sigmoid && renorm) m = wave_max_dpp(myl);  // the largest of the chosen: the others' exponentials stay finite
   double s = 0.0;
   if (filled) s = ga.sigmoid ? 1.0 / (1.0 + exp(-(double)myl)) : exp((double)myl - (double)m) / z;
   if (renorm) {
-    const double t = wave_sum_f64(s);
+    const double t = sum8_f64(s);
     s = t == 0.0 ? 0.0 : s / t;  // every chosen score underflows (or nothing is chosen): no weight
   }
   if (lane < k) {
@@ -456,8 +507,10 @@ hipError_t launch_route_fwd(const moe_desc& d, const void* x, const void* wr, co
 hipError_t launch_route_gated(const moe_desc& d, const moe_gate& g, const void* x, const void* wr, const float* bias,
                               int bg, const float* select_bias, float* logits, int32_t* idx, float* w, hipStream_t s) {
   const int size = d.n_experts / g.n_groups;
+  int lane_shift = 0;
+  while ((2 << lane_shift) * g.n_groups <= 64) ++lane_shift;
   const GateArgs ga{select_bias, g.scale, g.score == MOE_SCORE_SIGMOID, g.n_groups, g.topk_groups, g.group_top, size,
-                    (65536 + size - 1) / size};
+                    (65536 + size - 1) / size, lane_shift};
   if (d.dtype == MOE_BF16) return route_fwd_t<bf16, true>(d, x, wr, bias, bg, logits, idx, w, ga, s);
   return route_fwd_t<float, true>(d, x, wr, bias, bg, logits, idx, w, ga, s);
 }
