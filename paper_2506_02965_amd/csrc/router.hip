@@ -875,6 +875,119 @@ size_t route_bwd_ws_bytes(const moe_desc& d) {
   return align256((size_t)nch * d.n_experts * d.d_model * sizeof(float));
 }
 
+// dW_router = dlogits^T x of bf16 tokens on v_mfma_f32_16x16x32_bf16: the gradients of the scores as three bf16 numbers that
+// add up to each fp32 one exactly (8 + 8 + 8 bits), so the products are those of the fp32 contraction at five times its rate
+// (T = 16,384, E = 64, d = 2048: 4.3 GFLOP, 28 us on the fp32 matrix cores, 11 for three bf16 products; the tokens' 67 MB take
+// 14). A workgroup holds 128 columns x 16 NET experts; its wavefronts take the chunk's tokens 32 at a time in turn, with
+// accumulators of their own, which meet in LDS half the columns at a time and are added in wavefront order.
+//   tokens as K: lane (q, i) loads 16 bytes of tokens 8 q .. 8 q + 7 and turns the 8 x 8 block into operands of its columns
+//   8 i + s, s = 0 .. 7, by byte permutes; row i of expert tile m is expert NET i + m, so that a token's gradients of a
+//   lane's NET experts are one load. Tokens and experts past the end read as zeros.
+// An infinite gradient makes NaN (inf - inf in the split) where the fp32 contraction might make an infinity.
+constexpr int GDW_W = 8;
+template <int NET, bool VEC>
+__global__ __launch_bounds__(64 * GDW_W, 2) void gate_dw_kernel(int Tn, int d, int E, int tok_per_chunk,
+                                                                const bf16* __restrict__ x, const float* __restrict__ dl,
+                                                                float* __restrict__ part) {
+  __shared__ float4 red[GDW_W][16 * NET][16];
+  const int lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c0 = blockIdx.x * 128, e0 = blockIdx.y * 16 * NET;
+  const int tb = blockIdx.z * tok_per_chunk, te = min(Tn, tb + tok_per_chunk);
+  const auto xr = buf_rsrc(x + (size_t)tb * d + c0, ((size_t)(te - tb) * d - c0) * 2);
+  const auto gr = buf_rsrc(dl + (size_t)tb * E, (size_t)(te - tb) * E * 4);
+  const int el = e0 + NET * i;  // the lane's first expert
+  floatx4 acc[8][NET];
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+#pragma unroll
+    for (int m = 0; m < NET; ++m) acc[s][m] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int t0 = 32 * w; t0 < te - tb; t0 += 32 * GDW_W) {
+    Chunk xv[8];
+    uint32_t g[8][NET];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int t = t0 + 8 * q + j;
+      xv[j] = buf_ld16(xr, t < te - tb ? (t * d + 8 * i) * 2 : kBufPast);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int o = ((t0 + 8 * q + j) * E + el) * 4;
+      if constexpr (VEC && NET == 4) {
+        const Chunk c = buf_ld16(gr, el < E ? o : kBufPast);
+#pragma unroll
+        for (int m = 0; m < NET; ++m) g[j][m] = c.w[m];
+      } else {
+#pragma unroll
+        for (int m = 0; m < NET; ++m)
+          g[j][m] = __builtin_amdgcn_raw_buffer_load_b32(gr, el + m < E ? o + 4 * m : kBufPast, 0, 0);
+      }
+    }
+    Chunk a[NET][3];
+#pragma unroll
+    for (int m = 0; m < NET; ++m)
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        uint32_t hi[2], mid[2], low[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          hi[b] = g[2 * p + b][m];
+          mid[b] = __float_as_uint(__uint_as_float(hi[b]) - __uint_as_float(hi[b] & 0xffff0000u));
+          low[b] = __float_as_uint(__uint_as_float(mid[b]) - __uint_as_float(mid[b] & 0xffff0000u));
+        }
+        a[m][0].w[p] = __builtin_amdgcn_perm(hi[1], hi[0], 0x07060302u);
+        a[m][1].w[p] = __builtin_amdgcn_perm(mid[1], mid[0], 0x07060302u);
+        a[m][2].w[p] = __builtin_amdgcn_perm(low[1], low[0], 0x07060302u);
+      }
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      Chunk b;
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        b.w[p] = __builtin_amdgcn_perm(xv[2 * p + 1].w[s / 2], xv[2 * p].w[s / 2], s % 2 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+      for (int n = 2; n >= 0; --n)
+#pragma unroll
+        for (int m = 0; m < NET; ++m)
+          acc[s][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[m][n]),
+                                                              __builtin_bit_cast(bf16x8, b), acc[s][m], 0, 0, 0);
+    }
+  }
+  // register r of lane (q, i), product (s, m): expert e0 + NET (4 q + r) + m, column c0 + 8 i + s
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (h) __syncthreads();
+#pragma unroll
+    for (int m = 0; m < NET; ++m)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        red[w][NET * (4 * q + r) + m][i] =
+            float4{acc[4 * h][m][r], acc[4 * h + 1][m][r], acc[4 * h + 2][m][r], acc[4 * h + 3][m][r]};
+    __syncthreads();
+    for (int u = threadIdx.x; u < 16 * NET * 16; u += 64 * GDW_W) {
+      const int e = u >> 4, n = u & 15;
+      if (e0 + e >= E) break;
+      float4 v = red[0][e][n];
+#pragma unroll
+      for (int k = 1; k < GDW_W; ++k) {
+        const float4 o = red[k][e][n];
+        v.x += o.x;
+        v.y += o.y;
+        v.z += o.z;
+        v.w += o.w;
+      }
+      *reinterpret_cast<float4*>(part + ((size_t)blockIdx.z * E + e0 + e) * d + c0 + 8 * n + 4 * h) = v;
+    }
+  }
+}
+
+static void route_dw_sum(const moe_desc& d, int nch, const float* part, float* dwr, hipStream_t s) {
+  KernelTimer kt("route_dw_reduce", s);
+  const int n4 = d.n_experts * d.d_model / 4;
+  const int blocks = (n4 + 256 / RED_G - 1) / (256 / RED_G);
+  hipLaunchKernelGGL(route_dw_reduce_kernel, dim3(blocks), dim3(256), 0, s, n4, nch, (const float4*)part, (float4*)dwr);
+}
+
 static unsigned token_blocks(const moe_desc& d) { return std::min((d.T + 3) / 4, 4096); }
 
 // dW_router from the gradients of the scores.
@@ -912,13 +1025,36 @@ static hipError_t route_dw_t(const moe_desc& d, const void* x, const float* dl, 
 #undef RB_LAUNCH
     }
   }
-  if (nch > 1) {
-    KernelTimer kt("route_dw_reduce", s);
-    const int n4 = E * d.d_model / 4;
-    const int blocks = (n4 + 256 / RED_G - 1) / (256 / RED_G);
-    hipLaunchKernelGGL(route_dw_reduce_kernel, dim3(blocks), dim3(256), 0, s, n4, nch, (const float4*)part,
-                       (float4*)dwr);
+  if (nch > 1) route_dw_sum(d, nch, part, dwr, s);
+  return hipGetLastError();
+}
+
+// ... of bf16 tokens for the gated routing. Chunks of tokens: as many as give each CU a workgroup, at least a step of 32
+// tokens for each wavefront, and no more than the workspace holds.
+static hipError_t gate_dw(const moe_desc& d, const void* x, const float* dl, float* dwr, void* ws, hipStream_t s) {
+  const int E = d.n_experts, net = E <= 16 ? 1 : E <= 32 ? 2 : 4;
+  const int cols = d.d_model / 128, groups = (E + 16 * net - 1) / (16 * net);
+  int most, tpc;
+  bool wide;
+  route_bwd_chunks(d, &most, &tpc, &wide);
+  const int want = std::min({device_cus() / (cols * groups), d.T / (32 * GDW_W), most});
+  const int per = (d.T + std::max(want, 1) - 1) / std::max(want, 1);
+  tpc = (per + 31) / 32 * 32;
+  const int nch = (d.T + tpc - 1) / tpc;
+  float* part = nch == 1 ? dwr : (float*)ws;
+  {
+    KernelTimer kt("gate_dw", s);
+    const dim3 grid(cols, groups, nch);
+#define GD_LAUNCH(NET, VEC)                                                                                       \
+  hipLaunchKernelGGL((gate_dw_kernel<NET, VEC>), grid, dim3(64 * GDW_W), 0, s, d.T, d.d_model, E, tpc, (const bf16*)x, \
+                     dl, part)
+    if (net == 1) GD_LAUNCH(1, false);
+    else if (net == 2) GD_LAUNCH(2, false);
+    else if (E % 4) GD_LAUNCH(4, false);
+    else GD_LAUNCH(4, true);
+#undef GD_LAUNCH
   }
+  if (nch > 1) route_dw_sum(d, nch, part, dwr, s);
   return hipGetLastError();
 }
 
@@ -945,7 +1081,7 @@ hipError_t launch_route_gated_bwd(const moe_desc& d, const moe_gate& g, const vo
     hipLaunchKernelGGL(gate_dlogits_kernel, dim3(token_blocks(d)), dim3(256), 0, s, d.T, d.n_experts, d.top_k,
                        d.renormalize, (int)(g.score == MOE_SCORE_SIGMOID), g.scale, logits, idx, w, dgate, dl);
   }
-  return route_dw(d, x, dl, dwr, ws, s);
+  return d.dtype == MOE_BF16 ? gate_dw(d, x, dl, dwr, ws, s) : route_dw_t<float>(d, x, dl, dwr, ws, s);
 }
 
 }  // namespace pcmoe

@@ -178,7 +178,8 @@ def gate_formula(l, idx, g, w, score, renorm, scale):
 
 
 GRADS = [(1, 128, 4, 2), (2, 128, 256, 8), (31, 256, 8, 1), (33, 128, 64, 6), (257, 128, 17, 8), (1500, 512, 8, 2),
-         (700, 128, 200, 8), (3000, 256, 96, 4), (4096, 128, 256, 8)]
+         (700, 128, 200, 8), (3000, 256, 96, 4), (4096, 128, 256, 8), (258, 128, 66, 3), (1000, 256, 33, 2), (34, 640, 12, 4),
+         (16384, 128, 64, 6), (4098, 256, 130, 8), (514, 384, 17, 2), (8200, 4096, 24, 2)]
 
 
 @pytest.mark.parametrize("case", GRADS, ids=lambda c: "T{}_d{}_E{}_k{}".format(*c))
