@@ -102,132 +102,194 @@ __device__ __forceinline__ float wave_max_dpp(float v) {
   return __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
 }
 
-// One token: v[qq] is the score of expert lane + 64 qq (-inf past E). `row` is LDS that only this wavefront uses, E
-// doubles of it.
-template <int QE>
-__device__ __forceinline__ void gated_select(const float (&v)[QE], int E, int k, int renorm, const GateArgs& ga,
-                                             double* row, int32_t* __restrict__ idx, float* __restrict__ gw) {
+// NT tokens at once, whose chains of dependent instructions fill each other's waits: v[n][qq] is token n's score of expert
+// lane + 64 qq (-inf past E). row[n] is LDS that only this wavefront uses, E doubles of it. Token n's results go to idx + n
+// * step and gw + n * step, as long as n < valid.
+template <int QE, int NT>
+__device__ __forceinline__ void gated_select(const float (&v)[NT][QE], int E, int k, int renorm, const GateArgs& ga,
+                                             double* const (&row)[NT], int valid, size_t step,
+                                             int32_t* __restrict__ idx, float* __restrict__ gw) {
   const int lane = threadIdx.x & 63;
   const bool need = ga.bias || (ga.groups > 1 && ga.top == 2);  // are scores of all the experts needed?
-  double z = 1.0;                                                // softmax: the largest logit and the sum over E
-  float m = 0.f;
-  double sc[QE];
-  if (!ga.sigmoid && (need || !renorm)) {
-    float mm = v[0];
+  double z[NT];                                                  // softmax: the largest logit and the sum over E
+  float m[NT];
+  double sc[NT][QE];
 #pragma unroll
-    for (int qq = 1; qq < QE; ++qq) mm = fmaxf(mm, v[qq]);
-    m = wave_max_dpp(mm);
-    double zz = 0.0;
+  for (int n = 0; n < NT; ++n) {
+    z[n] = 1.0;
+    m[n] = 0.f;
+    if (!ga.sigmoid && (need || !renorm)) {
+      float mm = v[n][0];
 #pragma unroll
-    for (int qq = 0; qq < QE; ++qq) {
-      sc[qq] = v[qq] > -INFINITY ? exp((double)v[qq] - (double)m) : 0.0;  // nothing of a masked or NaN expert
-      zz += sc[qq];
+      for (int qq = 1; qq < QE; ++qq) mm = fmaxf(mm, v[n][qq]);
+      m[n] = wave_max_dpp(mm);
+      double zz = 0.0;
+#pragma unroll
+      for (int qq = 0; qq < QE; ++qq) {
+        sc[n][qq] = v[n][qq] > -INFINITY ? exp((double)v[n][qq] - (double)m[n]) : 0.0;  // nothing of a masked or NaN expert
+        zz += sc[n][qq];
+      }
+      z[n] = wave_sum_f64(zz);
     }
-    z = wave_sum_f64(zz);
   }
-  uint64_t key[QE];
-  double worth[QE];  // what a group's value is made of
+  uint64_t key[NT][QE];
+  double worth[NT][QE];  // what a group's value is made of
 #pragma unroll
   for (int qq = 0; qq < QE; ++qq) {
     const int e = lane + 64 * qq;
-    double c = (double)v[qq];
-    worth[qq] = c;
-    if (need) {
-      worth[qq] = ga.sigmoid ? 1.0 / (1.0 + exp(-c)) : sc[qq] / z;
-      if (ga.bias) {
-        worth[qq] += (double)(e < E ? ga.bias[e] : 0.f);
-        c = worth[qq];
+    const double bias = ga.bias && e < E ? (double)ga.bias[e] : 0.0;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      double c = (double)v[n][qq];
+      worth[n][qq] = c;
+      if (need) {
+        worth[n][qq] = ga.sigmoid ? 1.0 / (1.0 + exp(-c)) : sc[n][qq] / z[n];
+        if (ga.bias) {
+          worth[n][qq] += bias;
+          c = worth[n][qq];
+        }
       }
+      key[n][qq] = e < E && v[n][qq] > -INFINITY ? choice_key(c) : 0ull;
     }
-    key[qq] = e < E && v[qq] > -INFINITY ? choice_key(c) : 0ull;
   }
   if (ga.groups > 1) {
     // 2^lane_shift lanes find the largest and the second largest value of a group
-#pragma unroll
-    for (int qq = 0; qq < QE; ++qq)
-      if (lane + 64 * qq < E) row[lane + 64 * qq] = key[qq] ? worth[qq] : -INFINITY;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    double a = -INFINITY, b = -INFINITY;
     const int g = lane >> ga.lane_shift, lanes = 1 << ga.lane_shift;
+    double a[NT], b[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int qq = 0; qq < QE; ++qq)
+        if (lane + 64 * qq < E) row[n][lane + 64 * qq] = key[n][qq] ? worth[n][qq] : -INFINITY;
+      a[n] = b[n] = -INFINITY;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (g < ga.groups)
       for (int o = lane & (lanes - 1); o < ga.group_size; o += lanes) {
-        const double w = row[g * ga.group_size + o];
-        b = fmax(b, fmin(a, w));
-        a = fmax(a, w);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const double w = row[n][g * ga.group_size + o];
+          b[n] = fmax(b[n], fmin(a[n], w));
+          a[n] = fmax(a[n], w);
+        }
       }
-    auto merge = [&](double a2, double b2) {
-      b = fmax(fmax(b, b2), fmin(a, a2));
-      a = fmax(a, a2);
+    auto merge = [&](int n, double a2, double b2) {
+      b[n] = fmax(fmax(b[n], b2), fmin(a[n], a2));
+      a[n] = fmax(a[n], a2);
     };
     // lane pairs, quads (quad_perm), halves of 8 and 16 lanes (mirrors: the lanes merged so far are equal)
-    if (ga.lane_shift >= 1) merge(dpp_f64<0xb1>(a), dpp_f64<0xb1>(b));
-    if (ga.lane_shift >= 2) merge(dpp_f64<0x4e>(a), dpp_f64<0x4e>(b));
-    if (ga.lane_shift >= 3) merge(dpp_f64<0x141>(a), dpp_f64<0x141>(b));
-    if (ga.lane_shift >= 4) merge(dpp_f64<0x140>(a), dpp_f64<0x140>(b));
-    if (ga.lane_shift >= 5) merge(__shfl_xor(a, 16, 64), __shfl_xor(b, 16, 64));
-    if (ga.top == 2 && b > -INFINITY) a += b;
-    const uint64_t mine = choice_key(a);
-    int ahead = 0;  // groups that come before this one: of equals, the lower index first
+    if (ga.lane_shift >= 1)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) merge(n, dpp_f64<0xb1>(a[n]), dpp_f64<0xb1>(b[n]));
+    if (ga.lane_shift >= 2)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) merge(n, dpp_f64<0x4e>(a[n]), dpp_f64<0x4e>(b[n]));
+    if (ga.lane_shift >= 3)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) merge(n, dpp_f64<0x141>(a[n]), dpp_f64<0x141>(b[n]));
+    if (ga.lane_shift >= 4)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) merge(n, dpp_f64<0x140>(a[n]), dpp_f64<0x140>(b[n]));
+    if (ga.lane_shift >= 5)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) merge(n, __shfl_xor(a[n], 16, 64), __shfl_xor(b[n], 16, 64));
+    uint64_t mine[NT];
+    int ahead[NT];  // groups that come before the lane's: of equals, the lower index first
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (ga.top == 2 && b[n] > -INFINITY) a[n] += b[n];
+      mine[n] = choice_key(a[n]);
+      ahead[n] = 0;
+    }
     for (int h = 0; h < ga.groups; ++h) {
       const int l = h << ga.lane_shift;
-      const uint64_t o = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), l) << 32) |
-                         (uint32_t)__builtin_amdgcn_readlane((int)mine, l);
-      ahead += o > mine || (o == mine && h < g);
-    }
-    const uint64_t open = __ballot(g < ga.groups && ahead < ga.keep);
 #pragma unroll
-    for (int qq = 0; qq < QE; ++qq)
-      if (!((open >> (((((lane + 64 * qq) * ga.group_mul) >> 16) << ga.lane_shift) & 63)) & 1)) key[qq] = 0ull;
-  }
-  int myi = NO_EXPERT;
-  float myl = -INFINITY;
-  for (int j = 0; j < k; ++j) {
-    // the largest upper word; the lower words are compared only where several lanes hold it
-    uint32_t hi = (uint32_t)(key[0] >> 32);
-#pragma unroll
-    for (int qq = 1; qq < QE; ++qq) hi = max(hi, (uint32_t)(key[qq] >> 32));
-    hi = wave_max_u32(hi);
-    if (hi == 0u) break;  // nothing is left to choose from (a key above 0 has bits in its upper word)
-    int holders = 0;
-    uint32_t low = 0u;
-#pragma unroll
-    for (int qq = 0; qq < QE; ++qq) {
-      const bool is = (uint32_t)(key[qq] >> 32) == hi;
-      holders += __popcll(__ballot(is));
-      low = is ? max(low, (uint32_t)key[qq]) : low;
-    }
-    const bool one = holders == 1;
-    if (!one) low = wave_max_u32(low);
-    int best = NO_EXPERT;
-    float l = 0.f;
-#pragma unroll
-    for (int qq = QE - 1; qq >= 0; --qq) {
-      const uint64_t bl = __ballot((uint32_t)(key[qq] >> 32) == hi && (one || (uint32_t)key[qq] == low));
-      if (bl) {
-        const int ln = __builtin_ctzll(bl);
-        best = 64 * qq + ln;
-        l = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v[qq]), ln));
+      for (int n = 0; n < NT; ++n) {
+        const uint64_t o = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine[n] >> 32), l) << 32) |
+                           (uint32_t)__builtin_amdgcn_readlane((int)mine[n], l);
+        ahead[n] += o > mine[n] || (o == mine[n] && h < g);
       }
     }
 #pragma unroll
-    for (int qq = 0; qq < QE; ++qq)
-      if (lane + 64 * qq == best) key[qq] = 0ull;
-    if (lane == j) {
-      myi = best;
-      myl = l;
+    for (int n = 0; n < NT; ++n) {
+      const uint64_t open = __ballot(g < ga.groups && ahead[n] < ga.keep);
+#pragma unroll
+      for (int qq = 0; qq < QE; ++qq)
+        if (!((open >> (((((lane + 64 * qq) * ga.group_mul) >> 16) << ga.lane_shift) & 63)) & 1)) key[n][qq] = 0ull;
     }
   }
-  const bool filled = lane < k && myi != NO_EXPERT;
-  if (!ga.sigmoid && renorm) m = wave_max_dpp(myl);  // the largest of the chosen: the others' exponentials stay finite
-  double s = 0.0;
-  if (filled) s = ga.sigmoid ? 1.0 / (1.0 + exp(-(double)myl)) : exp((double)myl - (double)m) / z;
-  if (renorm) {
-    const double t = sum8_f64(s);
-    s = t == 0.0 ? 0.0 : s / t;  // every chosen score underflows (or nothing is chosen): no weight
+  int myi[NT];
+  float myl[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    myi[n] = NO_EXPERT;
+    myl[n] = -INFINITY;
   }
-  if (lane < k) {
-    idx[lane] = myi;
-    gw[lane] = (float)(s * (double)ga.scale);
+  for (int j = 0; j < k; ++j) {
+    // the largest upper word; the lower words are compared only where several lanes hold it
+    uint32_t hi[NT], low[NT];
+    bool one[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      hi[n] = (uint32_t)(key[n][0] >> 32);
+#pragma unroll
+      for (int qq = 1; qq < QE; ++qq) hi[n] = max(hi[n], (uint32_t)(key[n][qq] >> 32));
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) hi[n] = wave_max_u32(hi[n]);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      int holders = 0;
+      low[n] = 0u;
+#pragma unroll
+      for (int qq = 0; qq < QE; ++qq) {
+        const bool is = (uint32_t)(key[n][qq] >> 32) == hi[n];
+        holders += __popcll(__ballot(is));
+        low[n] = is ? max(low[n], (uint32_t)key[n][qq]) : low[n];
+      }
+      one[n] = holders == 1;
+      if (!one[n]) low[n] = wave_max_u32(low[n]);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      int best = NO_EXPERT;
+      float l = -INFINITY;
+#pragma unroll
+      for (int qq = QE - 1; qq >= 0; --qq) {
+        const uint64_t bl = __ballot((uint32_t)(key[n][qq] >> 32) == hi[n] && (one[n] || (uint32_t)key[n][qq] == low[n]));
+        const int ln = __builtin_ctzll(bl | 0x8000000000000000ull);
+        const float lv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v[n][qq]), ln));
+        best = bl ? 64 * qq + ln : best;
+        l = bl ? lv : l;
+      }
+      // nothing is left to choose from (a key above 0 has bits in its upper word)
+      if (hi[n] == 0u) {
+        best = NO_EXPERT;
+        l = -INFINITY;
+      }
+#pragma unroll
+      for (int qq = 0; qq < QE; ++qq)
+        if (lane + 64 * qq == best) key[n][qq] = 0ull;
+      if (lane == j) {
+        myi[n] = best;
+        myl[n] = l;
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const bool filled = lane < k && myi[n] != NO_EXPERT;
+    if (!ga.sigmoid && renorm) m[n] = wave_max_dpp(myl[n]);  // the largest of the chosen: the others' exponentials stay finite
+    double s = ga.sigmoid ? 1.0 / (1.0 + exp(-(double)myl[n])) : exp((double)myl[n] - (double)m[n]) / z[n];
+    if (!filled) s = 0.0;
+    if (renorm) {
+      const double t = sum8_f64(s);
+      s = t == 0.0 ? 0.0 : s / t;  // every chosen score underflows (or nothing is chosen): no weight
+    }
+    if (lane < k && n < valid) {
+      idx[n * step + lane] = myi[n];
+      gw[n * step + lane] = (float)(s * (double)ga.scale);
+    }
   }
 }
 
@@ -362,6 +424,40 @@ __global__ __launch_bounds__(64 * WE * WK) void route_fwd_kernel(const T* __rest
   // Each wavefront finishes tokens wave, wave + W, ...: fixed-order sum of the WK partials, bias, one rounding, then
   // k rounds of the wavefront maximum over order-preserving keys (lowest expert index among equal scores).
   constexpr int QE = (16 * NET * WE + 63) / 64;  // experts per lane: lane, lane + 64, ...
+  // the score of expert lane + 64 qq of a token (which is also stored)
+  auto score_of = [&](int row, int qq) -> float {
+    const int e = lane + 64 * qq, tt = t0 + row;
+    if (e >= E) return -INFINITY;
+    double sum = part[row * EW + e];
+#pragma unroll
+    for (int w = 1; w < WK; ++w) sum += part[(w * NTOK + row) * EW + e];
+    if (bias) sum += (double)bias[(size_t)(tt / bias_div) * E + e];
+    const float L = (float)sum;
+    logits[(size_t)tt * E + e] = L;
+    return L;
+  };
+  if constexpr (GATED) {
+    // as many tokens at once as the wavefront has, up to 4 (us at 1 / 2 / 4: T = 16,384, d = 128, E = 64, groups and bias
+    // 35.5 / 32.9 / 31.8; T = 8192, d = 2048, E = 256 166 / 163.3 / 162.5)
+    constexpr int NT = NTOK >= 4 * W ? 4 : NTOK >= 2 * W ? 2 : 1;
+    for (int row = wave; row < NTOK && t0 + row < Tn; row += NT * W) {
+      float v[NT][QE];
+      double* lds[NT];
+      int valid = 0;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const int r = row + n * W;
+        lds[n] = part + r * EW;
+        const bool in = t0 + r < Tn;
+        valid += in;
+#pragma unroll
+        for (int qq = 0; qq < QE; ++qq) v[n][qq] = in ? score_of(r, qq) : -INFINITY;
+      }
+      gated_select<QE, NT>(v, E, k, renorm, ga, lds, valid, (size_t)W * k, idx + (size_t)(t0 + row) * k,
+                           gw + (size_t)(t0 + row) * k);
+    }
+    return;
+  }
   for (int row = wave; row < NTOK; row += W) {
     const int tt = t0 + row;
     if (tt >= Tn) break;
@@ -369,23 +465,8 @@ __global__ __launch_bounds__(64 * WE * WK) void route_fwd_kernel(const T* __rest
     float v[QE];
 #pragma unroll
     for (int qq = 0; qq < QE; ++qq) {
-      const int e = lane + 64 * qq;
-      v[qq] = -INFINITY;
-      key[qq] = 0u;
-      if (e < E) {
-        double sum = part[row * EW + e];
-#pragma unroll
-        for (int w = 1; w < WK; ++w) sum += part[(w * NTOK + row) * EW + e];
-        if (bias) sum += (double)bias[(size_t)(tt / bias_div) * E + e];
-        const float L = (float)sum;
-        logits[(size_t)tt * E + e] = L;
-        v[qq] = L;
-        key[qq] = score_key(L);
-      }
-    }
-    if constexpr (GATED) {
-      gated_select<QE>(v, E, k, renorm, ga, part + row * EW, idx + (size_t)tt * k, gw + (size_t)tt * k);
-      continue;
+      v[qq] = score_of(row, qq);
+      key[qq] = lane + 64 * qq < E ? score_key(v[qq]) : 0u;
     }
     float myv = -INFINITY;
     int myi = 0;
