@@ -141,7 +141,8 @@ struct Q4Args {
   const int32_t* offsets;  // [Eloc + 1]
   const void* x;           // [T, d]: rows of the shared experts
   const void* xp;          // [T * k, d]
-  void* h;                 // [R, f]
+  void* h;                 // H [R, f] ...
+  int64_t h_low;           // ... of bf16 in two parts, the second this many bytes on; 0: in one
   void* y;                 // [R, d]
   const char* codes[2];    // gate, up; or down
   const bf16* scales[2];
@@ -212,36 +213,43 @@ __device__ __forceinline__ bool q4_tile(const Q4Args& p, int bid, int chunk, Q4T
   return true;
 }
 
-// The bf16 parts of eight activations: the numbers themselves, or three bf16 that add up to each fp32 number (truncated:
-// 8 + 8 + 8 bits). Infinities and NaN stay in the first part.
-template <typename T> struct Parts;
-template <> struct Parts<bf16> { static constexpr int N = 1; };
-template <> struct Parts<float> { static constexpr int N = 3; };
-template <typename T>
-struct XChunk {
-  Chunk c[8 / EPC<T>::value];
-};
-__device__ __forceinline__ void split(const XChunk<bf16>& x, Chunk (&out)[1]) { out[0] = x.c[0]; }
-__device__ __forceinline__ void split(const XChunk<float>& x, Chunk (&out)[3]) {
+// Eight activations as bf16 parts that add up to them, NP of them, and as they are loaded, XC chunks:
+//   bf16 tensors: one part (B = 1); or two (B = 2), of H, which the gate/up kernel holds in fp32 and then stores as two bf16
+//     arrays, its rounding and the rounding of the rest. Rounded to bf16 alone, H adds as much error to an output as the
+//     output's own rounding (2.3e-3 in place of 1.7e-3 of the outputs' norm). The split over K, which waits for its loads
+//     and not for products, takes two parts; the shared rows would pay 13 us of 51 (777 tokens, below) and 11 of 130 (24).
+//   fp32 tensors: three parts, exact (truncated: 8 + 8 + 8 bits), made of two chunks. Infinities and NaN stay in the first.
+template <typename T, int B>
+struct Acts {
+  static constexpr bool F32 = std::is_same<T, float>::value;
+  static constexpr int NP = F32 ? 3 : B, XC = F32 ? 2 : B;
+  Chunk c[XC];
+  __device__ __forceinline__ void parts(Chunk (&out)[NP]) const {
+    if constexpr (!F32) {
 #pragma unroll
-  for (int p = 0; p < 4; ++p) {  // pairs of values
-    uint32_t part[3][2];
+      for (int n = 0; n < NP; ++n) out[n] = c[n];
+    } else {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const uint32_t u = x.c[p / 2].w[2 * (p % 2) + e];
-      const bool special = (u & 0x7f800000u) == 0x7f800000u;
-      uint32_t hi = u & 0xffff0000u;
-      if (special && (u & 0x7fffffu)) hi = 0x7fc00000u;
-      const float r = special ? 0.f : __uint_as_float(u) - __uint_as_float(hi);
-      const uint32_t mid = __float_as_uint(r) & 0xffff0000u;
-      part[0][e] = hi;
-      part[1][e] = mid;
-      part[2][e] = __float_as_uint(r - __uint_as_float(mid));
+      for (int p = 0; p < 4; ++p) {  // pairs of values
+        uint32_t part[3][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t u = c[p / 2].w[2 * (p % 2) + e];
+          const bool special = (u & 0x7f800000u) == 0x7f800000u;
+          uint32_t hi = u & 0xffff0000u;
+          if (special && (u & 0x7fffffu)) hi = 0x7fc00000u;
+          const float r = special ? 0.f : __uint_as_float(u) - __uint_as_float(hi);
+          const uint32_t mid = __float_as_uint(r) & 0xffff0000u;
+          part[0][e] = hi;
+          part[1][e] = mid;
+          part[2][e] = __float_as_uint(r - __uint_as_float(mid));
+        }
+#pragma unroll
+        for (int n = 0; n < 3; ++n) out[n].w[p] = (part[n][0] >> 16) | (part[n][1] & 0xffff0000u);
+      }
     }
-#pragma unroll
-    for (int n = 0; n < 3; ++n) out[n].w[p] = (part[n][0] >> 16) | (part[n][1] & 0xffff0000u);
   }
-}
+};
 
 // 16 or 2 bytes at byte voff + soff of a buffer, soff wave-uniform; zeros where voff is past the end.
 __device__ __forceinline__ Chunk buf_ld16_at(__amdgpu_buffer_rsrc_t r, int voff, int soff) {
@@ -279,6 +287,16 @@ __device__ __forceinline__ void spread_scales(uint32_t v, float (&out)[SG]) {
 __device__ __forceinline__ float silu_of(float g, bf16) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
 __device__ __forceinline__ float silu_of(float g, float) { return g / (1.f + expf(-g)); }
 
+template <typename T>
+__device__ __forceinline__ void store_h(const Q4Args& p, int64_t at, float h) {
+  ((T*)p.h)[at] = from_f<T>(h);
+  if constexpr (std::is_same<T, bf16>::value)
+    if (p.h_low) {
+      const float rest = h - bf2f(f2bf(h));  // 0 where h rounds to an infinity: inf - inf would make its products NaN
+      ((bf16*)((char*)p.h + p.h_low))[at] = fabsf(rest) < INFINITY ? f2bf(rest) : (bf16)0;
+    }
+}
+
 // Up to 16 rows of a group against 16 NB columns of the output (GU: of gate and of up): the Q4_KS wavefronts take a part of K
 // each, 128 k at a time, read rows and weights straight into MFMA operands and share nothing until their sums meet in LDS
 // and are added in wavefront order. SG = 128 / group. Bound by the round trips of the loads: a wavefront's steps are few, so
@@ -286,18 +304,21 @@ __device__ __forceinline__ float silu_of(float g, float) { return g / (1.f + exp
 constexpr int Q4_KS = 8;
 template <typename T, bool GU, int NB, int SG>
 __global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
-  constexpr int NM = GU ? 2 : 1, NP = Parts<T>::N, XC = 8 / EPC<T>::value;
+  typedef Acts<T, GU ? 1 : 2> X;
+  constexpr int NM = GU ? 2 : 1, NP = X::NP, XC = X::XC, XB = sizeof(T);
   __shared__ __align__(16) floatx4 red[Q4_KS][NM * NB][64];
   Q4Tile t;
   if (!q4_tile(p, blockIdx.x, 16, t)) return;
   const int lane = threadIdx.x & 63, q = lane >> 4, li = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int K = GU ? p.d : p.f, N = GU ? p.f : p.d, units = K / 128, KB = K * (int)sizeof(T);
+  const int K = GU ? p.d : p.f, N = GU ? p.f : p.d, units = K / 128, KB = K * XB;
   const bool routed = t.g < p.Eloc;
   const int64_t rs = routed ? (int64_t)t.row0 : p.shared0 + (int64_t)(t.g - p.Eloc) * p.T;
   const char* xb = GU ? (routed ? (const char*)p.xp + (int64_t)t.row0 * KB : (const char*)p.x) : (const char*)p.h + rs * KB;
   const int m0 = t.ch * 16, m_rows = min(t.rows - m0, 16);
-  const auto xr = buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB);  // rows past the last read as zeros
+  // rows past the last read as zeros; of bf16 H also the second array
+  const __amdgpu_buffer_rsrc_t xr[2] = {buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB),
+                                        buf_rsrc(xb + (GU ? 0 : p.h_low) + (int64_t)m0 * KB, (size_t)m_rows * KB)};
   const int u0 = (int)((int64_t)units * w / Q4_KS), u1 = (int)((int64_t)units * (w + 1) / Q4_KS);
   const int nb0 = t.nb * NB;  // first 16-column block
   __amdgpu_buffer_rsrc_t cr[NM], sr[NM];
@@ -310,14 +331,14 @@ __global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
   struct Stage {
     Chunk c[NM][NB];
     uint32_t s[NM][NB];
-    XChunk<T> x[4];
+    X x[4];
   } st;
   auto load = [&](int u) {
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
       for (int c = 0; c < XC; ++c)
-        st.x[s].c[c] = buf_ld16_at(xr, li * KB + (32 * s + 8 * q) * (int)sizeof(T) + 16 * c, u * 128 * (int)sizeof(T));
+        st.x[s].c[c] = buf_ld16_at(xr[X::F32 ? 0 : c], li * KB + (32 * s + 8 * q) * XB + (X::F32 ? 16 * c : 0), u * 128 * XB);
 #pragma unroll
     for (int a = 0; a < NM; ++a)
 #pragma unroll
@@ -336,7 +357,7 @@ __global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
   for (int u = u0; u < u1; ++u) {
     Chunk xs[4][NP];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) split(st.x[s], xs[s]);
+    for (int s = 0; s < 4; ++s) st.x[s].parts(xs[s]);
 #pragma unroll
     for (int a = 0; a < NM; ++a)
 #pragma unroll
@@ -381,7 +402,7 @@ __global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
   for (int r = 0; r < 4; ++r) {
     if (4 * q + r >= m_rows) break;
     const int64_t row = rs + m0 + 4 * q + r;
-    if constexpr (GU) ((T*)p.h)[row * p.f + col] = from_f<T>(silu_of(v[0][r], T{}) * v[NM - 1][r]);
+    if constexpr (GU) store_h<T>(p, row * p.f + col, silu_of(v[0][r], T{}) * v[NM - 1][r]);
     else ((T*)p.y)[row * p.d + col] = from_f<T>(v[0][r]);
   }
 }
@@ -394,19 +415,20 @@ __global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
 template <typename T, bool GU, int MT, int NF, int SG, int D>
 __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
   static_assert(D % 2 == 0, "the steps of a round alternate between two LDS stages");
-  constexpr int NM = GU ? 2 : 1, NP = Parts<T>::N, XC = 8 / EPC<T>::value, ROWS = 16 * MT;
+  typedef Acts<T, 1> X;
+  constexpr int NM = GU ? 2 : 1, NP = X::NP, XC = X::XC, XB = sizeof(T), ROWS = 16 * MT;
   constexpr int PLANE = ROWS * 256;
   __shared__ __align__(16) char xs[2][NP * PLANE];
   Q4Tile t;
   if (!q4_tile(p, blockIdx.x, ROWS, t)) return;
   const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, li = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int K = GU ? p.d : p.f, N = GU ? p.f : p.d, units = K / 128, KB = K * (int)sizeof(T);
+  const int K = GU ? p.d : p.f, N = GU ? p.f : p.d, units = K / 128, KB = K * XB;
   const bool routed = t.g < p.Eloc;
   const int64_t rs = routed ? (int64_t)t.row0 : p.shared0 + (int64_t)(t.g - p.Eloc) * p.T;
   const char* xb = GU ? (routed ? (const char*)p.xp + (int64_t)t.row0 * KB : (const char*)p.x) : (const char*)p.h + rs * KB;
   const int m0 = t.ch * ROWS, m_rows = min(t.rows - m0, ROWS);
-  const auto xr = buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB);
+  const auto xr = buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB);  // rows past the last read as zeros
   const int nb0 = (t.nb * 4 + w) * NF;  // the wavefront's first 16-column block
   __amdgpu_buffer_rsrc_t cr[NM], sr[NM];
 #pragma unroll
@@ -432,22 +454,22 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
       }
   };
   // eight activations of row r, columns 8 c .. 8 c + 7 of the step: thread tid takes (r, c) = item tid + 256 j
-  auto load_x = [&](int u, XChunk<T> (&x)[MT]) {
-    const int so = u < units ? u * 128 * (int)sizeof(T) : 0;
+  auto load_x = [&](int u, X (&x)[MT]) {
+    const int so = u < units ? u * 128 * XB : 0;
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
       const int it = tid + 256 * j;
 #pragma unroll
       for (int c = 0; c < XC; ++c)
-        x[j].c[c] = buf_ld16_at(xr, u < units ? (it >> 4) * KB + 8 * (it & 15) * (int)sizeof(T) + 16 * c : kBufPast, so);
+        x[j].c[c] = buf_ld16_at(xr, u < units ? (it >> 4) * KB + 8 * (it & 15) * XB + 16 * c : kBufPast, so);
     }
   };
-  auto put_x = [&](int stage, const XChunk<T> (&x)[MT]) {
+  auto put_x = [&](int stage, const X (&x)[MT]) {
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
       const int it = tid + 256 * j, r = it >> 4;
       Chunk part[NP];
-      split(x[j], part);
+      x[j].parts(part);
 #pragma unroll
       for (int n = 0; n < NP; ++n) st_chunk(xs[stage] + n * PLANE + r * 256 + (((it & 15) ^ (r & 15)) << 4), part[n]);
     }
@@ -517,7 +539,7 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
         for (int m = 0; m < ML; ++m) asm volatile("" : "+v"(acc[a][i][m]));
   };
   Weights wt[D];
-  XChunk<T> xv[D][MT];
+  X xv[D][MT];
 #pragma unroll
   for (int j = 0; j < D - 1; ++j) {
     load_x(j, xv[j]);
@@ -552,7 +574,7 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
       for (int i = 0; i < NF; ++i) {
         const int col = (nb0 + i) * 16 + li;
         if constexpr (GU)
-          ((T*)p.h)[row * p.f + col] = from_f<T>(silu_of(acc[0][i][m][r], T{}) * acc[NM - 1][i][m][r]);
+          store_h<T>(p, row * p.f + col, silu_of(acc[0][i][m][r], T{}) * acc[NM - 1][i][m][r]);
         else
           ((T*)p.y)[row * p.d + col] = from_f<T>(acc[0][i][m][r]);
       }
@@ -604,14 +626,23 @@ hipError_t q4_run_rows(const moe_desc& d, Q4Args a, hipStream_t s) {
 //             777, 1024, 2816, 16, 2    95.2 / 67.4 / 38.2 / 30.7           56.9 / 37.0 / 23.2 / 20.2
 // Measured and not kept: 64- and 128-row chunks (777 rows: 36.8 and 49 us of gate/up), four and sixteen wavefronts of a
 // split, deeper prefetch in the split, non-temporal loads of the codes (equal, and worse where calls follow each other).
-template <typename T, bool GU, int SG>
-hipError_t q4_pick(const moe_desc& d, const Q4Args& a, hipStream_t s) {
+struct Q4Pick {
+  double rows;  // per active expert
+  bool split;   // K over the wavefronts
+};
+Q4Pick q4_rule(const moe_desc& d, int group, bool gate_up) {
   const double share = (double)d.top_k / d.n_experts;
   const double active = d.local_count * (1 - std::pow(1 - share, d.T)) + d.n_shared;
   const double rows = d.T * (share * d.local_count + d.n_shared) / active;
-  const double bytes = active * (GU ? 2 : 1) * d.d_ff * d.d_model * (0.5 + SG / 64.0);
-  const double chain = 2 + (GU ? 0.45 : 0.36) * ((GU ? d.d_model : d.d_ff) / 128);
-  if (rows <= 12 && chain > bytes / 5.5e6)
+  const double bytes = active * (gate_up ? 2 : 1) * d.d_ff * d.d_model * (0.5 + 2.0 / group);
+  const double chain = 2 + (gate_up ? 0.45 * (d.d_model / 128) : 0.36 * (d.d_ff / 128));
+  return {rows, rows <= 12 && chain > bytes / 5.5e6};
+}
+
+template <typename T, bool GU, int SG>
+hipError_t q4_pick(const moe_desc& d, const Q4Args& a, hipStream_t s) {
+  const auto [rows, split] = q4_rule(d, 128 / SG, GU);
+  if (split)
     return rows <= 2 ? q4_run_split<T, GU, 2, SG>(d, a, s) : q4_run_split<T, GU, 4, SG>(d, a, s);
   if constexpr (GU) return rows <= 8 ? q4_run_rows<T, GU, 1, 1, SG, 2>(d, a, s) : q4_run_rows<T, GU, 2, 1, SG, 2>(d, a, s);
   else return rows <= 40 ? q4_run_rows<T, GU, 1, 1, SG, 4>(d, a, s) : q4_run_rows<T, GU, 2, 2, SG, 2>(d, a, s);
@@ -640,7 +671,9 @@ hipError_t q4_ffn(const moe_desc& d, int group, const Q4Args& a, const Q4Weights
 
 }  // namespace
 
-size_t ffn_q4_ws_bytes(const moe_desc& d) { return align256((size_t)rows_total(d) * d.d_ff * elem_bytes(d)); }
+// H, in bf16 with room for a second array
+static size_t h_bytes(const moe_desc& d) { return align256((size_t)rows_total(d) * d.d_ff * elem_bytes(d)); }
+size_t ffn_q4_ws_bytes(const moe_desc& d) { return h_bytes(d) * (d.dtype == MOE_BF16 ? 2 : 1); }
 
 hipError_t launch_ffn_q4(const moe_desc& d, int group, const void* x, const void* xp, const int32_t* offsets,
                          const Q4Weights& gate, const Q4Weights& up, const Q4Weights& down, void* yp, void* ws,
@@ -656,6 +689,7 @@ hipError_t launch_ffn_q4(const moe_desc& d, int group, const void* x, const void
   a.x = x;
   a.xp = xp;
   a.h = ws;
+  a.h_low = d.dtype == MOE_BF16 && q4_rule(d, group, false).split ? (int64_t)h_bytes(d) : 0;
   a.y = yp;
   if (d.dtype == MOE_BF16) return q4_ffn<bf16>(d, group, a, gate, up, down, s);
   return q4_ffn<float>(d, group, a, gate, up, down, s);
