@@ -287,14 +287,10 @@ __device__ __forceinline__ void spread_scales(uint32_t v, float (&out)[SG]) {
 __device__ __forceinline__ float silu_of(float g, bf16) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
 __device__ __forceinline__ float silu_of(float g, float) { return g / (1.f + expf(-g)); }
 
-template <typename T>
-__device__ __forceinline__ void store_h(const Q4Args& p, int64_t at, float h) {
-  ((T*)p.h)[at] = from_f<T>(h);
-  if constexpr (std::is_same<T, bf16>::value)
-    if (p.h_low) {
-      const float rest = h - bf2f(f2bf(h));  // 0 where h rounds to an infinity: inf - inf would make its products NaN
-      ((bf16*)((char*)p.h + p.h_low))[at] = fabsf(rest) < INFINITY ? f2bf(rest) : (bf16)0;
-    }
+// The second part of a bf16 H: the rest of its rounding; 0 where h rounds to an infinity (inf - inf makes products NaN).
+__device__ __forceinline__ void store_h_low(const Q4Args& p, int64_t at, float h, bool in) {
+  const float rest = h - bf2f(f2bf(h));
+  if (in) ((bf16*)((char*)p.h + p.h_low))[at] = fabsf(rest) < INFINITY ? f2bf(rest) : (bf16)0;
 }
 
 // Up to 16 rows of a group against 16 NB columns of the output (GU: of gate and of up): the Q4_KS wavefronts take a part of K
@@ -402,8 +398,14 @@ __global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
   for (int r = 0; r < 4; ++r) {
     if (4 * q + r >= m_rows) break;
     const int64_t row = rs + m0 + 4 * q + r;
-    if constexpr (GU) store_h<T>(p, row * p.f + col, silu_of(v[0][r], T{}) * v[NM - 1][r]);
-    else ((T*)p.y)[row * p.d + col] = from_f<T>(v[0][r]);
+    if constexpr (GU) {
+      const float h = silu_of(v[0][r], T{}) * v[NM - 1][r];
+      ((T*)p.h)[row * p.f + col] = from_f<T>(h);
+      if constexpr (std::is_same<T, bf16>::value)
+        if (p.h_low) store_h_low(p, row * p.f + col, h, true);
+    } else {
+      ((T*)p.y)[row * p.d + col] = from_f<T>(v[0][r]);
+    }
   }
 }
 
@@ -564,21 +566,32 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
   // a loop of its own for half a chunk of rows (a branch inside one loop has its sides' conversions hoisted, and spills)
   if (MT >= 2 && m_rows <= 8 * MT) loop(std::integral_constant<int, (MT + 1) / 2>{});
   else loop(std::integral_constant<int, MT>{});
+  // Through LDS, so that the stores are 16 bytes a lane and whole rows of the workgroup's columns: a lane's own values are
+  // four rows of one column (by themselves 771 x 128, f = 5888, 24 experts, top-8 takes 87 us of gate/up, most of it stores).
+  constexpr int CB = 64 * NF * XB, PITCH = CB + 16;  // bytes of a row
+  static_assert(ROWS * PITCH <= (int)sizeof(xs), "the output tile");
+  char* out = xs[0];
+  __syncthreads();
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      if (16 * m + 4 * q + r >= m_rows) break;
-      const int64_t row = rs + m0 + 16 * m + 4 * q + r;
+    for (int i = 0; i < NF; ++i)
 #pragma unroll
-      for (int i = 0; i < NF; ++i) {
-        const int col = (nb0 + i) * 16 + li;
-        if constexpr (GU)
-          store_h<T>(p, row * p.f + col, silu_of(acc[0][i][m][r], T{}) * acc[NM - 1][i][m][r]);
-        else
-          ((T*)p.y)[row * p.d + col] = from_f<T>(acc[0][i][m][r]);
+      for (int r = 0; r < 4; ++r) {
+        float v = acc[0][i][m][r];
+        if constexpr (GU) v = silu_of(v, T{}) * acc[NM - 1][i][m][r];
+        if constexpr (GU && std::is_same<T, bf16>::value)
+          if (p.h_low) store_h_low(p, (rs + m0 + 16 * m + 4 * q + r) * p.f + (nb0 + i) * 16 + li, v, 16 * m + 4 * q + r < m_rows);
+        *reinterpret_cast<T*>(out + (16 * m + 4 * q + r) * PITCH + ((w * NF + i) * 16 + li) * XB) = from_f<T>(v);
       }
-    }
+  __syncthreads();
+  constexpr int PER = CB / 16;  // 16-byte chunks of a row
+  for (int c = tid; c < ROWS * PER; c += 256) {
+    const int r = c / PER, o = (c - r * PER) * 16;
+    if (r >= m_rows) break;
+    char* dst = GU ? (char*)p.h + (rs + m0 + r) * p.f * XB : (char*)p.y + (rs + m0 + r) * p.d * XB;
+    st_chunk(dst + (int64_t)t.nb * CB + o, ld_chunk(out + r * PITCH + o));
+  }
 }
 
 // ------------------------------------------------------------------------- host side
