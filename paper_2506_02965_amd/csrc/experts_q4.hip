@@ -137,6 +137,7 @@ __global__ __launch_bounds__(256) void q4_unpack_kernel(int64_t blocks, int kb, 
 
 struct Q4Args {
   int T, f, d, Eloc, S, n_blocks;
+  int walk;                // q4_short_kernel: column blocks of a workgroup
   int64_t shared0;         // T * k: first row of the shared experts in the row space
   const int32_t* offsets;  // [Eloc + 1]
   const void* x;           // [T, d]: rows of the shared experts
@@ -409,11 +410,89 @@ __global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
   }
 }
 
+// Codes and scales of a wavefront's columns for one step of 128 k, and the step's products of ML row blocks. The rows lie in
+// LDS as the NP parts that the MFMAs take, PLANE bytes each: 256 bytes a row, 16-byte chunk c of row r at c ^ (r & 15), so
+// that the 16 rows of an operand read fall on different banks. A read runs while the products of the one before do.
+template <int NM, int NF, int SG>
+struct Q4Step {
+  Chunk c[NM][NF];
+  uint32_t s[NM][NF];
+  // block i of 16 columns, step u: `blk` is i * units + u, `past` 0 or kBufPast (zeros)
+  __device__ __forceinline__ void load(int a, int i, __amdgpu_buffer_rsrc_t cr, __amdgpu_buffer_rsrc_t sr, int blk, int past) {
+    const int lane = threadIdx.x & 63;
+    c[a][i] = buf_ld16_at(cr, lane * 16 | past, blk * 1024);
+    s[a][i] = buf_ld2_at(sr, (((lane >> 4) % SG) * 32 + 2 * (lane & 15)) | past, blk * SG * 32);
+  }
+  template <int NP, int ML, int MT>
+  __device__ __forceinline__ void mul(const char* xs, int plane, floatx4 (&acc)[NM][NF][MT]) const {
+    const int lane = threadIdx.x & 63, q = lane >> 4, li = lane & 15;
+    Chunk xf[2][ML][NP];
+    auto read = [&](int k, Chunk (&f)[ML][NP]) {
+#pragma unroll
+      for (int m = 0; m < ML; ++m)
+#pragma unroll
+        for (int n = 0; n < NP; ++n) f[m][n] = ld_chunk(xs + n * plane + (16 * m + li) * 256 + (((4 * k + q) ^ li) << 4));
+    };
+    read(0, xf[0]);
+    float sc[NM][NF][SG];
+#pragma unroll
+    for (int a = 0; a < NM; ++a)
+#pragma unroll
+      for (int i = 0; i < NF; ++i) spread_scales<SG>(s[a][i], sc[a][i]);
+    floatx4 sum[NM][NF][ML];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k < 3) read(k + 1, xf[(k + 1) & 1]);
+      const int z = k * SG / 4;
+#pragma unroll
+      for (int a = 0; a < NM; ++a)
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+          const Chunk wv = codes8(c[a][i].w[k]);
+#pragma unroll
+          for (int m = 0; m < ML; ++m) {
+            if (k % (4 / SG) == 0) sum[a][i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int n = 0; n < NP; ++n)
+              sum[a][i][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xf[k & 1][m][n]),
+                                                                     __builtin_bit_cast(bf16x8, wv), sum[a][i][m], 0, 0, 0);
+          }
+        }
+      if ((k + 1) % (4 / SG) == 0) {
+#pragma unroll
+        for (int a = 0; a < NM; ++a)
+#pragma unroll
+          for (int i = 0; i < NF; ++i)
+#pragma unroll
+            for (int m = 0; m < ML; ++m)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[a][i][m][r] = fmaf(sc[a][i][z], sum[a][i][m][r], acc[a][i][m][r]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the sums are due here: left alone, the compiler moves the scaling past the next branch, with every product live
+#pragma unroll
+    for (int a = 0; a < NM; ++a)
+#pragma unroll
+      for (int i = 0; i < NF; ++i)
+#pragma unroll
+        for (int m = 0; m < ML; ++m) asm volatile("" : "+v"(acc[a][i][m]));
+  }
+};
+
+// Item j of 256 of a step's rows: eight activations of row r, columns 8 c .. 8 c + 7, into LDS as above.
+template <int NP, typename X>
+__device__ __forceinline__ void put_acts(char* xs, int plane, int it, const X& x) {
+  const int r = it >> 4;
+  Chunk part[NP];
+  x.parts(part);
+#pragma unroll
+  for (int n = 0; n < NP; ++n) st_chunk(xs + n * plane + r * 256 + (((it & 15) ^ (r & 15)) << 4), part[n]);
+}
+
 // Up to 16 MT rows of a group against 64 NF columns of the output: the four wavefronts split the columns (16 NF each; GU: of
 // gate and of up) and share the rows, which pass through LDS 128 k at a time in two stages, as the bf16 parts that the MFMAs
-// take. One barrier per step; the next step's rows and codes are loaded while this one is multiplied.
-// LDS rows: 256 bytes of one part, 16-byte chunk c of row r at c ^ (r & 15): the 16 rows of an operand read fall on
-// different banks.
+// take. One barrier per step; the next steps' rows and codes are loaded while this one is multiplied.
 template <typename T, bool GU, int MT, int NF, int SG, int D>
 __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
   static_assert(D % 2 == 0, "the steps of a round alternate between two LDS stages");
@@ -439,21 +518,13 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
     cr[a] = buf_rsrc(p.codes[a] + blk * 1024, (size_t)NF * units * 1024);
     sr[a] = buf_rsrc((const char*)p.scales[a] + blk * SG * 32, (size_t)NF * units * SG * 32);
   }
-  struct Weights {
-    Chunk c[NM][NF];
-    uint32_t s[NM][NF];
-  };
-  // steps past the end read zeros
-  auto load_w = [&](int u, Weights& st) {
+  typedef Q4Step<NM, NF, SG> Weights;
+  auto load_w = [&](int u, Weights& st) {  // steps past the end read zeros
     const int past = u < units ? 0 : kBufPast;
 #pragma unroll
     for (int a = 0; a < NM; ++a)
 #pragma unroll
-      for (int i = 0; i < NF; ++i) {
-        const int o = u < units ? i * units + u : 0;
-        st.c[a][i] = buf_ld16_at(cr[a], lane * 16 | past, o * 1024);
-        st.s[a][i] = buf_ld2_at(sr[a], ((q % SG) * 32 + 2 * li) | past, o * SG * 32);
-      }
+      for (int i = 0; i < NF; ++i) st.load(a, i, cr[a], sr[a], u < units ? i * units + u : 0, past);
   };
   // eight activations of row r, columns 8 c .. 8 c + 7 of the step: thread tid takes (r, c) = item tid + 256 j
   auto load_x = [&](int u, X (&x)[MT]) {
@@ -468,13 +539,7 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
   };
   auto put_x = [&](int stage, const X (&x)[MT]) {
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-      const int it = tid + 256 * j, r = it >> 4;
-      Chunk part[NP];
-      x[j].parts(part);
-#pragma unroll
-      for (int n = 0; n < NP; ++n) st_chunk(xs[stage] + n * PLANE + r * 256 + (((it & 15) ^ (r & 15)) << 4), part[n]);
-    }
+    for (int j = 0; j < MT; ++j) put_acts<NP>(xs[stage], PLANE, tid + 256 * j, x[j]);
   };
   floatx4 acc[NM][NF][MT];
 #pragma unroll
@@ -483,63 +548,6 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
     for (int i = 0; i < NF; ++i)
 #pragma unroll
       for (int m = 0; m < MT; ++m) acc[a][i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
-  // One step of 128 k on the first ML row blocks (those past the chunk's rows are left out, in halves of the chunk): an
-  // operand of the rows is read from LDS while the products of the one before run.
-  auto mul = [&](int stage, const Weights& st, auto ml) {
-    constexpr int ML = decltype(ml)::value;
-    Chunk xf[2][ML][NP];
-    auto read = [&](int s, Chunk (&f)[ML][NP]) {
-#pragma unroll
-      for (int m = 0; m < ML; ++m)
-#pragma unroll
-        for (int n = 0; n < NP; ++n)
-          f[m][n] = ld_chunk(xs[stage] + n * PLANE + (16 * m + li) * 256 + (((4 * s + q) ^ li) << 4));
-    };
-    read(0, xf[0]);
-    float sc[NM][NF][SG];
-#pragma unroll
-    for (int a = 0; a < NM; ++a)
-#pragma unroll
-      for (int i = 0; i < NF; ++i) spread_scales<SG>(st.s[a][i], sc[a][i]);
-    floatx4 sum[NM][NF][ML];
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      if (s < 3) read(s + 1, xf[(s + 1) & 1]);
-      const int z = s * SG / 4;
-#pragma unroll
-      for (int a = 0; a < NM; ++a)
-#pragma unroll
-        for (int i = 0; i < NF; ++i) {
-          const Chunk wv = codes8(st.c[a][i].w[s]);
-#pragma unroll
-          for (int m = 0; m < ML; ++m) {
-            if (s % (4 / SG) == 0) sum[a][i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int n = 0; n < NP; ++n)
-              sum[a][i][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xf[s & 1][m][n]),
-                                                                     __builtin_bit_cast(bf16x8, wv), sum[a][i][m], 0, 0, 0);
-          }
-        }
-      if ((s + 1) % (4 / SG) == 0) {
-#pragma unroll
-        for (int a = 0; a < NM; ++a)
-#pragma unroll
-          for (int i = 0; i < NF; ++i)
-#pragma unroll
-            for (int m = 0; m < ML; ++m)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) acc[a][i][m][r] = fmaf(sc[a][i][z], sum[a][i][m][r], acc[a][i][m][r]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    // the sums are due here: left alone, the compiler moves the scaling past the next branch, with every product live
-#pragma unroll
-    for (int a = 0; a < NM; ++a)
-#pragma unroll
-      for (int i = 0; i < NF; ++i)
-#pragma unroll
-        for (int m = 0; m < ML; ++m) asm volatile("" : "+v"(acc[a][i][m]));
-  };
   Weights wt[D];
   X xv[D][MT];
 #pragma unroll
@@ -558,12 +566,13 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
         load_x(u0 + j + D - 1, xv[(j + D - 1) % D]);
         load_w(u0 + j + D - 1, wt[(j + D - 1) % D]);
         __builtin_amdgcn_sched_barrier(0);
-        mul(j & 1, wt[j], ml);
+        wt[j].template mul<NP, decltype(ml)::value>(xs[j & 1], PLANE, acc);
         put_x((j + 1) & 1, xv[(j + 1) % D]);
       }
     }
   };
-  // a loop of its own for half a chunk of rows (a branch inside one loop has its sides' conversions hoisted, and spills)
+  // Row blocks past the chunk's rows are left out, in halves of the chunk, by a loop of its own (a branch inside one loop
+  // has its sides' conversions hoisted, and spills).
   if (MT >= 2 && m_rows <= 8 * MT) loop(std::integral_constant<int, (MT + 1) / 2>{});
   else loop(std::integral_constant<int, MT>{});
   // Through LDS, so that the stores are 16 bytes a lane and whole rows of the workgroup's columns: a lane's own values are
@@ -594,6 +603,114 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
   }
 }
 
+// K of up to 256 (U = 1 or 2 steps): the group's rows stay in LDS and the four wavefronts, with 16 NF columns each, walk over
+// p.walk blocks of 64 NF columns, the next block's weights loading meanwhile. Nothing is shared after the rows are there:
+// each wavefront turns its outputs in LDS of its own. In q4_rows_kernel, whose workgroup ends after one block, finding the
+// tile and waiting for the first loads were most of such a workgroup's time (771 tokens, d = 128, f = 5888, 24 experts, top-8:
+// gate/up 70 us there).
+template <typename T, bool GU, int MT, int NF, int SG, int U>
+__global__ __launch_bounds__(256, 2) void q4_short_kernel(Q4Args p) {
+  typedef Acts<T, (GU || MT > 1) ? 1 : 2> X;  // up to 16 rows H comes in two parts
+  constexpr int NM = GU ? 2 : 1, NP = X::NP, XC = X::XC, XB = sizeof(T), ROWS = 16 * MT, PLANE = ROWS * 256;
+  constexpr int CB = 16 * NF * XB, PITCH = CB + 16;  // bytes of a wavefront's output row
+  __shared__ __align__(16) char xs[U][NP * PLANE];
+  __shared__ __align__(16) char turn[4][ROWS * PITCH];
+  Q4Tile t;
+  if (!q4_tile(p, blockIdx.x, ROWS, t)) return;
+  const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, li = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int N = GU ? p.f : p.d, units = U, KB = U * 128 * XB;
+  const bool routed = t.g < p.Eloc;
+  const int64_t rs = routed ? (int64_t)t.row0 : p.shared0 + (int64_t)(t.g - p.Eloc) * p.T;
+  const char* xb = GU ? (routed ? (const char*)p.xp + (int64_t)t.row0 * KB : (const char*)p.x) : (const char*)p.h + rs * KB;
+  const int m0 = t.ch * ROWS, m_rows = min(t.rows - m0, ROWS);
+  // rows past the last read as zeros; of bf16 H in two parts also the second array
+  const __amdgpu_buffer_rsrc_t xr[2] = {buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB),
+                                        buf_rsrc(xb + (GU ? 0 : p.h_low) + (int64_t)m0 * KB, (size_t)m_rows * KB)};
+  // column blocks b0 .. b1 of 64 NF columns
+  const int b0 = t.nb * p.walk, b1 = min(b0 + p.walk, N / (64 * NF));
+  typedef Q4Step<NM, NF, SG> Weights;
+  __amdgpu_buffer_rsrc_t cr[NM], sr[NM];
+#pragma unroll
+  for (int a = 0; a < NM; ++a) {
+    const int64_t blk = ((int64_t)t.g * (N / 16) + (b0 * 4 + w) * NF) * units;
+    const size_t n = ((size_t)(b1 - b0 - 1) * 4 + 1) * NF * units;
+    cr[a] = buf_rsrc(p.codes[a] + blk * 1024, n * 1024);
+    sr[a] = buf_rsrc((const char*)p.scales[a] + blk * SG * 32, n * SG * 32);
+  }
+  auto load_w = [&](int b, Weights (&st)[U]) {
+    const int past = b < b1 ? 0 : kBufPast;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int a = 0; a < NM; ++a)
+#pragma unroll
+        for (int i = 0; i < NF; ++i) st[u].load(a, i, cr[a], sr[a], b < b1 ? ((b - b0) * 4 * NF + i) * units + u : 0, past);
+  };
+  Weights wt[2][U];
+  {
+    X x[U][MT];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < MT; ++j) {
+        const int it = tid + 256 * j;
+#pragma unroll
+        for (int c = 0; c < XC; ++c)
+          x[u][j].c[c] = buf_ld16_at(xr[X::F32 ? 0 : c], (it >> 4) * KB + 8 * (it & 15) * XB + (X::F32 ? 16 * c : 0), u * 128 * XB);
+      }
+    load_w(b0, wt[0]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < MT; ++j) put_acts<NP>(xs[u], PLANE, tid + 256 * j, x[u][j]);
+  }
+  __syncthreads();
+  char* out = turn[w];
+  for (int bb = b0; bb < b1; bb += 2) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int b = bb + j;
+      if (b >= b1) break;
+      load_w(b + 1, wt[j ^ 1]);
+      __builtin_amdgcn_sched_barrier(0);
+      floatx4 acc[NM][NF][MT];
+#pragma unroll
+      for (int a = 0; a < NM; ++a)
+#pragma unroll
+        for (int i = 0; i < NF; ++i)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[a][i][m] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < U; ++u) wt[j][u].template mul<NP, MT>(xs[u], PLANE, acc);
+      const int col = (b * 4 + w) * 16 * NF;
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < NF; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int row = 16 * m + 4 * q + r;
+            float v = acc[0][i][m][r];
+            if constexpr (GU) v = silu_of(v, T{}) * acc[NM - 1][i][m][r];
+            if constexpr (GU && std::is_same<T, bf16>::value)
+              if (p.h_low) store_h_low(p, (rs + m0 + row) * p.f + col + 16 * i + li, v, row < m_rows);
+            *reinterpret_cast<T*>(out + row * PITCH + (16 * i + li) * XB) = from_f<T>(v);
+          }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      constexpr int PER = CB / 16;  // 16-byte chunks of a row
+#pragma unroll
+      for (int c = 0; c < ROWS * PER / 64; ++c) {
+        const int r = (c * 64 + lane) / PER, o = (c * 64 + lane) % PER * 16;
+        char* dst = GU ? (char*)p.h + (rs + m0 + r) * p.f * XB : (char*)p.y + (rs + m0 + r) * p.d * XB;
+        if (r < m_rows) st_chunk(dst + (int64_t)col * XB + o, ld_chunk(out + r * PITCH + o));
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+  }
+}
+
 // ------------------------------------------------------------------------- host side
 
 // Upper bound on the row chunks: each routed chunk holds at least one row, and all but one per group are full.
@@ -621,12 +738,28 @@ hipError_t q4_run_rows(const moe_desc& d, Q4Args a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <typename T, bool GU, int MT, int SG, int U>
+hipError_t q4_run_short(const moe_desc& d, Q4Args a, hipStream_t s) {
+  constexpr int NF = 2;
+  const int blocks = (GU ? d.d_ff : d.d_model) / (64 * NF);
+  // four workgroups per CU, as long as each has a block
+  const int64_t chunks = chunks_of(d, 16 * MT);
+  a.walk = (int)std::max<int64_t>(1, std::min<int64_t>(blocks, chunks * blocks / (4 * device_cus())));
+  a.n_blocks = (blocks + a.walk - 1) / a.walk;
+  const unsigned grid = (unsigned)((chunks * a.n_blocks + 7) / 8 * 8);
+  KernelTimer kt(GU ? "q4_gate_up" : "q4_down", s);
+  hipLaunchKernelGGL((q4_short_kernel<T, GU, MT, NF, SG, U>), dim3(grid), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 // Which kernel a projection takes, by the rows that an active expert can expect (the counts stay on the device; a shard's
-// share of the slots, experts equally likely) and by whether the shared-rows kernel would be bound by the chain of its steps
-// (0.45 and 0.36 us each, gate/up and down, and 2 us around them) rather than by reading the weights (5.5 TB/s):
-//   * chain-bound and up to 12 rows: K split over 8 wavefronts, 32 columns each up to 2 rows, 64 above;
+// share of the slots, experts equally likely):
+//   * K up to 256: the walking kernel, 16-row chunks up to 16 rows, 32-row chunks above;
+//   * up to 12 rows where the shared-rows kernel would be bound by the chain of its steps (0.45 and 0.36 us each, gate/up
+//     and down, and 2 us around them) rather than by reading the weights (5.5 TB/s): K split over 8 wavefronts, 32 columns
+//     up to 2 rows, 64 above;
 //   * else shared rows. Gate/up: 16-row chunks up to 8 rows, 32-row chunks above. Down, whose K is the long one: 16-row
-//     chunks with four steps in flight up to 40 rows, 32-row chunks and 128 columns above.
+//     chunks with four steps in flight, or, above 40 rows and where that leaves a workgroup per CU, 32 rows x 128 columns.
 // us of split 32 / split 64 / rows 16 / rows 32 (down: rows 16 / rows 32 x 128), group 64, at T, d, f, E, k, shared:
 //   gate/up:  1, 2048, 1408, 64, 6, 2   10.1 /  9.9 / 11.2 / 12.6     down:  7.3 /  7.4 /  8.2 /  9.5
 //             1, 4096, 14336, 8, 2      27.0 / 26.8 / 25.5 / 28.5           17.6 / 21.0 / 38.9 / 66.8
@@ -637,28 +770,40 @@ hipError_t q4_run_rows(const moe_desc& d, Q4Args a, hipStream_t s) {
 //             64, 1024, 2816, 16, 2     19.2 / 16.1 / 14.0 / 12.5           11.2 /  9.4 / 11.0 / 13.9
 //             128, 4096, 14336, 8, 2   219.3 / 163  / 136  / 124           167   / 107  / 91.2 / 85.3
 //             777, 1024, 2816, 16, 2    95.2 / 67.4 / 38.2 / 30.7           56.9 / 37.0 / 23.2 / 20.2
+//             254, 128, 6912, 8, 4                                          31.3 / 21.8 / 18.5 / 28.6
+// Walking / rows 32: gate/up 771, 128, 5888, 24, 8 50 / 73; 700, 256, 14336, 4, 2 43 / 50; down 451, 4096, 128, 256, 8, 2
+// 31 / 70 (rows 32 x 128: 51); 451, 4096, 256, 64, 8, 2 27 / 41 (34).
 // Measured and not kept: 64- and 128-row chunks (777 rows: 36.8 and 49 us of gate/up), four and sixteen wavefronts of a
 // split, deeper prefetch in the split, non-temporal loads of the codes (equal, and worse where calls follow each other).
 struct Q4Pick {
   double rows;  // per active expert
+  int units;    // steps of 128 k
   bool split;   // K over the wavefronts
+  bool two;     // the projection (down) reads H in two parts
 };
 Q4Pick q4_rule(const moe_desc& d, int group, bool gate_up) {
   const double share = (double)d.top_k / d.n_experts;
   const double active = d.local_count * (1 - std::pow(1 - share, d.T)) + d.n_shared;
   const double rows = d.T * (share * d.local_count + d.n_shared) / active;
+  const int units = (gate_up ? d.d_model : d.d_ff) / 128;
   const double bytes = active * (gate_up ? 2 : 1) * d.d_ff * d.d_model * (0.5 + 2.0 / group);
-  const double chain = 2 + (gate_up ? 0.45 * (d.d_model / 128) : 0.36 * (d.d_ff / 128));
-  return {rows, rows <= 12 && chain > bytes / 5.5e6};
+  const double chain = 2 + (gate_up ? 0.45 : 0.36) * units;
+  const bool split = units > 2 && rows <= 12 && chain > bytes / 5.5e6;
+  return {rows, units, split, split || (units <= 2 && rows <= 16)};
 }
 
 template <typename T, bool GU, int SG>
 hipError_t q4_pick(const moe_desc& d, const Q4Args& a, hipStream_t s) {
-  const auto [rows, split] = q4_rule(d, 128 / SG, GU);
-  if (split)
-    return rows <= 2 ? q4_run_split<T, GU, 2, SG>(d, a, s) : q4_run_split<T, GU, 4, SG>(d, a, s);
-  if constexpr (GU) return rows <= 8 ? q4_run_rows<T, GU, 1, 1, SG, 2>(d, a, s) : q4_run_rows<T, GU, 2, 1, SG, 2>(d, a, s);
-  else return rows <= 40 ? q4_run_rows<T, GU, 1, 1, SG, 4>(d, a, s) : q4_run_rows<T, GU, 2, 2, SG, 2>(d, a, s);
+  const Q4Pick k = q4_rule(d, 128 / SG, GU);
+  if (k.units == 1) return k.rows <= 16 ? q4_run_short<T, GU, 1, SG, 1>(d, a, s) : q4_run_short<T, GU, 2, SG, 1>(d, a, s);
+  if (k.units == 2) return k.rows <= 16 ? q4_run_short<T, GU, 1, SG, 2>(d, a, s) : q4_run_short<T, GU, 2, SG, 2>(d, a, s);
+  if (k.split) return k.rows <= 2 ? q4_run_split<T, GU, 2, SG>(d, a, s) : q4_run_split<T, GU, 4, SG>(d, a, s);
+  if constexpr (GU) {
+    return k.rows <= 8 ? q4_run_rows<T, GU, 1, 1, SG, 2>(d, a, s) : q4_run_rows<T, GU, 2, 1, SG, 2>(d, a, s);
+  } else {
+    const bool wide = k.rows > 40 && chunks_of(d, 32) * (d.d_model / 128) >= device_cus();
+    return wide ? q4_run_rows<T, GU, 2, 2, SG, 2>(d, a, s) : q4_run_rows<T, GU, 1, 1, SG, 4>(d, a, s);
+  }
 }
 
 template <typename T, int SG>
@@ -702,7 +847,7 @@ hipError_t launch_ffn_q4(const moe_desc& d, int group, const void* x, const void
   a.x = x;
   a.xp = xp;
   a.h = ws;
-  a.h_low = d.dtype == MOE_BF16 && q4_rule(d, group, false).split ? (int64_t)h_bytes(d) : 0;
+  a.h_low = d.dtype == MOE_BF16 && q4_rule(d, group, false).two ? (int64_t)h_bytes(d) : 0;
   a.y = yp;
   if (d.dtype == MOE_BF16) return q4_ffn<bf16>(d, group, a, gate, up, down, s);
   return q4_ffn<float>(d, group, a, gate, up, down, s);

@@ -128,6 +128,26 @@ def test_experts(case, group, dtype):
         assert bool((y == 77).all())
 
 
+KERNELS = [  # T, d, f, rows per hosted expert, k, E, shared: K past 256 in both projections
+    (1, 384, 384, [1, 0, 1], 2, 3, 1),                                    # K split, 32 columns; fewer steps than wavefronts
+    (1, 1152, 1408, [0, 1], 1, 2, 2),                                     # ... more steps than wavefronts
+    (9, 640, 1152, [9, 4, 5], 2, 3, 0),                                   # K split, 64 columns
+    (60, 384, 512, [20, 17, 33, 16, 1, 33], 2, 6, 0),                     # 32-row chunks; 16-row chunks, four steps in flight
+    (100, 640, 384, [50, 49, 97, 4], 2, 4, 1),                            # ... an odd number of steps
+    (800, 640, 384, [200, 129, 31, 33, 800, 0, 7, 400], 2, 8, 0),         # 32 rows x 128 columns
+    (42, 384, 1024, [3, 4, 5, 2, 0, 1, 17, 3] * 6, 5, 48, 0),             # 16-row chunks of gate/up
+]
+
+
+@pytest.mark.parametrize("case", KERNELS, ids=lambda c: "T{}_d{}_f{}_G{}_S{}".format(c[0], c[1], c[2], len(c[3]), c[6]))
+@pytest.mark.parametrize("group,dtype", [(32, "bf16"), (64, "bf16"), (128, "bf16"), (32, "f32"), (128, "f32")])
+def test_each_kernel(case, group, dtype):
+    T, d, f, counts, k, E, S = case
+    log(f"[q4] kernels T={T} d={d} f={f} group={group} {dtype}")
+    y, ref, valid, _ = run(T, d, f, counts, k, E, S, group, dtype)
+    check(y, ref, valid, dtype)
+
+
 @pytest.mark.parametrize("G", [65, 256])
 def test_many_experts(G):
     counts = [(3 * g + g // 64) % 4 for g in range(G)]
