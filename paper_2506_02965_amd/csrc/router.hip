@@ -309,12 +309,23 @@ __device__ __forceinline__ void gated_select(const float (&v)[NT][QE], int E, in
 // are 14 us of a CU's fp64 rate, whatever the token count. Long batches take TT token tiles per wavefront: an expert
 // chunk is then converted once for TT products, a token chunk once for NET.
 // PF column steps of loads are in flight per wavefront.
-template <typename T, bool GATED, int TB, int TT, int NET, int WE, int WK, int PF>
+// MODE says what becomes of the scores. SCORES: they are all there is to do, and a workgroup takes the 16 NET WE experts
+// from 16 NET WE blockIdx.y on.
+enum { ROUTE = 0, GATED = 1, SCORES = 2 };
+template <typename T, int MODE, int TB, int TT, int NET, int WE, int WK, int PF>
 __global__ __launch_bounds__(64 * WE * WK) void route_fwd_kernel(const T* __restrict__ x, const T* __restrict__ wr,
                                                               const float* __restrict__ bias, int bias_div, int Tn,
                                                               int d, int E, int k, int renorm,
                                                               float* __restrict__ logits, int32_t* __restrict__ idx,
                                                               float* __restrict__ gw, GateArgs ga) {
+  const int ld = E;  // row length of logits and bias
+  if constexpr (MODE == SCORES) {
+    const int eb = blockIdx.y * 16 * NET * WE;
+    wr += (size_t)eb * d;
+    logits += eb;
+    if (bias) bias += eb;
+    E = min(E - eb, 16 * NET * WE);
+  }
   constexpr int EP = EPC<T>::value;        // elements per 16-byte chunk
   constexpr int EW = 16 * NET * WE + 1;    // padded expert stride of the partial-sum table
   constexpr int NTOK = TB * TT;
@@ -431,12 +442,18 @@ __global__ __launch_bounds__(64 * WE * WK) void route_fwd_kernel(const T* __rest
     double sum = part[row * EW + e];
 #pragma unroll
     for (int w = 1; w < WK; ++w) sum += part[(w * NTOK + row) * EW + e];
-    if (bias) sum += (double)bias[(size_t)(tt / bias_div) * E + e];
+    if (bias) sum += (double)bias[(size_t)(tt / bias_div) * ld + e];
     const float L = (float)sum;
-    logits[(size_t)tt * E + e] = L;
+    logits[(size_t)tt * ld + e] = L;
     return L;
   };
-  if constexpr (GATED) {
+  if constexpr (MODE == SCORES) {
+    for (int row = wave; row < NTOK && t0 + row < Tn; row += W)
+#pragma unroll
+      for (int qq = 0; qq < QE; ++qq) (void)score_of(row, qq);
+    return;
+  }
+  if constexpr (MODE == GATED) {
     // as many tokens at once as the wavefront has, up to 4 (us at 1 / 2 / 4: T = 16,384, d = 128, E = 64, groups and bias
     // 35.5 / 32.9 / 31.8; T = 8192, d = 2048, E = 256 166 / 163.3 / 162.5)
     constexpr int NT = NTOK >= 4 * W ? 4 : NTOK >= 2 * W ? 2 : 1;
@@ -508,24 +525,25 @@ __global__ __launch_bounds__(64 * WE * WK) void route_fwd_kernel(const T* __rest
   }
 }
 
-template <typename T, bool GATED, int TB, int TT, int NET, int WE, int WK, int PF>
+template <typename T, int MODE, int TB, int TT, int NET, int WE, int WK, int PF>
 static hipError_t route_fwd_run(const moe_desc& d, const void* x, const void* wr, const float* bias, int div,
                                 float* logits, int32_t* idx, float* w, const GateArgs& ga, hipStream_t s) {
   constexpr int NTOK = TB * TT;
   constexpr size_t LDS = (size_t)WK * NTOK * (16 * NET * WE + 1) * sizeof(double);
   static_assert(LDS <= 160 * 1024, "partial-sum table");
-  auto kern = route_fwd_kernel<T, GATED, TB, TT, NET, WE, WK, PF>;
+  auto kern = route_fwd_kernel<T, MODE, TB, TT, NET, WE, WK, PF>;
   if (LDS > 65536) {
     static std::atomic<uint64_t> lds_set{0};
     if (hipError_t e = lds_limit_once((const void*)kern, (int)LDS, lds_set); e != hipSuccess) return e;
   }
-  KernelTimer kt(GATED ? "route_gated" : "route_fwd", s);
-  hipLaunchKernelGGL(kern, dim3((d.T + NTOK - 1) / NTOK), dim3(64 * WE * WK), LDS, s, (const T*)x, (const T*)wr, bias,
+  KernelTimer kt(MODE == SCORES ? "gate_scores" : MODE == GATED ? "route_gated" : "route_fwd", s);
+  const dim3 grid((d.T + NTOK - 1) / NTOK, MODE == SCORES ? (d.n_experts + 16 * NET * WE - 1) / (16 * NET * WE) : 1);
+  hipLaunchKernelGGL(kern, grid, dim3(64 * WE * WK), LDS, s, (const T*)x, (const T*)wr, bias,
                      div, d.T, d.d_model, d.n_experts, d.top_k, d.renormalize, logits, idx, w, ga);
   return hipGetLastError();
 }
 
-template <typename T, bool GATED>
+template <typename T, int MODE>
 static hipError_t route_fwd_t(const moe_desc& d, const void* x, const void* wr, const float* bias, int bg,
                               float* logits, int32_t* idx, float* w, const GateArgs& ga, hipStream_t s) {
   const int E = d.n_experts;
@@ -542,7 +560,7 @@ static hipError_t route_fwd_t(const moe_desc& d, const void* x, const void* wr, 
   // Wavefronts: as many as fit the LDS table and, at 16 of them, 128 VGPRs without spills; 4 to a workgroup of 16 tokens
   // in long batches, where several workgroups share a CU.
 #define RT(TB, TT, NET, WE, WK, PF) \
-  return route_fwd_run<T, GATED, TB, TT, NET, WE, WK, PF>(d, x, wr, bias, div, logits, idx, w, ga, s)
+  return route_fwd_run<T, MODE, TB, TT, NET, WE, WK, PF>(d, x, wr, bias, div, logits, idx, w, ga, s)
   const int cus = device_cus();
   const int r16 = (d.T + 16 * cus - 1) / (16 * cus), r32 = (r16 + 1) / 2;  // rounds of 16 and of 32 tokens per CU
   const bool by32 = r32 == 1 || ((E > 32 || d.dtype == MOE_F32) && 20 * r32 <= 11 * r16);
@@ -581,8 +599,66 @@ static hipError_t route_fwd_t(const moe_desc& d, const void* x, const void* wr, 
 hipError_t launch_route_fwd(const moe_desc& d, const void* x, const void* wr, const float* bias, int bg,
                             float* logits, int32_t* idx, float* w, hipStream_t s) {
   const GateArgs none{};
-  if (d.dtype == MOE_BF16) return route_fwd_t<bf16, false>(d, x, wr, bias, bg, logits, idx, w, none, s);
-  return route_fwd_t<float, false>(d, x, wr, bias, bg, logits, idx, w, none, s);
+  if (d.dtype == MOE_BF16) return route_fwd_t<bf16, ROUTE>(d, x, wr, bias, bg, logits, idx, w, none, s);
+  return route_fwd_t<float, ROUTE>(d, x, wr, bias, bg, logits, idx, w, none, s);
+}
+
+// Selection from scores that are there: one wavefront per token.
+template <int QE>
+__global__ __launch_bounds__(256) void gate_select_kernel(const float* __restrict__ logits, int Tn, int E, int k, int renorm,
+                                                          int32_t* __restrict__ idx, float* __restrict__ gw, GateArgs ga) {
+  __shared__ double values[4][64 * QE];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = blockIdx.x * 4 + w;
+  if (t >= Tn) return;
+  float v[1][QE];
+#pragma unroll
+  for (int qq = 0; qq < QE; ++qq) v[0][qq] = lane + 64 * qq < E ? logits[(size_t)t * E + lane + 64 * qq] : -INFINITY;
+  double* row[1] = {values[w]};
+  gated_select<QE, 1>(v, E, k, renorm, ga, row, 1, 0, idx + (size_t)t * k, gw + (size_t)t * k);
+}
+
+template <typename T>
+static hipError_t route_gated_t(const moe_desc& d, const void* x, const void* wr, const float* bias, int bg,
+                                float* logits, int32_t* idx, float* w, const GateArgs& ga, hipStream_t s) {
+  const int E = d.n_experts, div = d.T / bg, cus = device_cus();
+  // The fused kernel holds all the experts' scores of its tokens in one workgroup, on one CU. Where its workgroups would
+  // leave CUs idle, the scores are spread over them instead, 16, 32 or 64 experts to a workgroup, and selected from by a
+  // second launch: the smallest tile of which there are no more than CUs. That launch costs 4 us, so not for scores that
+  // are soon done (up to 32 experts, or E * d below 48 k), nor past one round of the chip, where the fused kernel converts
+  // and reads less. us, fused / spread (bf16, top-4, groups and bias), T, d, E:
+  //   1, 2048, 64 11.6 / 8.7;  1, 4096, 200 56.7 / 12.7;  1, 512, 200 13.1 / 8.4;  17, 256, 256 10.9 / 9.0;
+  //   64, 2048, 64 12.1 / 8.9;  200, 4096, 200 58.0 / 20.4;  465, 4096, 200 73.3 / 29.3;  1000, 2048, 64 15.1 / 12.8;
+  //   2048, 2048, 64 26.2 / 17.5;  2048, 4096, 200 159 / 79.4;  2048, 256, 256 21.7 / 15.0; fp32 1, 4096, 200 104 / 16.6;
+  //   fused instead: 1, 1408, 16 5.9 / 8.3;  1000, 2560, 32 11.9 / 13.9;  4096, 2048, 64 26.8 / 27.2;
+  //   4096, 2048, 256 86.8 / 85.0;  8192, 2048, 256 156 / 165.
+  bool spread = E > 32 && (int64_t)E * d.d_model >= 48 * 1024;
+  hipError_t e = hipSuccess;
+  const auto fits = [&](int tokens, int experts) {
+    return (int64_t)((d.T + tokens - 1) / tokens) * ((E + experts - 1) / experts) <= cus;
+  };
+#define GS(TB, TT, NET, WK, PF) \
+  e = route_fwd_run<T, SCORES, TB, TT, NET, 1, WK, PF>(d, x, wr, bias, div, logits, nullptr, nullptr, ga, s)
+  if (!spread) {}
+  else if (fits(1, 16)) GS(1, 1, 1, 16, 4);
+  else if (fits(4, 16)) GS(4, 1, 1, 16, 4);
+  else if (fits(16, 16)) GS(16, 1, 1, 16, 4);
+  else if (fits(16, 32)) GS(16, 1, 2, 8, 3);
+  else if (E > 64 && fits(32, 32)) GS(16, 2, 2, 8, 2);
+  else if (E > 64 && fits(32, 64)) GS(16, 2, 4, 8, 2);
+  else spread = false;
+#undef GS
+  if (!spread) return route_fwd_t<T, GATED>(d, x, wr, bias, bg, logits, idx, w, ga, s);
+  if (e != hipSuccess) return e;
+  KernelTimer kt("gate_select", s);
+  const dim3 grid((d.T + 3) / 4);
+#define GSEL(QE) \
+  hipLaunchKernelGGL(gate_select_kernel<QE>, grid, dim3(256), 0, s, logits, d.T, E, d.top_k, d.renormalize, idx, w, ga)
+  if (E <= 64) GSEL(1);
+  else if (E <= 128) GSEL(2);
+  else GSEL(4);
+#undef GSEL
+  return hipGetLastError();
 }
 
 hipError_t launch_route_gated(const moe_desc& d, const moe_gate& g, const void* x, const void* wr, const float* bias,
@@ -592,8 +668,8 @@ hipError_t launch_route_gated(const moe_desc& d, const moe_gate& g, const void* 
   while ((2 << lane_shift) * g.n_groups <= 64) ++lane_shift;
   const GateArgs ga{select_bias, g.scale, g.score == MOE_SCORE_SIGMOID, g.n_groups, g.topk_groups, g.group_top, size,
                     (65536 + size - 1) / size, lane_shift};
-  if (d.dtype == MOE_BF16) return route_fwd_t<bf16, true>(d, x, wr, bias, bg, logits, idx, w, ga, s);
-  return route_fwd_t<float, true>(d, x, wr, bias, bg, logits, idx, w, ga, s);
+  if (d.dtype == MOE_BF16) return route_gated_t<bf16>(d, x, wr, bias, bg, logits, idx, w, ga, s);
+  return route_gated_t<float>(d, x, wr, bias, bg, logits, idx, w, ga, s);
 }
 
 // ------------------------------------------------------------------------------ backward

@@ -92,6 +92,10 @@ CASES = [  # T, d, E, k, groups, keep, top
     (1025, 128, 65, 4, 5, 2, 2), (300, 256, 256, 8, 8, 4, 2), (2000, 128, 200, 8, 25, 3, 2), (4097, 128, 256, 8, 64, 2, 1),
     (4100, 128, 32, 2, 16, 16, 2), (33, 128, 96, 8, 3, 3, 1), (8195, 128, 40, 6, 20, 3, 2), (700, 128, 33, 8, 1, 1, 2),
     (40, 128, 8, 8, 1, 1, 1), (64, 128, 256, 4, 2, 1, 2),
+    # the scores spread over the CUs, 16, 32 and 64 experts to a workgroup of 1, 4, 16 and 32 tokens
+    (1, 1024, 64, 6, 8, 4, 2), (3, 512, 200, 8, 1, 1, 1), (62, 768, 66, 4, 2, 2, 1), (150, 512, 100, 3, 5, 2, 2),
+    (300, 1024, 50, 2, 1, 1, 1), (501, 384, 129, 8, 3, 2, 2), (999, 256, 199, 4, 1, 1, 1), (2047, 256, 256, 8, 16, 4, 2),
+    (1050, 768, 64, 6, 1, 1, 1),
 ]
 
 
