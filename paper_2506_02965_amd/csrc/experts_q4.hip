@@ -294,16 +294,15 @@ __device__ __forceinline__ void store_h_low(const Q4Args& p, int64_t at, float h
   if (in) ((bf16*)((char*)p.h + p.h_low))[at] = fabsf(rest) < INFINITY ? f2bf(rest) : (bf16)0;
 }
 
-// Up to 16 rows of a group against 16 NB columns of the output (GU: of gate and of up): the Q4_KS wavefronts take a part of K
+// Up to 16 rows of a group against 16 NB columns of the output (GU: of gate and of up): the KS wavefronts take a part of K
 // each, 128 k at a time, read rows and weights straight into MFMA operands and share nothing until their sums meet in LDS
 // and are added in wavefront order. SG = 128 / group. Bound by the round trips of the loads: a wavefront's steps are few, so
 // the next one's loads, issued behind a step's products, are all that is in flight.
-constexpr int Q4_KS = 8;
-template <typename T, bool GU, int NB, int SG>
-__global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
+template <typename T, bool GU, int NB, int SG, int KS>
+__global__ __launch_bounds__(64 * KS) void q4_split_kernel(Q4Args p) {
   typedef Acts<T, GU ? 1 : 2> X;
   constexpr int NM = GU ? 2 : 1, NP = X::NP, XC = X::XC, XB = sizeof(T);
-  __shared__ __align__(16) floatx4 red[Q4_KS][NM * NB][64];
+  __shared__ __align__(16) floatx4 red[KS][NM * NB][64];
   Q4Tile t;
   if (!q4_tile(p, blockIdx.x, 16, t)) return;
   const int lane = threadIdx.x & 63, q = lane >> 4, li = lane & 15;
@@ -316,7 +315,7 @@ __global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
   // rows past the last read as zeros; of bf16 H also the second array
   const __amdgpu_buffer_rsrc_t xr[2] = {buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB),
                                         buf_rsrc(xb + (GU ? 0 : p.h_low) + (int64_t)m0 * KB, (size_t)m_rows * KB)};
-  const int u0 = (int)((int64_t)units * w / Q4_KS), u1 = (int)((int64_t)units * (w + 1) / Q4_KS);
+  const int u0 = (int)((int64_t)units * w / KS), u1 = (int)((int64_t)units * (w + 1) / KS);
   const int nb0 = t.nb * NB;  // first 16-column block
   __amdgpu_buffer_rsrc_t cr[NM], sr[NM];
 #pragma unroll
@@ -392,7 +391,7 @@ __global__ __launch_bounds__(64 * Q4_KS) void q4_split_kernel(Q4Args p) {
   for (int a = 0; a < NM; ++a) {
     v[a] = red[0][a * NB + w][lane];
 #pragma unroll
-    for (int k = 1; k < Q4_KS; ++k) v[a] += red[k][a * NB + w][lane];
+    for (int k = 1; k < KS; ++k) v[a] += red[k][a * NB + w][lane];
   }
   const int col = (nb0 + w) * 16 + li;
 #pragma unroll
@@ -720,12 +719,12 @@ int64_t chunks_of(const moe_desc& d, int chunk) {
          (int64_t)d.n_shared * ((d.T + chunk - 1) / chunk);
 }
 
-template <typename T, bool GU, int NB, int SG>
+template <typename T, bool GU, int NB, int SG, int KS>
 hipError_t q4_run_split(const moe_desc& d, Q4Args a, hipStream_t s) {
   a.n_blocks = (GU ? d.d_ff : d.d_model) / (16 * NB);
   const unsigned grid = (unsigned)((chunks_of(d, 16) * a.n_blocks + 7) / 8 * 8);
   KernelTimer kt(GU ? "q4_gate_up" : "q4_down", s);
-  hipLaunchKernelGGL((q4_split_kernel<T, GU, NB, SG>), dim3(grid), dim3(64 * Q4_KS), 0, s, a);
+  hipLaunchKernelGGL((q4_split_kernel<T, GU, NB, SG, KS>), dim3(grid), dim3(64 * KS), 0, s, a);
   return hipGetLastError();
 }
 
@@ -797,7 +796,7 @@ hipError_t q4_pick(const moe_desc& d, const Q4Args& a, hipStream_t s) {
   const Q4Pick k = q4_rule(d, 128 / SG, GU);
   if (k.units == 1) return k.rows <= 16 ? q4_run_short<T, GU, 1, SG, 1>(d, a, s) : q4_run_short<T, GU, 2, SG, 1>(d, a, s);
   if (k.units == 2) return k.rows <= 16 ? q4_run_short<T, GU, 1, SG, 2>(d, a, s) : q4_run_short<T, GU, 2, SG, 2>(d, a, s);
-  if (k.split) return k.rows <= 2 ? q4_run_split<T, GU, 2, SG>(d, a, s) : q4_run_split<T, GU, 4, SG>(d, a, s);
+  if (k.split) return k.rows <= 2 ? q4_run_split<T, GU, 2, SG, 8>(d, a, s) : q4_run_split<T, GU, 4, SG, 8>(d, a, s);
   if constexpr (GU) {
     return k.rows <= 8 ? q4_run_rows<T, GU, 1, 1, SG, 2>(d, a, s) : q4_run_rows<T, GU, 2, 1, SG, 2>(d, a, s);
   } else {

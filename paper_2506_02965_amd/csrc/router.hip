@@ -623,30 +623,49 @@ static hipError_t route_gated_t(const moe_desc& d, const void* x, const void* wr
                                 float* logits, int32_t* idx, float* w, const GateArgs& ga, hipStream_t s) {
   const int E = d.n_experts, div = d.T / bg, cus = device_cus();
   // The fused kernel holds all the experts' scores of its tokens in one workgroup, on one CU. Where its workgroups would
-  // leave CUs idle, the scores are spread over them instead, 16, 32 or 64 experts to a workgroup, and selected from by a
-  // second launch: the smallest tile of which there are no more than CUs. That launch costs 4 us, so not for scores that
-  // are soon done (up to 32 experts, or E * d below 48 k), nor past one round of the chip, where the fused kernel converts
-  // and reads less. us, fused / spread (bf16, top-4, groups and bias), T, d, E:
+  // leave CUs idle, or fill a last round badly, the scores are spread over them instead, in tiles of fewer experts, and
+  // selected from by a second launch. The estimates: us of a tile's products at d = 2048 times the tiles that the busiest CU
+  // gets, and 4 us around one launch, 6.5 around two; the fused kernel's tile is as wide as its padded experts (multiples
+  // of 16) and has the tokens that route_fwd_t gives it. us, fused / spread (bf16, top-4, groups and bias), T, d, E:
   //   1, 2048, 64 11.6 / 8.7;  1, 4096, 200 56.7 / 12.7;  1, 512, 200 13.1 / 8.4;  17, 256, 256 10.9 / 9.0;
   //   64, 2048, 64 12.1 / 8.9;  200, 4096, 200 58.0 / 20.4;  465, 4096, 200 73.3 / 29.3;  1000, 2048, 64 15.1 / 12.8;
   //   2048, 2048, 64 26.2 / 17.5;  2048, 4096, 200 159 / 79.4;  2048, 256, 256 21.7 / 15.0; fp32 1, 4096, 200 104 / 16.6;
   //   fused instead: 1, 1408, 16 5.9 / 8.3;  1000, 2560, 32 11.9 / 13.9;  4096, 2048, 64 26.8 / 27.2;
-  //   4096, 2048, 256 86.8 / 85.0;  8192, 2048, 256 156 / 165.
-  bool spread = E > 32 && (int64_t)E * d.d_model >= 48 * 1024;
-  hipError_t e = hipSuccess;
-  const auto fits = [&](int tokens, int experts) {
-    return (int64_t)((d.T + tokens - 1) / tokens) * ((E + experts - 1) / experts) <= cus;
+  //   8192, 2048, 256 156 / 165.
+  const double per = d.d_model / 2048.0;
+  const auto rounds = [&](int tokens, int experts) {
+    return (double)(((int64_t)((d.T + tokens - 1) / tokens) * ((E + experts - 1) / experts) + cus - 1) / cus);
   };
+  const int wide = E <= 16 ? 16 : E <= 32 ? 32 : E <= 64 ? 64 : E <= 128 ? 128 : 256;
+  const double fused = 4 + per * (wide / 16) *
+                               (d.T <= cus       ? 1.65
+                                : d.T <= 4 * cus ? 2.5
+                                                 : std::min(5.5 * rounds(16, wide), 9.7 * rounds(32, wide)));
+  static constexpr struct {
+    int tokens, experts;
+    double us;
+  } tiles[] = {{1, 16, 2.5}, {4, 16, 4}, {16, 16, 7}, {16, 32, 12}, {32, 32, 21}, {32, 64, 40}};
+  int pick = -1;
+  double best = fused;
+  for (int i = 0; i < 6; ++i) {
+    const double us = 6.5 + per * tiles[i].us * rounds(tiles[i].tokens, tiles[i].experts);
+    if (us < best) {
+      best = us;
+      pick = i;
+    }
+  }
+  const bool spread = pick >= 0;
+  hipError_t e = hipSuccess;
 #define GS(TB, TT, NET, WK, PF) \
   e = route_fwd_run<T, SCORES, TB, TT, NET, 1, WK, PF>(d, x, wr, bias, div, logits, nullptr, nullptr, ga, s)
-  if (!spread) {}
-  else if (fits(1, 16)) GS(1, 1, 1, 16, 4);
-  else if (fits(4, 16)) GS(4, 1, 1, 16, 4);
-  else if (fits(16, 16)) GS(16, 1, 1, 16, 4);
-  else if (fits(16, 32)) GS(16, 1, 2, 8, 3);
-  else if (E > 64 && fits(32, 32)) GS(16, 2, 2, 8, 2);
-  else if (E > 64 && fits(32, 64)) GS(16, 2, 4, 8, 2);
-  else spread = false;
+  switch (pick) {
+    case 0: GS(1, 1, 1, 16, 4); break;
+    case 1: GS(4, 1, 1, 16, 4); break;
+    case 2: GS(16, 1, 1, 16, 4); break;
+    case 3: GS(16, 1, 2, 8, 3); break;
+    case 4: GS(16, 2, 2, 8, 2); break;
+    case 5: GS(16, 2, 4, 8, 2); break;
+  }
 #undef GS
   if (!spread) return route_fwd_t<T, GATED>(d, x, wr, bias, bg, logits, idx, w, ga, s);
   if (e != hipSuccess) return e;
