@@ -298,7 +298,8 @@ __device__ __forceinline__ void store_h_low(const Q4Args& p, int64_t at, float h
 // each, 128 k at a time, read rows and weights straight into MFMA operands and share nothing until their sums meet in LDS
 // and are added in wavefront order. SG = 128 / group. Bound by the round trips of the loads: a wavefront's steps are few, so
 // the next one's loads, issued behind a step's products, are all that is in flight.
-template <typename T, bool GU, int NB, int SG, int KS>
+constexpr int KS = 8;
+template <typename T, bool GU, int NB, int SG>
 __global__ __launch_bounds__(64 * KS) void q4_split_kernel(Q4Args p) {
   typedef Acts<T, GU ? 1 : 2> X;
   constexpr int NM = GU ? 2 : 1, NP = X::NP, XC = X::XC, XB = sizeof(T);
@@ -719,12 +720,12 @@ int64_t chunks_of(const moe_desc& d, int chunk) {
          (int64_t)d.n_shared * ((d.T + chunk - 1) / chunk);
 }
 
-template <typename T, bool GU, int NB, int SG, int KS>
+template <typename T, bool GU, int NB, int SG>
 hipError_t q4_run_split(const moe_desc& d, Q4Args a, hipStream_t s) {
   a.n_blocks = (GU ? d.d_ff : d.d_model) / (16 * NB);
   const unsigned grid = (unsigned)((chunks_of(d, 16) * a.n_blocks + 7) / 8 * 8);
   KernelTimer kt(GU ? "q4_gate_up" : "q4_down", s);
-  hipLaunchKernelGGL((q4_split_kernel<T, GU, NB, SG, KS>), dim3(grid), dim3(64 * KS), 0, s, a);
+  hipLaunchKernelGGL((q4_split_kernel<T, GU, NB, SG>), dim3(grid), dim3(64 * KS), 0, s, a);
   return hipGetLastError();
 }
 
@@ -755,8 +756,9 @@ hipError_t q4_run_short(const moe_desc& d, Q4Args a, hipStream_t s) {
 // share of the slots, experts equally likely):
 //   * K up to 256: the walking kernel, 16-row chunks up to 16 rows, 32-row chunks above;
 //   * up to 12 rows where the shared-rows kernel would be bound by the chain of its steps (0.45 and 0.36 us each, gate/up
-//     and down, and 2 us around them) rather than by reading the weights (5.5 TB/s): K split over 8 wavefronts, 32 columns
-//     up to 2 rows, 64 above;
+//     and down, and 2 us around them) rather than by reading the weights (5.5 TB/s), and K is long enough to split: K split
+//     over 8 wavefronts. 64 columns to a workgroup from 280 workgroups of 32 on (gate/up: and more than 2 rows), which
+//     share their reads of the rows; 32 below, and in the down projection 16 where there are less than 160 of 32;
 //   * else shared rows. Gate/up: 16-row chunks up to 8 rows, 32-row chunks above. Down, whose K is the long one: 16-row
 //     chunks with four steps in flight, or, above 40 rows and where that leaves a workgroup per CU, 32 rows x 128 columns.
 // us of split 32 / split 64 / rows 16 / rows 32 (down: rows 16 / rows 32 x 128), group 64, at T, d, f, E, k, shared:
@@ -770,12 +772,15 @@ hipError_t q4_run_short(const moe_desc& d, Q4Args a, hipStream_t s) {
 //             128, 4096, 14336, 8, 2   219.3 / 163  / 136  / 124           167   / 107  / 91.2 / 85.3
 //             777, 1024, 2816, 16, 2    95.2 / 67.4 / 38.2 / 30.7           56.9 / 37.0 / 23.2 / 20.2
 //             254, 128, 6912, 8, 4                                          31.3 / 21.8 / 18.5 / 28.6
+// Split 16 / 32 / 64, down: 1, 640, 11392, 6, 6 11.5 / 14.7 / 17.2; 14, 128, 14208, 8, 4 23.1 / 24.1 / 26.2; 4, 1024, 2816,
+// 16, 2 9.0 / 7.9 / 8.8; 2, 4096, 4096, 8, 2 13.4 / 12.3 / 10.9; 1, 4096, 14336, 8, 2 30.2 / 21.6 / 24.6. Sixteen wavefronts
+// were no faster (23.1, 12.0, 10.8, 18.9 and 32.0 us for these with 16 columns).
 // Walking / rows 32: gate/up 771, 128, 5888, 24, 8 50 / 73; 700, 256, 14336, 4, 2 43 / 50; down 451, 4096, 128, 256, 8, 2
 // 31 / 70 (rows 32 x 128: 51); 451, 4096, 256, 64, 8, 2 27 / 41 (34).
-// Measured and not kept: 64- and 128-row chunks (777 rows: 36.8 and 49 us of gate/up), four and sixteen wavefronts of a
-// split, deeper prefetch in the split, non-temporal loads of the codes (equal, and worse where calls follow each other).
+// Measured and not kept: 64- and 128-row chunks (777 rows: 36.8 and 49 us of gate/up), four wavefronts of a split, deeper
+// prefetch in the split, non-temporal loads of the codes (equal, and worse where calls follow each other).
 struct Q4Pick {
-  double rows;  // per active expert
+  double active, rows;  // experts with a row, and their rows
   int units;    // steps of 128 k
   bool split;   // K over the wavefronts
   bool two;     // the projection (down) reads H in two parts
@@ -787,8 +792,8 @@ Q4Pick q4_rule(const moe_desc& d, int group, bool gate_up) {
   const int units = (gate_up ? d.d_model : d.d_ff) / 128;
   const double bytes = active * (gate_up ? 2 : 1) * d.d_ff * d.d_model * (0.5 + 2.0 / group);
   const double chain = 2 + (gate_up ? 0.45 : 0.36) * units;
-  const bool split = units > 2 && rows <= 12 && chain > bytes / 5.5e6;
-  return {rows, units, split, split || (units <= 2 && rows <= 16)};
+  const bool split = units >= 6 && rows <= 12 && chain > bytes / 5.5e6;
+  return {active, rows, units, split, split || (units <= 2 && rows <= 16)};
 }
 
 template <typename T, bool GU, int SG>
@@ -796,7 +801,11 @@ hipError_t q4_pick(const moe_desc& d, const Q4Args& a, hipStream_t s) {
   const Q4Pick k = q4_rule(d, 128 / SG, GU);
   if (k.units == 1) return k.rows <= 16 ? q4_run_short<T, GU, 1, SG, 1>(d, a, s) : q4_run_short<T, GU, 2, SG, 1>(d, a, s);
   if (k.units == 2) return k.rows <= 16 ? q4_run_short<T, GU, 1, SG, 2>(d, a, s) : q4_run_short<T, GU, 2, SG, 2>(d, a, s);
-  if (k.split) return k.rows <= 2 ? q4_run_split<T, GU, 2, SG, 8>(d, a, s) : q4_run_split<T, GU, 4, SG, 8>(d, a, s);
+  if (k.split) {
+    const double wgs = k.active * ((GU ? d.d_ff : d.d_model) / 32);
+    if (!GU && wgs < 160) return q4_run_split<T, false, 1, SG>(d, a, s);
+    return wgs < 280 || (GU && k.rows <= 2) ? q4_run_split<T, GU, 2, SG>(d, a, s) : q4_run_split<T, GU, 4, SG>(d, a, s);
+  }
   if constexpr (GU) {
     return k.rows <= 8 ? q4_run_rows<T, GU, 1, 1, SG, 2>(d, a, s) : q4_run_rows<T, GU, 2, 1, SG, 2>(d, a, s);
   } else {

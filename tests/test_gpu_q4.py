@@ -129,9 +129,11 @@ def test_experts(case, group, dtype):
 
 
 KERNELS = [  # T, d, f, rows per hosted expert, k, E, shared: K past 256 in both projections
-    (1, 384, 384, [1, 0, 1], 2, 3, 1),                                    # K split, 32 columns; fewer steps than wavefronts
-    (1, 1152, 1408, [0, 1], 1, 2, 2),                                     # ... more steps than wavefronts
-    (9, 640, 1152, [9, 4, 5], 2, 3, 0),                                   # K split, 64 columns
+    (1, 384, 384, [1, 0, 1], 2, 3, 1),                                    # few steps, an odd number of them
+    (1, 1152, 1408, [0, 1], 1, 2, 2),                                     # K split, 32 columns
+    (9, 640, 1152, [9, 4, 5], 2, 3, 0),                                   # ... 16 columns of the down projection
+    (9, 4096, 1024, [9, 4, 5], 2, 3, 0),                                  # K split, 64 columns
+    (12, 1024, 5120, [12, 1], 2, 2, 1),                                   # ... of both projections
     (60, 384, 512, [20, 17, 33, 16, 1, 33], 2, 6, 0),                     # 32-row chunks; 16-row chunks, four steps in flight
     (100, 640, 384, [50, 49, 97, 4], 2, 4, 1),                            # ... an odd number of steps
     (800, 640, 384, [200, 129, 31, 33, 800, 0, 7, 400], 2, 8, 0),         # 32 rows x 128 columns
