@@ -761,70 +761,82 @@ __global__ __launch_bounds__(256) void route_dlogits_kernel(int Tn, int E, int k
   }
 }
 
-// ... of the gated routing (one wavefront per token). With w_j the returned weight of slot j, g_j its gradient, c the scale:
+// ... of the gated routing. With w_j the returned weight of slot j, g_j its gradient, c the scale:
 //   renormalised: dl_j = w_j (g_j - sum_i w_i g_i / c), for sigmoid scores times (1 - s_j);
 //   sigmoid:      dl_j = w_j (1 - s_j) g_j;       softmax: dl_e = p_e (c g_e - sum_i c p_i g_i) over all the experts.
 // 1 - s is formed as sigmoid(-l), which does not cancel. Slots that no expert fills give nothing.
+// A wavefront takes 8 tokens: first a lane per slot (lane 8 n + j has slot j of token n), so that the loads' latencies are
+// paid once for all of them, then the rows one by one, a lane per expert (T = 16,384, E = 64, top-6: 6.3 us, 8.2 with a
+// wavefront per token). DENSE, which reads whole rows of scores: one token (T = 1500, E = 8: 3.9 us, 10 with eight).
+template <bool DENSE>
 __global__ __launch_bounds__(256) void gate_dlogits_kernel(int Tn, int E, int k, int renorm, int sigmoid, float scale,
                                                            const float* __restrict__ logits,
                                                            const int32_t* __restrict__ idx,
                                                            const float* __restrict__ gw,
                                                            const float* __restrict__ dgate, float* __restrict__ dl) {
-  constexpr int NQ = 4;  // E <= 256
+  constexpr int NQ = 4, TW = DENSE ? 1 : 8;  // E <= 256; tokens of a wavefront
   const int lane = threadIdx.x & 63;
-  const int wave = (blockIdx.x * blockDim.x + threadIdx.x) >> 6;
-  const int nwaves = (gridDim.x * blockDim.x) >> 6;
-  for (int t = wave; t < Tn; t += nwaves) {
-    float wj = 0.f, gj = 0.f;
-    int ij = NO_EXPERT;
-    if (lane < k) {
-      ij = idx[(size_t)t * k + lane];
-      if ((unsigned)ij < (unsigned)E) {
-        wj = gw[(size_t)t * k + lane];
-        gj = dgate[(size_t)t * k + lane];
-      }
+  const int t0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * TW;
+  if (t0 >= Tn) return;
+  const int t = t0 + (lane >> 3), j = lane & 7;
+  const size_t slot = (size_t)t * k + j;
+  float wj = 0.f, gj = 0.f, lj = 0.f;
+  int ij = NO_EXPERT;
+  if (lane < 8 * TW && t < Tn && j < k) ij = idx[slot];
+  const bool filled = (unsigned)ij < (unsigned)E;
+  if (filled) {
+    wj = gw[slot];
+    gj = dgate[slot];
+    if (sigmoid) lj = logits[(size_t)t * E + ij];
+  }
+  float val = DENSE ? scale * gj : gj;  // what the slot adds to its expert
+  if constexpr (!DENSE) {
+    if (renorm) {
+      float s = wj * gj;
+      s += __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(s), 0xb1, 0xf, 0xf, false));   // lane pairs,
+      s += __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(s), 0x4e, 0xf, 0xf, false));   // quads,
+      s += __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(s), 0x141, 0xf, 0xf, false));  // eights
+      val -= s / scale;
     }
+    val *= wj;
+    if (sigmoid && filled) val /= 1.f + expf(lj);
+  }
+  for (int n = 0; n < TW && t0 + n < Tn; ++n) {
+    const size_t row = (size_t)(t0 + n) * E;
     float out[NQ] = {0.f, 0.f, 0.f, 0.f};
-    const bool dense = !renorm && !sigmoid;
-    float val = dense ? scale * gj : gj;  // what slot `lane` adds to its expert
-    if (!dense) {
-      if (renorm) val -= wave_sum(wj * gj) / scale;
-      val *= wj;
-      if (sigmoid && (unsigned)ij < (unsigned)E) val /= 1.f + expf(logits[(size_t)t * E + ij]);
-    }
     for (int jj = 0; jj < k; ++jj) {
-      const int i2 = __builtin_amdgcn_readlane(ij, jj);
-      const float g2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(val), jj));
+      const int i2 = __builtin_amdgcn_readlane(ij, 8 * n + jj);
+      const float g2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(val), 8 * n + jj));
 #pragma unroll
-      for (int n = 0; n < NQ; ++n)
-        if (lane + 64 * n == i2) out[n] = g2;
+      for (int q = 0; q < NQ; ++q)
+        if (lane + 64 * q == i2) out[q] = g2;
     }
-    if (dense) {
+    if constexpr (DENSE) {
       float p[NQ], m = -INFINITY, zp = 0.f, spg = 0.f;
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        p[n] = lane + 64 * n < E ? logits[(size_t)t * E + lane + 64 * n] : -INFINITY;
-        m = fmaxf(m, p[n]);
+      for (int q = 0; q < NQ; ++q) {
+        p[q] = lane + 64 * q < E ? logits[row + lane + 64 * q] : -INFINITY;
+        m = fmaxf(m, p[q]);
       }
-      m = wave_max(m);
+      m = wave_max_dpp(m);
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        p[n] = p[n] > -INFINITY ? expf(p[n] - m) : 0.f;
-        zp += p[n];
+      for (int q = 0; q < NQ; ++q) {
+        p[q] = p[q] > -INFINITY ? expf(p[q] - m) : 0.f;
+        zp += p[q];
       }
       const float z = wave_sum(zp);
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        p[n] = z == 0.f ? 0.f : p[n] / z;  // z = 0: every expert is masked
-        spg += p[n] * out[n];
+      for (int q = 0; q < NQ; ++q) {
+        p[q] = z == 0.f ? 0.f : p[q] / z;  // z = 0: every expert is masked
+        spg += p[q] * out[q];
       }
       spg = wave_sum(spg);
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) out[n] = p[n] * (out[n] - spg);
+      for (int q = 0; q < NQ; ++q) out[q] = p[q] * (out[q] - spg);
     }
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
-      if (lane + 64 * n < E) dl[(size_t)t * E + lane + 64 * n] = out[n];
+    for (int q = 0; q < NQ; ++q)
+      if (lane + 64 * q < E) dl[row + lane + 64 * q] = out[q];
   }
 }
 
@@ -1254,8 +1266,10 @@ hipError_t launch_route_gated_bwd(const moe_desc& d, const moe_gate& g, const vo
                                   void* ws, hipStream_t s) {
   {
     KernelTimer kt("gate_dlogits", s);
-    hipLaunchKernelGGL(gate_dlogits_kernel, dim3(token_blocks(d)), dim3(256), 0, s, d.T, d.n_experts, d.top_k,
-                       d.renormalize, (int)(g.score == MOE_SCORE_SIGMOID), g.scale, logits, idx, w, dgate, dl);
+    const bool sigmoid = g.score == MOE_SCORE_SIGMOID, dense = !d.renormalize && !sigmoid;
+    hipLaunchKernelGGL(dense ? gate_dlogits_kernel<true> : gate_dlogits_kernel<false>,
+                       dim3(dense ? (d.T + 3) / 4 : (d.T + 31) / 32), dim3(256), 0, s, d.T, d.n_experts, d.top_k,
+                       d.renormalize, (int)sigmoid, g.scale, logits, idx, w, dgate, dl);
   }
   return d.dtype == MOE_BF16 ? gate_dw(d, x, dl, dwr, ws, s) : route_dw_t<float>(d, x, dl, dwr, ws, s);
 }

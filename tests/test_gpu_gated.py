@@ -275,3 +275,31 @@ def test_layer_with_empty_slots():
     assert torch.equal(other.topk_idx, layer.topk_idx[keep])
     for a, b in ((layer.y[keep], other.y), (layer.dx[keep], other.dx)):
         assert float((a.float() - b.float()).abs().max() / b.float().abs().max()) <= 2e-2
+
+
+def test_training_step_graph_replays():
+    """Forward and backward with gated routing and 8-bit checkpoints captured into a graph: replays on other inputs, with eager
+    work in between, equal the eager step bit for bit."""
+    cfg = LayerConfig("gt", T=300, d=256, f=384, E=64, k=4, n_shared=1, seed=12)
+    inp = make_inputs(cfg, with_dy=True)
+    w = upload(inp)
+    w.select_bias = torch.linspace(-0.02, 0.02, 64, device="cuda")
+    gate = P.make_gate("sigmoid", 8, 4, 2, 2.0)
+    layer, eager = MoELayer(cfg, gate=gate, checkpoint=True), MoELayer(cfg, gate=gate, checkpoint=True)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        layer.forward(w)
+        layer.backward(w)
+    stream.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        layer.forward(w)
+        layer.backward(w)
+    for seed in range(4):
+        w.x.copy_(torch.randn(300, 256, generator=torch.Generator().manual_seed(seed)))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager.forward(w)
+        eager.backward(w)
+        torch.cuda.synchronize()
+        for name in ("y", "dx", "dw_gate", "dw_up", "dw_down", "dw_router", "dlogits", "topk_idx"):
+            assert torch.equal(getattr(layer, name), getattr(eager, name)), (seed, name)
