@@ -80,7 +80,7 @@ moe_status moe_ffn_restore(const moe_desc* desc, const int32_t* offsets, const v
  *   codes   [n, rows/16, cols/128, q = 4, i = 16, s = 4, b = 4] bytes: row 16 rb + i; the low half of byte b is column
  *           128 cb + 32 s + 8 q + 2 b, the high half the next
  *   scales  [n, rows/16, cols/group, 16] bf16
- * moe_q4_pack makes them from n matrices w [n, rows, cols] of dtype: scale = bf16(max|w| / 6) of the group, code = the
+ * moe_q4_pack makes them from n matrices w [n, rows, cols] of dtype: scale = bf16(max|w| * fp32(1/6)) of the group, code = the
  * nearest to w / scale, ties to the even code; a group with a NaN or an infinity gets a NaN scale. moe_q4_unpack writes
  * the weights that they stand for (in bf16 rounded once).
  * MOE_ERR_INVALID_ARGUMENT: n, rows or cols < 1, bad group or dtype, null or misaligned pointers; MOE_ERR_UNSUPPORTED: rows

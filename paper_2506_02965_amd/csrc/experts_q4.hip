@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(int64_t blocks, int kb, in
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
     // a group with a NaN or an infinity: its scale, and with it every product, is NaN
-    const bf16 sb = top[s] < 0x7f800000u ? f2bf(__uint_as_float(top[s]) / 6.f) : (bf16)0x7fc0;
+    const bf16 sb = top[s] < 0x7f800000u ? f2bf(__uint_as_float(top[s]) * (1.f / 6.f)) : (bf16)0x7fc0;
     out.w[s] = codes_of(v[s], bf2f(sb), T{});
     if (q == 0 && s % per == 0) scales[((nb * kb + k0) * (4 / per) + s / per) * 16 + i] = sb;
   }

@@ -36,7 +36,7 @@ def unpack_ref(codes, scales, group):
     return v * scales.cpu().double()[:, r // 16, k // group, r % 16]
 
 
-@pytest.mark.parametrize("shape", [(1, 16, 128), (3, 48, 256), (2, 128, 640), (5, 16, 384)])
+@pytest.mark.parametrize("shape", [(1, 16, 128), (3, 48, 256), (2, 128, 640), (5, 16, 384), (2, 2048, 1024)])
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_pack(shape, group, dtype):
@@ -54,7 +54,7 @@ def test_pack(shape, group, dtype):
     got = unpack_ref(codes, scales, group)
     g = w.double().view(n, N, K // group, group)
     bad = ~torch.isfinite(g).all(3)
-    s = (g.abs().amax(3).float() / 6).bfloat16()
+    s = (g.abs().amax(3).float() * torch.tensor(1 / 6, dtype=torch.float32)).bfloat16()   # the definition: times fp32(1/6)
     s[bad] = math.nan
     sg = scales.cpu().permute(0, 1, 3, 2).reshape(n, N, -1)
     assert torch.equal(torch.isnan(sg), bad) and torch.equal(sg[~bad], s[~bad])
