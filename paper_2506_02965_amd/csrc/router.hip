@@ -774,6 +774,7 @@ __global__ __launch_bounds__(256) void gate_dlogits_kernel(int Tn, int E, int k,
                                                            const int32_t* __restrict__ idx,
                                                            const float* __restrict__ gw,
                                                            const float* __restrict__ dgate, float* __restrict__ dl) {
+  const float per_scale = 1.f / scale;
   constexpr int NQ = 4, TW = DENSE ? 1 : 8;  // E <= 256; tokens of a wavefront
   const int lane = threadIdx.x & 63;
   const int t0 = (blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * TW;
@@ -792,11 +793,14 @@ __global__ __launch_bounds__(256) void gate_dlogits_kernel(int Tn, int E, int k,
   float val = DENSE ? scale * gj : gj;  // what the slot adds to its expert
   if constexpr (!DENSE) {
     if (renorm) {
+      // g - (sum w g) / c, each operation rounded by itself: where one expert is chosen the two cancel
+#pragma clang fp contract(off)
       float s = wj * gj;
       s += __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(s), 0xb1, 0xf, 0xf, false));   // lane pairs,
       s += __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(s), 0x4e, 0xf, 0xf, false));   // quads,
       s += __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(s), 0x141, 0xf, 0xf, false));  // eights
-      val -= s / scale;
+      s *= per_scale;
+      val -= s;
     }
     val *= wj;
     if (sigmoid && filled) val /= 1.f + expf(lj);
