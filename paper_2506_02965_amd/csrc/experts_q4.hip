@@ -218,7 +218,8 @@ __device__ __forceinline__ bool q4_tile(const Q4Args& p, int bid, int chunk, Q4T
 //   bf16 tensors: one part (B = 1); or two (B = 2), of H, which the gate/up kernel holds in fp32 and then stores as two bf16
 //     arrays, its rounding and the rounding of the rest. Rounded to bf16 alone, H adds as much error to an output as the
 //     output's own rounding (2.3e-3 in place of 1.7e-3 of the outputs' norm). The split over K, which waits for its loads
-//     and not for products, takes two parts; the shared rows would pay 13 us of 51 (777 tokens, below) and 11 of 130 (24).
+//     and not for products, takes two parts, and so do calls of few outputs; many shared rows would pay 13 us of 51 (777
+//     tokens, below) and 11 of 130 (24).
 //   fp32 tensors: three parts, exact (truncated: 8 + 8 + 8 bits), made of two chunks. Infinities and NaN stay in the first.
 template <typename T, int B>
 struct Acts {
@@ -493,10 +494,10 @@ __device__ __forceinline__ void put_acts(char* xs, int plane, int it, const X& x
 // Up to 16 MT rows of a group against 64 NF columns of the output: the four wavefronts split the columns (16 NF each; GU: of
 // gate and of up) and share the rows, which pass through LDS 128 k at a time in two stages, as the bf16 parts that the MFMAs
 // take. One barrier per step; the next steps' rows and codes are loaded while this one is multiplied.
-template <typename T, bool GU, int MT, int NF, int SG, int D>
+template <typename T, bool GU, int MT, int NF, int SG, int D, int B>
 __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
   static_assert(D % 2 == 0, "the steps of a round alternate between two LDS stages");
-  typedef Acts<T, 1> X;
+  typedef Acts<T, B> X;
   constexpr int NM = GU ? 2 : 1, NP = X::NP, XC = X::XC, XB = sizeof(T), ROWS = 16 * MT;
   constexpr int PLANE = ROWS * 256;
   __shared__ __align__(16) char xs[2][NP * PLANE];
@@ -509,7 +510,9 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
   const int64_t rs = routed ? (int64_t)t.row0 : p.shared0 + (int64_t)(t.g - p.Eloc) * p.T;
   const char* xb = GU ? (routed ? (const char*)p.xp + (int64_t)t.row0 * KB : (const char*)p.x) : (const char*)p.h + rs * KB;
   const int m0 = t.ch * ROWS, m_rows = min(t.rows - m0, ROWS);
-  const auto xr = buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB);  // rows past the last read as zeros
+  // rows past the last read as zeros; of bf16 H in two parts (B = 2) also the second array
+  const __amdgpu_buffer_rsrc_t xr[2] = {buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB),
+                                        buf_rsrc(xb + (B == 2 ? p.h_low : 0) + (int64_t)m0 * KB, (size_t)m_rows * KB)};
   const int nb0 = (t.nb * 4 + w) * NF;  // the wavefront's first 16-column block
   __amdgpu_buffer_rsrc_t cr[NM], sr[NM];
 #pragma unroll
@@ -534,7 +537,8 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
       const int it = tid + 256 * j;
 #pragma unroll
       for (int c = 0; c < XC; ++c)
-        x[j].c[c] = buf_ld16_at(xr, u < units ? (it >> 4) * KB + 8 * (it & 15) * XB + 16 * c : kBufPast, so);
+        x[j].c[c] = buf_ld16_at(xr[X::F32 ? 0 : c],
+                                u < units ? (it >> 4) * KB + 8 * (it & 15) * XB + (X::F32 ? 16 * c : 0) : kBufPast, so);
     }
   };
   auto put_x = [&](int stage, const X (&x)[MT]) {
@@ -729,12 +733,12 @@ hipError_t q4_run_split(const moe_desc& d, Q4Args a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, bool GU, int MT, int NF, int SG, int D>
+template <typename T, bool GU, int MT, int NF, int SG, int D, int B = 1>
 hipError_t q4_run_rows(const moe_desc& d, Q4Args a, hipStream_t s) {
   a.n_blocks = (GU ? d.d_ff : d.d_model) / (64 * NF);
   const unsigned grid = (unsigned)((chunks_of(d, 16 * MT) * a.n_blocks + 7) / 8 * 8);
   KernelTimer kt(GU ? "q4_gate_up" : "q4_down", s);
-  hipLaunchKernelGGL((q4_rows_kernel<T, GU, MT, NF, SG, D>), dim3(grid), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((q4_rows_kernel<T, GU, MT, NF, SG, D, B>), dim3(grid), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -793,7 +797,11 @@ Q4Pick q4_rule(const moe_desc& d, int group, bool gate_up) {
   const double bytes = active * (gate_up ? 2 : 1) * d.d_ff * d.d_model * (0.5 + 2.0 / group);
   const double chain = 2 + (gate_up ? 0.45 : 0.36) * units;
   const bool split = units >= 6 && rows <= 12 && chain > bytes / 5.5e6;
-  return {active, rows, units, split, split || (units <= 2 && rows <= 16)};
+  // A call of few outputs keeps H's second part where its products cost little. One part / two, us: T, d_model, d_ff, experts,
+  // top_k = 8, 512, 512, 8, 2: 9.4 / 9.5; 24, 256, 2816, 2, 2: 15.0 / 16.6; 24, 512, 4096, 4, 2: 18.2 / 20.2; 100, 128, 6912,
+  // 4, 2: 24.8 / 28.3. From 32768 outputs on they cost more than that (777 tokens: 13 us of 51).
+  const bool few = rows * active * d.d_model < 32768;
+  return {active, rows, units, split, split || (units <= 2 ? rows <= 16 : few)};
 }
 
 template <typename T, bool GU, int SG>
@@ -809,6 +817,7 @@ hipError_t q4_pick(const moe_desc& d, const Q4Args& a, hipStream_t s) {
   if constexpr (GU) {
     return k.rows <= 8 ? q4_run_rows<T, GU, 1, 1, SG, 2>(d, a, s) : q4_run_rows<T, GU, 2, 1, SG, 2>(d, a, s);
   } else {
+    if (k.two) return q4_run_rows<T, GU, 1, 1, SG, 4, sizeof(T) == 2 ? 2 : 1>(d, a, s);
     const bool wide = k.rows > 40 && chunks_of(d, 32) * (d.d_model / 128) >= device_cus();
     return wide ? q4_run_rows<T, GU, 2, 2, SG, 2>(d, a, s) : q4_run_rows<T, GU, 1, 1, SG, 4>(d, a, s);
   }
