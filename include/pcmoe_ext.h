@@ -62,8 +62,8 @@ moe_status moe_route_gated_bwd(const moe_desc* desc, const moe_gate* gate, const
  *   moe_ffn_checkpoint  reads saved after the forward and writes ckpt;
  *   moe_ffn_restore     writes saved for the moe_expert_ffn_bwd of the same call shape and offsets.
  * 32 consecutive columns of a row of G|U share a power of two 2^e, the smallest with max|v| <= 127 2^e (-126 <= e <= 121); a
- * value is restored as 2^e times rint(v / 2^e), ties to even, at most 127 either way, which no dtype rounds again. Infinities and NaN are restored as NaN and
- * do not count for e. H is restored as silu(G) U of the restored values.
+ * value is restored as 2^e times rint(v / 2^e), ties to even, at most 127 either way, which no dtype rounds again.
+ * Infinities and NaN are restored as NaN and do not count for e. H is restored as silu(G) U of the restored values.
  *   saved   G|U [R, 2f] dtype, at the next multiple of 256 bytes H [R, f] dtype, then the tile plan (opaque)
  *   ckpt    MOE_WS_FFN_CKPT bytes (opaque), 256-byte aligned as a workspace
  * Rows [offsets[local_count], T*k) are neither read nor written. One call's ckpt and saved must not overlap.
@@ -94,8 +94,9 @@ moe_status moe_q4_unpack(int32_t n, int32_t rows, int32_t cols, int32_t group, i
 /*
  * moe_expert_ffn_fwd from 4-bit weights, for inference over few rows per expert (decoding, short prompts; nothing is saved
  * for a backward): H = silu(h W_gate^T) * (h W_up^T), O = H W_down^T for every hosted and every shared expert. Sums over
- * codes are held in fp32 and scaled in fp32; H is rounded to dtype. The order of the sums over K follows the shape of the
- * call: equal calls give equal bits, a row in a batch of another size can differ in its last bits.
+ * codes are held in fp32 and scaled in fp32. H is rounded to dtype; calls of few rows per expert or few outputs carry the
+ * rest of a bf16 rounding along. That and the order of the sums over K follow the shape of the call: equal calls give equal
+ * bits, a row in a batch of another size can differ in its last bits.
  *   x, x_perm, offsets, y_perm   as for moe_expert_ffn_fwd
  *   gate_*, up_*   [local_count + n_shared] matrices [f, d], down_* [d, f], codes and scales as above, one group size
  *   ws      MOE_WS_FFN_Q4 bytes of scratch (H); calls that overlap on the GPU need their own
