@@ -784,8 +784,10 @@ hipError_t q4_run_short(const moe_desc& d, Q4Args a, hipStream_t s) {
 // Measured and not kept: 64- and 128-row chunks (777 rows: 36.8 and 49 us of gate/up), four wavefronts of a split, deeper
 // prefetch in the split, non-temporal loads of the codes (equal, and worse where calls follow each other), and the walking
 // kernel for K of up to 1024 with a chunk's rows held in LDS whole (rows 32 / walking, gate/up: 777, 1024, 2816, 16, 2 37.7 /
-// 39.6; 1500, 1024, 4096, 8, 2 83.9 / 81.3; 777, 512, 2048, 32, 4 29.7 / 25.8; down 777, 2048, 768, 64, 6 32.8 / 36.5): many
-// rows are bound by their instructions, not by waits. An MFMA takes 18 cycles of a SIMD, its 4 scalings 18, both 29.
+// 39.6; 1500, 1024, 4096, 8, 2 83.9 / 81.3; 777, 512, 2048, 32, 4 29.7 / 25.8; down 777, 2048, 768, 64, 6 32.8 / 36.5), four
+// steps in flight of 32-row chunks (gate/up of the first 49.5 against 38.7), a group's scalings among the next one's products
+// (equal). So neither waits nor their order bind many rows, but the instructions: an MFMA takes 18 cycles of a SIMD, its 4
+// scalings (groups of 32) 18, both together 27 to 29.
 struct Q4Pick {
   double active, rows;  // experts with a row, and their rows
   int units;    // steps of 128 k
