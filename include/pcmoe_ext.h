@@ -21,7 +21,7 @@ typedef struct {
   int32_t n_groups;     /* groups of n_experts / n_groups consecutive experts; divides n_experts, at most 64; 1: none */
   int32_t topk_groups;  /* groups open to a token, 1..n_groups */
   int32_t group_top;    /* a group's value: its largest choice value (1), or the sum of its two largest (2) */
-  float scale;          /* factor of the gate weights, > 0 and finite */
+  float scale;          /* factor of the gate weights, > 0, finite and not subnormal */
 } moe_gate;
 #define MOE_NO_EXPERT 0x7fffffff /* topk_idx of a slot that no expert fills */
 

@@ -95,8 +95,8 @@ moe_status check_gate(const moe_desc& d, const moe_gate* g) {
     return fail(MOE_ERR_INVALID_ARGUMENT, "group_top=2 with groups of one expert");
   if (d.top_k > g->topk_groups * size)
     return fail(MOE_ERR_INVALID_ARGUMENT, "top_k=%d > %d experts of the open groups", d.top_k, g->topk_groups * size);
-  if (!(g->scale > 0.f) || !std::isfinite(g->scale))
-    return fail(MOE_ERR_INVALID_ARGUMENT, "scale must be > 0 and finite");
+  if (!(g->scale > 0.f) || !std::isnormal(g->scale))  // the adjoint multiplies by its reciprocal
+    return fail(MOE_ERR_INVALID_ARGUMENT, "scale must be a normal number > 0");
   if (g->n_groups > 64) return fail(MOE_ERR_UNSUPPORTED, "n_groups=%d > 64", g->n_groups);
   return MOE_OK;
 }

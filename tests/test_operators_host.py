@@ -43,6 +43,11 @@ def test_gate_settings(kw, status):
     refused(status, P.moe_route_gated_bwd, desc(), g, OK, OK, OK, OK, OK, OK, OK, OK, 1 << 40)
 
 
+def test_subnormal_scale_has_no_reciprocal():
+    refused(INV, P.moe_route_gated, desc(), P.make_gate(scale=1e-39), OK, OK, None, 1, None, OK, OK, OK)
+    refused(INV, P.moe_route_gated_bwd, desc(), P.make_gate(scale=1e-39), OK, OK, OK, OK, OK, OK, OK, OK, 1 << 40)
+
+
 def test_more_groups_than_lanes():
     refused(UNS, P.moe_route_gated, desc(n_experts=256), P.make_gate(n_groups=128, topk_groups=128), OK, OK, None, 1, None,
             OK, OK, OK)
