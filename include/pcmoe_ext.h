@@ -94,9 +94,9 @@ moe_status moe_q4_unpack(int32_t n, int32_t rows, int32_t cols, int32_t group, i
 /*
  * moe_expert_ffn_fwd from 4-bit weights, for inference over few rows per expert (decoding, short prompts; nothing is saved
  * for a backward): H = silu(h W_gate^T) * (h W_up^T), O = H W_down^T for every hosted and every shared expert. Sums over
- * codes are held in fp32 and scaled in fp32. H is rounded to dtype; calls of few rows per expert or few outputs carry the
- * rest of a bf16 rounding along. That and the order of the sums over K follow the shape of the call: equal calls give equal
- * bits, a row in a batch of another size can differ in its last bits.
+ * codes are held in fp32 and scaled in fp32. H is held in fp32, or for bf16 in two bf16 numbers, its rounding and the
+ * rounding of the rest, so that a bf16 output is a sum rounded once. The order of the sums over K follows the shape of the
+ * call: equal calls give equal bits, a row in a batch of another size can differ in its last bits.
  *   x, x_perm, offsets, y_perm   as for moe_expert_ffn_fwd
  *   gate_*, up_*   [local_count + n_shared] matrices [f, d], down_* [d, f], codes and scales as above, one group size
  *   ws      MOE_WS_FFN_Q4 bytes of scratch (H); calls that overlap on the GPU need their own

@@ -143,7 +143,7 @@ struct Q4Args {
   const void* x;           // [T, d]: rows of the shared experts
   const void* xp;          // [T * k, d]
   void* h;                 // H [R, f] ...
-  int64_t h_low;           // ... of bf16 in two parts, the second this many bytes on; 0: in one
+  int64_t h_low;           // ... of bf16 in two parts, the second this many bytes on
   void* y;                 // [R, d]
   const char* codes[2];    // gate, up; or down
   const bf16* scales[2];
@@ -215,11 +215,9 @@ __device__ __forceinline__ bool q4_tile(const Q4Args& p, int bid, int chunk, Q4T
 }
 
 // Eight activations as bf16 parts that add up to them, NP of them, and as they are loaded, XC chunks:
-//   bf16 tensors: one part (B = 1); or two (B = 2), of H, which the gate/up kernel holds in fp32 and then stores as two bf16
+//   bf16 tensors: one part (B = 1) of x; two (B = 2) of H, which the gate/up kernel holds in fp32 and then stores as two bf16
 //     arrays, its rounding and the rounding of the rest. Rounded to bf16 alone, H adds as much error to an output as the
-//     output's own rounding (2.3e-3 in place of 1.7e-3 of the outputs' norm). The split over K, which waits for its loads
-//     and not for products, takes two parts, and so do calls of few outputs; many shared rows would pay 13 us of 51 (777
-//     tokens, below) and 11 of 130 (24).
+//     output's own rounding (2.3e-3 in place of 1.7e-3 of the outputs' norm).
 //   fp32 tensors: three parts, exact (truncated: 8 + 8 + 8 bits), made of two chunks. Infinities and NaN stay in the first.
 template <typename T, int B>
 struct Acts {
@@ -290,9 +288,9 @@ __device__ __forceinline__ float silu_of(float g, bf16) { return g * __builtin_a
 __device__ __forceinline__ float silu_of(float g, float) { return g / (1.f + expf(-g)); }
 
 // The second part of a bf16 H: the rest of its rounding; 0 where h rounds to an infinity (inf - inf makes products NaN).
-__device__ __forceinline__ void store_h_low(const Q4Args& p, int64_t at, float h, bool in) {
+__device__ __forceinline__ bf16 h_rest(float h) {
   const float rest = h - bf2f(f2bf(h));
-  if (in) ((bf16*)((char*)p.h + p.h_low))[at] = fabsf(rest) < INFINITY ? f2bf(rest) : (bf16)0;
+  return fabsf(rest) < INFINITY ? f2bf(rest) : (bf16)0;
 }
 
 // Up to 16 rows of a group against 16 NB columns of the output (GU: of gate and of up): the KS wavefronts take a part of K
@@ -403,8 +401,7 @@ __global__ __launch_bounds__(64 * KS) void q4_split_kernel(Q4Args p) {
     if constexpr (GU) {
       const float h = silu_of(v[0][r], T{}) * v[NM - 1][r];
       ((T*)p.h)[row * p.f + col] = from_f<T>(h);
-      if constexpr (std::is_same<T, bf16>::value)
-        if (p.h_low) store_h_low(p, row * p.f + col, h, true);
+      if constexpr (std::is_same<T, bf16>::value) ((bf16*)((char*)p.h + p.h_low))[row * p.f + col] = h_rest(h);
     } else {
       ((T*)p.y)[row * p.d + col] = from_f<T>(v[0][r]);
     }
@@ -494,10 +491,10 @@ __device__ __forceinline__ void put_acts(char* xs, int plane, int it, const X& x
 // Up to 16 MT rows of a group against 64 NF columns of the output: the four wavefronts split the columns (16 NF each; GU: of
 // gate and of up) and share the rows, which pass through LDS 128 k at a time in two stages, as the bf16 parts that the MFMAs
 // take. One barrier per step; the next steps' rows and codes are loaded while this one is multiplied.
-template <typename T, bool GU, int MT, int NF, int SG, int D, int B>
+template <typename T, bool GU, int MT, int NF, int SG, int D>
 __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
   static_assert(D % 2 == 0, "the steps of a round alternate between two LDS stages");
-  typedef Acts<T, B> X;
+  typedef Acts<T, GU ? 1 : 2> X;
   constexpr int NM = GU ? 2 : 1, NP = X::NP, XC = X::XC, XB = sizeof(T), ROWS = 16 * MT;
   constexpr int PLANE = ROWS * 256;
   __shared__ __align__(16) char xs[2][NP * PLANE];
@@ -510,9 +507,9 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
   const int64_t rs = routed ? (int64_t)t.row0 : p.shared0 + (int64_t)(t.g - p.Eloc) * p.T;
   const char* xb = GU ? (routed ? (const char*)p.xp + (int64_t)t.row0 * KB : (const char*)p.x) : (const char*)p.h + rs * KB;
   const int m0 = t.ch * ROWS, m_rows = min(t.rows - m0, ROWS);
-  // rows past the last read as zeros; of bf16 H in two parts (B = 2) also the second array
+  // rows past the last read as zeros; of bf16 H also the second array
   const __amdgpu_buffer_rsrc_t xr[2] = {buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB),
-                                        buf_rsrc(xb + (B == 2 ? p.h_low : 0) + (int64_t)m0 * KB, (size_t)m_rows * KB)};
+                                        buf_rsrc(xb + (GU ? 0 : p.h_low) + (int64_t)m0 * KB, (size_t)m_rows * KB)};
   const int nb0 = (t.nb * 4 + w) * NF;  // the wavefront's first 16-column block
   __amdgpu_buffer_rsrc_t cr[NM], sr[NM];
 #pragma unroll
@@ -582,7 +579,8 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
   // Through LDS, so that the stores are 16 bytes a lane and whole rows of the workgroup's columns: a lane's own values are
   // four rows of one column (by themselves 771 x 128, f = 5888, 24 experts, top-8 takes 87 us of gate/up, most of it stores).
   constexpr int CB = 64 * NF * XB, PITCH = CB + 16;  // bytes of a row
-  static_assert(ROWS * PITCH <= (int)sizeof(xs), "the output tile");
+  constexpr int PARTS = GU && !X::F32 ? 2 : 1;       // of H
+  static_assert(PARTS * ROWS * PITCH <= (int)sizeof(xs), "the output tile");
   char* out = xs[0];
   __syncthreads();
 #pragma unroll
@@ -593,18 +591,20 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
       for (int r = 0; r < 4; ++r) {
         float v = acc[0][i][m][r];
         if constexpr (GU) v = silu_of(v, T{}) * acc[NM - 1][i][m][r];
-        if constexpr (GU && std::is_same<T, bf16>::value)
-          if (p.h_low) store_h_low(p, (rs + m0 + 16 * m + 4 * q + r) * p.f + (nb0 + i) * 16 + li, v, 16 * m + 4 * q + r < m_rows);
-        *reinterpret_cast<T*>(out + (16 * m + 4 * q + r) * PITCH + ((w * NF + i) * 16 + li) * XB) = from_f<T>(v);
+        T* o = reinterpret_cast<T*>(out + (16 * m + 4 * q + r) * PITCH + ((w * NF + i) * 16 + li) * XB);
+        *o = from_f<T>(v);
+        if constexpr (PARTS == 2) o[ROWS * PITCH / XB] = h_rest(v);
       }
   __syncthreads();
   constexpr int PER = CB / 16;  // 16-byte chunks of a row
-  for (int c = tid; c < ROWS * PER; c += 256) {
-    const int r = c / PER, o = (c - r * PER) * 16;
-    if (r >= m_rows) break;
-    char* dst = GU ? (char*)p.h + (rs + m0 + r) * p.f * XB : (char*)p.y + (rs + m0 + r) * p.d * XB;
-    st_chunk(dst + (int64_t)t.nb * CB + o, ld_chunk(out + r * PITCH + o));
-  }
+#pragma unroll
+  for (int n = 0; n < PARTS; ++n)
+    for (int c = tid; c < ROWS * PER; c += 256) {
+      const int r = c / PER, o = (c - r * PER) * 16;
+      if (r >= m_rows) break;
+      char* dst = GU ? (char*)p.h + n * p.h_low + (rs + m0 + r) * p.f * XB : (char*)p.y + (rs + m0 + r) * p.d * XB;
+      st_chunk(dst + (int64_t)t.nb * CB + o, ld_chunk(out + (n * ROWS + r) * PITCH + o));
+    }
 }
 
 // K of up to 256 (U = 1 or 2 steps): the group's rows stay in LDS and the four wavefronts, with 16 NF columns each, walk over
@@ -614,11 +614,12 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
 // gate/up 70 us there).
 template <typename T, bool GU, int MT, int NF, int SG, int U>
 __global__ __launch_bounds__(256, 2) void q4_short_kernel(Q4Args p) {
-  typedef Acts<T, (GU || MT > 1) ? 1 : 2> X;  // up to 16 rows H comes in two parts
+  typedef Acts<T, GU ? 1 : 2> X;
   constexpr int NM = GU ? 2 : 1, NP = X::NP, XC = X::XC, XB = sizeof(T), ROWS = 16 * MT, PLANE = ROWS * 256;
   constexpr int CB = 16 * NF * XB, PITCH = CB + 16;  // bytes of a wavefront's output row
+  constexpr int PARTS = GU && !X::F32 ? 2 : 1;       // of H
   __shared__ __align__(16) char xs[U][NP * PLANE];
-  __shared__ __align__(16) char turn[4][ROWS * PITCH];
+  __shared__ __align__(16) char turn[4][PARTS * ROWS * PITCH];
   Q4Tile t;
   if (!q4_tile(p, blockIdx.x, ROWS, t)) return;
   const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, li = lane & 15;
@@ -628,7 +629,7 @@ __global__ __launch_bounds__(256, 2) void q4_short_kernel(Q4Args p) {
   const int64_t rs = routed ? (int64_t)t.row0 : p.shared0 + (int64_t)(t.g - p.Eloc) * p.T;
   const char* xb = GU ? (routed ? (const char*)p.xp + (int64_t)t.row0 * KB : (const char*)p.x) : (const char*)p.h + rs * KB;
   const int m0 = t.ch * ROWS, m_rows = min(t.rows - m0, ROWS);
-  // rows past the last read as zeros; of bf16 H in two parts also the second array
+  // rows past the last read as zeros; of bf16 H also the second array
   const __amdgpu_buffer_rsrc_t xr[2] = {buf_rsrc(xb + (int64_t)m0 * KB, (size_t)m_rows * KB),
                                         buf_rsrc(xb + (GU ? 0 : p.h_low) + (int64_t)m0 * KB, (size_t)m_rows * KB)};
   // column blocks b0 .. b1 of 64 NF columns
@@ -698,17 +699,17 @@ __global__ __launch_bounds__(256, 2) void q4_short_kernel(Q4Args p) {
             const int row = 16 * m + 4 * q + r;
             float v = acc[0][i][m][r];
             if constexpr (GU) v = silu_of(v, T{}) * acc[NM - 1][i][m][r];
-            if constexpr (GU && std::is_same<T, bf16>::value)
-              if (p.h_low) store_h_low(p, (rs + m0 + row) * p.f + col + 16 * i + li, v, row < m_rows);
-            *reinterpret_cast<T*>(out + row * PITCH + (16 * i + li) * XB) = from_f<T>(v);
+            T* o = reinterpret_cast<T*>(out + row * PITCH + (16 * i + li) * XB);
+            *o = from_f<T>(v);
+            if constexpr (PARTS == 2) o[ROWS * PITCH / XB] = h_rest(v);
           }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       constexpr int PER = CB / 16;  // 16-byte chunks of a row
 #pragma unroll
-      for (int c = 0; c < ROWS * PER / 64; ++c) {
-        const int r = (c * 64 + lane) / PER, o = (c * 64 + lane) % PER * 16;
-        char* dst = GU ? (char*)p.h + (rs + m0 + r) * p.f * XB : (char*)p.y + (rs + m0 + r) * p.d * XB;
-        if (r < m_rows) st_chunk(dst + (int64_t)col * XB + o, ld_chunk(out + r * PITCH + o));
+      for (int c = 0; c < PARTS * ROWS * PER / 64; ++c) {
+        const int n = c / (ROWS * PER / 64), r = (c * 64 + lane) / PER - n * ROWS, o = (c * 64 + lane) % PER * 16;
+        char* dst = GU ? (char*)p.h + n * p.h_low + (rs + m0 + r) * p.f * XB : (char*)p.y + (rs + m0 + r) * p.d * XB;
+        if (r < m_rows) st_chunk(dst + (int64_t)col * XB + o, ld_chunk(out + (n * ROWS + r) * PITCH + o));
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
@@ -733,12 +734,12 @@ hipError_t q4_run_split(const moe_desc& d, Q4Args a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, bool GU, int MT, int NF, int SG, int D, int B = 1>
+template <typename T, bool GU, int MT, int NF, int SG, int D>
 hipError_t q4_run_rows(const moe_desc& d, Q4Args a, hipStream_t s) {
   a.n_blocks = (GU ? d.d_ff : d.d_model) / (64 * NF);
   const unsigned grid = (unsigned)((chunks_of(d, 16 * MT) * a.n_blocks + 7) / 8 * 8);
   KernelTimer kt(GU ? "q4_gate_up" : "q4_down", s);
-  hipLaunchKernelGGL((q4_rows_kernel<T, GU, MT, NF, SG, D, B>), dim3(grid), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((q4_rows_kernel<T, GU, MT, NF, SG, D>), dim3(grid), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -764,23 +765,30 @@ hipError_t q4_run_short(const moe_desc& d, Q4Args a, hipStream_t s) {
 //     over 8 wavefronts. 64 columns to a workgroup from 280 workgroups of 32 on (gate/up: and more than 2 rows), which
 //     share their reads of the rows; 32 below, and in the down projection 16 where there are less than 160 of 32;
 //   * else shared rows. Gate/up: 16-row chunks up to 8 rows, 32-row chunks above. Down, whose K is the long one: 16-row
-//     chunks with four steps in flight, or, above 40 rows and where that leaves a workgroup per CU, 32 rows x 128 columns.
-// us of split 32 / split 64 / rows 16 / rows 32 (down: rows 16 / rows 32 x 128), group 64, at T, d, f, E, k, shared:
-//   gate/up:  1, 2048, 1408, 64, 6, 2   10.1 /  9.9 / 11.2 / 12.6     down:  7.3 /  7.4 /  8.2 /  9.5
-//             1, 4096, 14336, 8, 2      27.0 / 26.8 / 25.5 / 28.5           17.6 / 21.0 / 38.9 / 66.8
-//             8, 1024, 2816, 16, 2      11.5 / 11.2 / 10.3 / 10.1            7.9 /  8.2 / 10.6 / 13.7
-//             16, 2048, 1408, 64, 6, 2  39.5 / 38.0 / 33.0 / 40.0           31.7 / 25.7 / 20.1 / 20.2
-//             16, 4096, 1408, 8, 2      15.6 / 13.6 / 18.1 / 19.2           11.9 / 10.0 /  9.0 / 10.0
-//             24, 4096, 14336, 8, 2     96.3 / 89.5 / 84.8 / 85.7           60.4 / 50.8 / 49.5 / 75.3
-//             64, 1024, 2816, 16, 2     19.2 / 16.1 / 14.0 / 12.5           11.2 /  9.4 / 11.0 / 13.9
-//             128, 4096, 14336, 8, 2   219.3 / 163  / 136  / 124           167   / 107  / 91.2 / 85.3
-//             777, 1024, 2816, 16, 2    95.2 / 67.4 / 38.2 / 30.7           56.9 / 37.0 / 23.2 / 20.2
-//             254, 128, 6912, 8, 4                                          31.3 / 21.8 / 18.5 / 28.6
-// Split 16 / 32 / 64, down: 1, 640, 11392, 6, 6 11.5 / 14.7 / 17.2; 14, 128, 14208, 8, 4 23.1 / 24.1 / 26.2; 4, 1024, 2816,
-// 16, 2 9.0 / 7.9 / 8.8; 2, 4096, 4096, 8, 2 13.4 / 12.3 / 10.9; 1, 4096, 14336, 8, 2 30.2 / 21.6 / 24.6. Sixteen wavefronts
-// were no faster (23.1, 12.0, 10.8, 18.9 and 32.0 us for these with 16 columns).
-// Walking / rows 32: gate/up 771, 128, 5888, 24, 8 50 / 73; 700, 256, 14336, 4, 2 43 / 50; down 451, 4096, 128, 256, 8, 2
-// 31 / 70 (rows 32 x 128: 51); 451, 4096, 256, 64, 8, 2 27 / 41 (34).
+//     chunks of 64 columns with four steps in flight, or, where that leaves two workgroups per CU, of 128 columns with two.
+// us of split 32 / split 64 / rows 16 / rows 32 (down: rows 16 / rows 16 x 128), group 64, at T, d, f, E, k, shared:
+//   gate/up:  1, 2048, 1408, 64, 6, 2    9.9 / 10.0 / 12.0 / 13.1     down:  7.8 /  7.7 /  9.0 / 10.3
+//             1, 4096, 14336, 8, 2      25.8 / 25.7 / 26.4 / 29.1           21.6 / 24.1 / 44.9 / 65.7
+//             8, 1024, 2816, 16, 2      10.6 / 11.2 / 10.2 / 10.7            9.0 /  9.1 / 12.2 / 15.1
+//             16, 2048, 1408, 64, 6, 2  35.2 / 35.4 / 34.5 / 40.7           35.0 / 28.4 / 23.6 / 20.8
+//             16, 4096, 1408, 8, 2      15.3 / 14.0 / 18.2 / 19.7           13.6 / 10.3 / 10.5 / 10.5
+//             24, 4096, 14336, 8, 2     91.5 / 88.2 / 86.8 / 88.2           91.3 / 63.8 / 59.2 / 72.0
+//             48, 4096, 14336, 8, 2    105.2 / 92.4 / 94.0 / 92.5          127.4 / 92.4 / 75.6 / 79.0
+//             64, 1024, 2816, 16, 2     16.1 / 15.1 / 12.9 / 13.1           13.8 / 11.3 / 12.5 / 15.0
+//             128, 4096, 14336, 8, 2   188   / 145  / 135  / 124           269   / 162  / 122  / 104
+//             400, 1024, 1408, 16, 2    23.8 / 19.5 / 14.3 / 14.0           27.0 / 18.4 / 13.6 / 12.4
+//             777, 1024, 2816, 16, 2    65.1 / 56.0 / 34.3 / 31.1           72.7 / 46.3 / 32.0 / 27.9
+//             1000, 4096, 4096, 8, 2   312   / 222  / 188  / 157           482   / 276  / 186  / 142
+//             254, 128, 6912, 8, 4                                          31.3 / 21.8 / 21.8 / 28.9
+// (32 rows x 128 columns of the down projection: 80.5, 84.1, 119, 16.0, 27.9, 140 us for 24, 48, 128,
+// 400, 777 and 1000 tokens.) Split 16 / 32 / 64, down: 1, 640, 11392, 6, 6 11.7 / 14.7 / 18.1; 14, 128, 14208, 8, 4 22.9 / 24.1
+// / 26.4; 4, 1024, 2816, 16, 2 8.9 / 7.8 / 8.7; 2, 4096, 4096, 8, 2 13.4 / 12.3 / 10.9; 1, 4096, 14336, 8, 2 30.5 / 21.6 / 24.1.
+// Sixteen wavefronts were no faster than eight (23.1, 12.0, 10.8, 18.9 and 32.0 us for these with 16 columns).
+// Walking / rows 32: gate/up 771, 128, 5888, 24, 8 65 / 84; 700, 256, 14336, 4, 2 49 / 49; walking / rows 16 x 128: down 451,
+// 4096, 128, 256, 8, 2 31 / 51; 451, 4096, 256, 64, 8, 2 32 / 41.
+// The second part of H is a second array written and read: with one part (2.3e-3 of the outputs' norm off in place of 1.7e-3)
+// both projections of 24, 4096, 14336, 8, 2 took 134 us in place of 146, of 777, 1024, 2816, 16, 2 51 in place of 59, of 771,
+// 128, 5888, 24, 8 the gate/up 50 in place of 65.
 // Measured and not kept: 64- and 128-row chunks (777 rows: 36.8 and 49 us of gate/up), four wavefronts of a split, deeper
 // prefetch in the split, non-temporal loads of the codes (equal, and worse where calls follow each other), and the walking
 // kernel for K of up to 1024 with a chunk's rows held in LDS whole (rows 32 / walking, gate/up: 777, 1024, 2816, 16, 2 37.7 /
@@ -792,7 +800,6 @@ struct Q4Pick {
   double active, rows;  // experts with a row, and their rows
   int units;    // steps of 128 k
   bool split;   // K over the wavefronts
-  bool two;     // the projection (down) reads H in two parts
 };
 Q4Pick q4_rule(const moe_desc& d, int group, bool gate_up) {
   const double share = (double)d.top_k / d.n_experts;
@@ -802,11 +809,7 @@ Q4Pick q4_rule(const moe_desc& d, int group, bool gate_up) {
   const double bytes = active * (gate_up ? 2 : 1) * d.d_ff * d.d_model * (0.5 + 2.0 / group);
   const double chain = 2 + (gate_up ? 0.45 : 0.36) * units;
   const bool split = units >= 6 && rows <= 12 && chain > bytes / 5.5e6;
-  // A call of few outputs keeps H's second part where its products cost little. One part / two, us: T, d_model, d_ff, experts,
-  // top_k = 8, 512, 512, 8, 2: 9.4 / 9.5; 24, 256, 2816, 2, 2: 15.0 / 16.6; 24, 512, 4096, 4, 2: 18.2 / 20.2; 100, 128, 6912,
-  // 4, 2: 24.8 / 28.3. From 32768 outputs on they cost more than that (777 tokens: 13 us of 51).
-  const bool few = rows * active * d.d_model < 32768;
-  return {active, rows, units, split, split || (units <= 2 ? rows <= 16 : few)};
+  return {active, rows, units, split};
 }
 
 template <typename T, bool GU, int SG>
@@ -822,9 +825,8 @@ hipError_t q4_pick(const moe_desc& d, const Q4Args& a, hipStream_t s) {
   if constexpr (GU) {
     return k.rows <= 8 ? q4_run_rows<T, GU, 1, 1, SG, 2>(d, a, s) : q4_run_rows<T, GU, 2, 1, SG, 2>(d, a, s);
   } else {
-    if (k.two) return q4_run_rows<T, GU, 1, 1, SG, 4, sizeof(T) == 2 ? 2 : 1>(d, a, s);
-    const bool wide = k.rows > 40 && chunks_of(d, 32) * (d.d_model / 128) >= device_cus();
-    return wide ? q4_run_rows<T, GU, 2, 2, SG, 2>(d, a, s) : q4_run_rows<T, GU, 1, 1, SG, 4>(d, a, s);
+    const bool wide = chunks_of(d, 16) * (d.d_model / 128) >= 2 * device_cus();
+    return wide ? q4_run_rows<T, GU, 1, 2, SG, 2>(d, a, s) : q4_run_rows<T, GU, 1, 1, SG, 4>(d, a, s);
   }
 }
 
@@ -851,7 +853,7 @@ hipError_t q4_ffn(const moe_desc& d, int group, const Q4Args& a, const Q4Weights
 
 }  // namespace
 
-// H, in bf16 with room for a second array
+// H, of bf16 in two arrays
 static size_t h_bytes(const moe_desc& d) { return align256((size_t)rows_total(d) * d.d_ff * elem_bytes(d)); }
 size_t ffn_q4_ws_bytes(const moe_desc& d) { return h_bytes(d) * (d.dtype == MOE_BF16 ? 2 : 1); }
 
@@ -869,7 +871,7 @@ hipError_t launch_ffn_q4(const moe_desc& d, int group, const void* x, const void
   a.x = x;
   a.xp = xp;
   a.h = ws;
-  a.h_low = d.dtype == MOE_BF16 && q4_rule(d, group, false).two ? (int64_t)h_bytes(d) : 0;
+  a.h_low = d.dtype == MOE_BF16 ? (int64_t)h_bytes(d) : 0;
   a.y = yp;
   if (d.dtype == MOE_BF16) return q4_ffn<bf16>(d, group, a, gate, up, down, s);
   return q4_ffn<float>(d, group, a, gate, up, down, s);
