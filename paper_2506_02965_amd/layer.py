@@ -70,7 +70,8 @@ class Q4Experts:
 
 class MoELayer:
     """gate: a pcmoe.make_gate(...) for gated routing. checkpoint: keep the activations of the backward in 8 bits;
-    `saved`, the buffer of their full form, may then be shared by layers that run one after the other."""
+    `saved`, the buffer of their full form, may then be shared by layers that run one after the other: at least
+    MOE_WS_FFN_SAVED bytes of the largest of them."""
 
     def __init__(self, cfg, device="cuda", backward=None, router_backward=None, gate=None, checkpoint=False, saved=None):
         self.cfg = cfg
@@ -97,11 +98,11 @@ class MoELayer:
         self.y = torch.empty(T, d, dtype=dt, **kw)
         ws = lambda which: torch.empty(max(P.moe_workspace_size(self.desc, which), 1), dtype=torch.uint8, **kw)
         self.ws_permute = ws(P.MOE_WS_PERMUTE)
+        if saved is not None:
+            self._check_saved(saved)
         self.saved = ws(P.MOE_WS_FFN_SAVED) if saved is None else saved
         if checkpoint:
             self.ckpt = ws(P.MOE_WS_FFN_CKPT)
-        elif saved is not None:
-            raise ValueError("a shared saved buffer needs checkpoint=True: it does not outlive the next layer's forward")
         self.ws_q4 = None   # of forward_q4, allocated by its first call
         self.ws_ffn_fwd = ws(P.MOE_WS_FFN_FWD)
         if self.backward_enabled:
@@ -118,6 +119,18 @@ class MoELayer:
                 self.dlogits = torch.empty(T, E, dtype=torch.float32, **kw)
                 self.dw_router = torch.empty(E, d, dtype=torch.float32, **kw)
                 self.ws_route_bwd = ws(P.MOE_WS_ROUTE_BWD)
+
+    def _check_saved(self, saved):
+        """The calls that write a saved buffer do not take its size, so a caller's is measured here."""
+        if not self.checkpoint:
+            raise ValueError("a shared saved buffer needs checkpoint=True: it does not outlive the next layer's forward")
+        if saved.device != self.logits.device:
+            raise ValueError(f"the shared saved buffer is on device {saved.device}, the layer on {self.logits.device}")
+        if not saved.is_contiguous():
+            raise ValueError("the shared saved buffer is not contiguous")
+        need, have = P.moe_workspace_size(self.desc, P.MOE_WS_FFN_SAVED), saved.numel() * saved.element_size()
+        if have < need:
+            raise ValueError(f"the shared saved buffer has {have} bytes, this layer needs {need} bytes (MOE_WS_FFN_SAVED)")
 
     # ------------------------------------------------------------------ forward
     def route(self, w: LayerWeights):

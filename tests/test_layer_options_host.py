@@ -1,0 +1,36 @@
+"""What MoELayer and Q4Experts refuse, before any launch (no GPU is touched: the layers' buffers are host tensors)."""
+import os
+
+import pytest
+import torch
+
+from paper_2506_02965_amd import pcmoe as P
+from paper_2506_02965_amd.layer import MoELayer
+from paper_2506_02965_amd.synth import LayerConfig
+
+pytestmark = pytest.mark.skipif(not os.path.exists(P.LIB_PATH), reason="libpcmoe.so not built")
+CFG = LayerConfig("h", T=40, d=128, f=256, E=4, k=2, n_shared=1)
+
+
+def saved_bytes(cfg):
+    return P.moe_workspace_size(MoELayer(cfg, device="cpu", backward=False).desc, P.MOE_WS_FFN_SAVED)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_shared_buffer_of_a_smaller_layer_is_refused(dtype):
+    cfg = CFG.scaled(dtype=dtype)
+    need = saved_bytes(cfg)
+    for n in (0, 1, need - 1, saved_bytes(cfg.scaled(T=39)), saved_bytes(cfg.scaled(f=128))):
+        with pytest.raises(ValueError, match=f"{need} bytes"):
+            MoELayer(cfg, device="cpu", checkpoint=True, saved=torch.empty(n, dtype=torch.uint8))
+    for ok in (torch.empty(need, dtype=torch.uint8), torch.empty(saved_bytes(cfg.scaled(T=41)), dtype=torch.uint8),
+               torch.empty((need + 3) // 4, dtype=torch.float32)):
+        assert MoELayer(cfg, device="cpu", checkpoint=True, saved=ok).saved is ok
+
+
+def test_shared_buffer_elsewhere_or_strided_is_refused():
+    need = saved_bytes(CFG)
+    with pytest.raises(ValueError, match="device"):
+        MoELayer(CFG, device="cpu", checkpoint=True, saved=torch.empty(need, dtype=torch.uint8, device="meta"))
+    with pytest.raises(ValueError, match="contiguous"):
+        MoELayer(CFG, device="cpu", checkpoint=True, saved=torch.empty(2 * need, dtype=torch.uint8)[::2])
