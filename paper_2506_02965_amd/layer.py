@@ -59,11 +59,15 @@ class Q4Experts:
 
     @staticmethod
     def pack(w: LayerWeights, group: int = 64) -> "Q4Experts":
+        names = {torch.bfloat16: "bf16", torch.float32: "f32"}
+
         def one(t):
+            if t.dtype not in names:
+                raise ValueError(f"weights of dtype {t.dtype}: bfloat16 or float32 are packed")
             n, rows, cols = t.shape
             codes = torch.empty(n, rows // 16, cols // 128, 4, 16, 4, 4, dtype=torch.uint8, device=t.device)
             scales = torch.empty(n, rows // 16, cols // group, 16, dtype=torch.bfloat16, device=t.device)
-            P.moe_q4_pack(n, rows, cols, group, "bf16" if t.dtype == torch.bfloat16 else "f32", t, codes, scales)
+            P.moe_q4_pack(n, rows, cols, group, names[t.dtype], t, codes, scales)
             return codes, scales
         return Q4Experts(group, one(w.w_gate), one(w.w_up), one(w.w_down))
 

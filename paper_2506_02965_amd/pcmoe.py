@@ -239,7 +239,10 @@ def moe_ffn_restore(desc, offsets, ckpt, ckpt_bytes, saved, stream=None):
 
 
 def _dtype(dtype) -> int:
-    return MOE_BF16 if dtype == "bf16" else MOE_F32
+    kinds = {"bf16": MOE_BF16, "f32": MOE_F32, "fp32": MOE_F32}
+    if dtype not in kinds:
+        raise ValueError(f"dtype {dtype!r} is not one of {sorted(kinds)}")
+    return kinds[dtype]
 
 
 def moe_q4_pack(n, rows, cols, group, dtype, w, codes, scales, stream=None):

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2506_02965_amd import pcmoe as P
-from paper_2506_02965_amd.layer import MoELayer
+from paper_2506_02965_amd.layer import LayerWeights, MoELayer, Q4Experts
 from paper_2506_02965_amd.synth import LayerConfig
 
 pytestmark = pytest.mark.skipif(not os.path.exists(P.LIB_PATH), reason="libpcmoe.so not built")
@@ -34,3 +34,18 @@ def test_shared_buffer_elsewhere_or_strided_is_refused():
         MoELayer(CFG, device="cpu", checkpoint=True, saved=torch.empty(need, dtype=torch.uint8, device="meta"))
     with pytest.raises(ValueError, match="contiguous"):
         MoELayer(CFG, device="cpu", checkpoint=True, saved=torch.empty(2 * need, dtype=torch.uint8)[::2])
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bfloat16", "half", "", None])
+def test_weight_types_other_than_the_librarys_are_refused(dtype):
+    """Read as fp32, a 16-bit tensor would be read past its end."""
+    for call in (P.moe_q4_pack, P.moe_q4_unpack):
+        with pytest.raises(ValueError, match="dtype"):
+            call(1, 16, 128, 32, dtype, None, None, None, stream=0)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64])
+def test_packing_other_weight_types_is_refused(dtype):
+    w = [torch.zeros(2, *s, dtype=dtype) for s in ((256, 128), (256, 128), (128, 256))]
+    with pytest.raises(ValueError, match="dtype"):
+        Q4Experts.pack(LayerWeights(None, None, None, 1, *w))
