@@ -108,6 +108,7 @@ class MoELayer:
         if checkpoint:
             self.ckpt = ws(P.MOE_WS_FFN_CKPT)
         self.ws_q4 = None   # of forward_q4, allocated by its first call
+        self.saved_nothing = False  # the last forward was forward_q4
         self.ws_ffn_fwd = ws(P.MOE_WS_FFN_FWD)
         if self.backward_enabled:
             G = Eloc + S
@@ -149,6 +150,7 @@ class MoELayer:
                       self.x_perm, self.ws_permute, self.ws_permute.numel())
 
     def ffn_fwd(self, w: LayerWeights):
+        self.saved_nothing = False
         P.moe_expert_ffn_fwd(self.desc, w.x, self.x_perm, self.offsets, w.w_gate, w.w_up, w.w_down, self.y_perm,
                              self.saved, self.ws_ffn_fwd, self.ws_ffn_fwd.numel())
         if self.checkpoint:
@@ -165,10 +167,12 @@ class MoELayer:
         return self.y
 
     def forward_q4(self, w: LayerWeights, q: Q4Experts):
-        """The forward with the experts' 4-bit weights (inference: nothing is saved; w's expert weights are not read)."""
+        """The forward with the experts' 4-bit weights (inference: nothing is saved, no backward can
+        follow; w's expert weights are not read)."""
         if self.ws_q4 is None:
             self.ws_q4 = torch.empty(P.moe_workspace_size(self.desc, P.MOE_WS_FFN_Q4), dtype=torch.uint8,
                                      device=self.device)
+        self.saved_nothing = True
         self.route(w)
         self.permute(w)
         P.moe_expert_ffn_q4(self.desc, q.group, w.x, self.x_perm, self.offsets, *q.gate, *q.up, *q.down, self.y_perm,
@@ -177,10 +181,15 @@ class MoELayer:
         return self.y
 
     # ----------------------------------------------------------------- backward
+    def _need_saved(self):
+        if self.saved_nothing:
+            raise RuntimeError("the last forward was forward_q4, which saves nothing for a backward")
+
     def combine_bwd(self, dy):
         P.moe_combine_bwd(self.desc, dy, self.y_perm, self.slot_to_row, self.topk_w, self.dy_perm, self.dgate)
 
     def ffn_bwd(self, w: LayerWeights, dy):
+        self._need_saved()
         if self.checkpoint:
             P.moe_ffn_restore(self.desc, self.offsets, self.ckpt, self.ckpt.numel(), self.saved)
         P.moe_expert_ffn_bwd(self.desc, w.x, self.x_perm, dy, self.dy_perm, self.offsets, w.w_gate, w.w_up, w.w_down,
@@ -200,6 +209,7 @@ class MoELayer:
                           w.w_router, self.dx)
 
     def backward(self, w: LayerWeights, dy=None):
+        self._need_saved()
         dy = w.dy if dy is None else dy
         self.combine_bwd(dy)
         self.ffn_bwd(w, dy)

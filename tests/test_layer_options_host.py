@@ -49,3 +49,28 @@ def test_packing_other_weight_types_is_refused(dtype):
     w = [torch.zeros(2, *s, dtype=dtype) for s in ((256, 128), (256, 128), (128, 256))]
     with pytest.raises(ValueError, match="dtype"):
         Q4Experts.pack(LayerWeights(None, None, None, 1, *w))
+
+
+def test_backward_needs_the_activations_of_its_own_forward(monkeypatch):
+    """forward_q4 routes anew and saves nothing: a backward after it would read activations (or, where no forward ran, a tile
+    plan) that do not belong to its rows."""
+    calls = []
+    for name in P.EXPORTS + P.EXPORTS_EXT:
+        if name not in ("moe_workspace_size", "moe_status_string", "moe_last_error"):
+            monkeypatch.setattr(P, name, lambda *a, _n=name, **k: calls.append(_n), raising=False)
+    x = torch.zeros(CFG.T, CFG.d)
+    w = LayerWeights(x, None, None, 1, None, None, None)
+    q = Q4Experts(32, (None, None), (None, None), (None, None))
+    for checkpoint in (False, True):
+        layer = MoELayer(CFG, device="cpu", checkpoint=checkpoint)
+        layer.forward_q4(w, q)
+        calls.clear()
+        with pytest.raises(RuntimeError, match="forward_q4"):
+            layer.backward(w, x)
+        assert not calls
+        layer.forward(w)
+        layer.backward(w, x)
+        assert "moe_expert_ffn_bwd" in calls
+        layer.forward_q4(w, q)
+        with pytest.raises(RuntimeError, match="forward_q4"):
+            layer.ffn_bwd(w, x)
