@@ -246,14 +246,19 @@ class MoELayer:
         return int(self.offsets[-1].item())
 
 
-def training_footprint(cfg, local_count: int, master: bool = True) -> dict:
+def training_footprint(cfg, local_count: int, master: bool = True, checkpoint: bool = False,
+                       shared_saved: bool = False) -> dict:
     """Device bytes one party allocates for the expert layer's training step (route, permute, expert FFN forward
     and backward, combine and its adjoint, router adjoint, expert AdamW update) when it hosts `local_count` of the
     cfg.E routed experts, by category:
       expert_state  hosted experts' weights and weight gradients (dtype) plus fp32 moments and master copy;
       activations   row-space buffers (capacity T*k + S*T rows), saved activations and the FFN workspaces;
       owner         the owner-side buffers of its own T tokens (input, router, combine, input gradient).
+    checkpoint: with the 8-bit checkpoint of a MoELayer(checkpoint=True). shared_saved: without the saved activations, for
+    a layer that is given a buffer which all the layers of a stack share, and whose size is returned as `shared_saved`.
     The sizes are those MoELayer and init_update_state allocate, with workspace sizes from the library."""
+    if shared_saved and not checkpoint:
+        raise ValueError("a shared saved buffer needs checkpoint=True")
     T, d, f, E, k, S = cfg.T, cfg.d, cfg.f, cfg.E, cfg.k, cfg.n_shared
     es = 2 if cfg.dtype == "bf16" else 4
     desc = P.make_desc(T, d, f, E, k, 0, local_count, S, cfg.renormalize, cfg.dtype)
@@ -265,7 +270,8 @@ def training_footprint(cfg, local_count: int, master: bool = True) -> dict:
                    + R * d * es              # y_perm
                    + T * k * d * es          # dy_perm
                    + R * d * es              # dx_perm
-                   + ws(P.MOE_WS_FFN_SAVED) + ws(P.MOE_WS_FFN_FWD) + ws(P.MOE_WS_FFN_BWD) + ws(P.MOE_WS_PERMUTE)
+                   + (0 if shared_saved else ws(P.MOE_WS_FFN_SAVED)) + (ws(P.MOE_WS_FFN_CKPT) if checkpoint else 0)
+                   + ws(P.MOE_WS_FFN_FWD) + ws(P.MOE_WS_FFN_BWD) + ws(P.MOE_WS_PERMUTE)
                    + (local_count + 1) * 4 + max(local_count, 1) * 4 + 2 * T * k * 4)   # offsets, counts, maps
     owner = (T * d * es * 3                  # x, y, dx
              + T * d * es                    # dy
@@ -273,5 +279,8 @@ def training_footprint(cfg, local_count: int, master: bool = True) -> dict:
              + T * E * 4 * 2                 # logits, dlogits
              + T * k * (4 + 4 + 4)           # topk_idx, topk_w, dgate
              + ws(P.MOE_WS_ROUTE_BWD))
-    return {"local_experts": local_count, "expert_state": expert_state, "activations": activations, "owner": owner,
-            "total": expert_state + activations + owner}
+    out = {"local_experts": local_count, "expert_state": expert_state, "activations": activations, "owner": owner,
+           "total": expert_state + activations + owner}
+    if shared_saved:
+        out["shared_saved"] = ws(P.MOE_WS_FFN_SAVED)
+    return out

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2506_02965_amd import pcmoe as P
-from paper_2506_02965_amd.layer import LayerWeights, MoELayer, Q4Experts
+from paper_2506_02965_amd.layer import LayerWeights, MoELayer, Q4Experts, training_footprint
 from paper_2506_02965_amd.synth import LayerConfig
 
 pytestmark = pytest.mark.skipif(not os.path.exists(P.LIB_PATH), reason="libpcmoe.so not built")
@@ -74,3 +74,23 @@ def test_backward_needs_the_activations_of_its_own_forward(monkeypatch):
         layer.forward_q4(w, q)
         with pytest.raises(RuntimeError, match="forward_q4"):
             layer.ffn_bwd(w, x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_training_footprint_of_a_checkpointed_layer(dtype):
+    """What a layer with checkpoint=True allocates, its own saved buffer or one that several layers share: the accounts differ
+    by the buffers that MoELayer allocates."""
+    cfg = CFG.scaled(dtype=dtype)
+    plain = training_footprint(cfg, cfg.E)
+    desc = MoELayer(cfg, device="cpu", backward=False).desc
+    saved, ckpt = (P.moe_workspace_size(desc, which) for which in (P.MOE_WS_FFN_SAVED, P.MOE_WS_FFN_CKPT))
+    own = MoELayer(cfg, device="cpu", backward=False, checkpoint=True)
+    assert (own.saved.numel(), own.ckpt.numel()) == (saved, ckpt)
+    one = training_footprint(cfg, cfg.E, checkpoint=True)
+    assert one["activations"] == plain["activations"] + ckpt and one["total"] == plain["total"] + ckpt
+    shared = training_footprint(cfg, cfg.E, checkpoint=True, shared_saved=True)
+    assert shared["activations"] == plain["activations"] - saved + ckpt
+    assert shared["total"] == plain["total"] - saved + ckpt and shared["shared_saved"] == saved
+    assert {k: v for k, v in training_footprint(cfg, cfg.E, checkpoint=False).items()} == plain
+    with pytest.raises(ValueError):
+        training_footprint(cfg, cfg.E, shared_saved=True)
