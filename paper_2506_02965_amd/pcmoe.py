@@ -135,8 +135,11 @@ def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
     import torch
-    if torch.cuda.is_initialized():  # the same stream without its Python object: 0.2 us in place of 2.8, of a call's 7
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    if torch.cuda.is_initialized():
+        try:  # the same stream without its Python object: 0.2 us in place of 2.8, of a call's 7
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        except AttributeError:  # private names, which another torch need not have
+            pass
     return torch.cuda.current_stream().cuda_stream
 
 

@@ -94,3 +94,18 @@ def test_training_footprint_of_a_checkpointed_layer(dtype):
     assert {k: v for k, v in training_footprint(cfg, cfg.E, checkpoint=False).items()} == plain
     with pytest.raises(ValueError):
         training_footprint(cfg, cfg.E, shared_saved=True)
+
+
+def test_current_stream_without_torchs_private_names(monkeypatch):
+    """The stream lookup of every call takes torch's public way where its private short cut is gone."""
+    class Stream:
+        cuda_stream = 0x5170
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream())
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        with monkeypatch.context() as m:
+            m.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+            m.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0xBAD, raising=False)
+            assert P._stream(None) == 0xBAD
+            m.delattr(torch._C, name)
+            assert P._stream(None) == 0x5170
