@@ -33,9 +33,9 @@ typedef struct {
  *   - w = scale * s[I] / sum s[I] (renormalize = 1) or scale * s[I]; the bias has no part in the weights.
  * s and c are formed in fp64 from the fp32 l; without select_bias the experts rank by l itself (the same order). Equal
  * values go to the lower index, experts and groups alike. An expert whose l or bias is NaN or -inf is never selected and
- * one whose l is has no part in the softmax; a group's value sums what selectable experts it has. Slots left over get
- * MOE_NO_EXPERT and weight 0: the other calls take them as slots hosted elsewhere. Where all the selected s are 0 in
- * fp64, renormalised weights are 0.
+ * one whose l is has no part in the softmax; a group's value sums what selectable experts it has. Experts of l = +inf share
+ * the softmax equally, as its limit. Slots left over get MOE_NO_EXPERT and weight 0: the other calls take them as slots
+ * hosted elsewhere. Where all the selected s are 0 in fp64, renormalised weights are 0.
  *   select_bias [E] fp32 or NULL; logit_bias, bias_groups, the other arguments and their layouts: moe_route
  * Errors as above, and MOE_ERR_INVALID_ARGUMENT for a setting outside the ranges stated in moe_gate, group_top = 2 with
  * groups of one expert, or top_k > topk_groups * (E / n_groups); MOE_ERR_UNSUPPORTED for more than 64 groups.

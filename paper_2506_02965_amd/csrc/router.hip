@@ -126,7 +126,8 @@ __device__ __forceinline__ void gated_select(const float (&v)[NT][QE], int E, in
       double zz = 0.0;
 #pragma unroll
       for (int qq = 0; qq < QE; ++qq) {
-        sc[n][qq] = v[n][qq] > -INFINITY ? exp((double)v[n][qq] - (double)m[n]) : 0.0;  // nothing of a masked or NaN expert
+        // nothing of a masked or NaN expert; the maximum may be +inf
+        sc[n][qq] = v[n][qq] > -INFINITY ? (v[n][qq] == m[n] ? 1.0 : exp((double)v[n][qq] - (double)m[n])) : 0.0;
         zz += sc[n][qq];
       }
       z[n] = wave_sum_f64(zz);
@@ -280,7 +281,8 @@ __device__ __forceinline__ void gated_select(const float (&v)[NT][QE], int E, in
   for (int n = 0; n < NT; ++n) {
     const bool filled = lane < k && myi[n] != NO_EXPERT;
     if (!ga.sigmoid && renorm) m[n] = wave_max_dpp(myl[n]);  // the largest of the chosen: the others' exponentials stay finite
-    double s = ga.sigmoid ? 1.0 / (1.0 + exp(-(double)myl[n])) : exp((double)myl[n] - (double)m[n]) / z[n];
+    double s = ga.sigmoid ? 1.0 / (1.0 + exp(-(double)myl[n]))
+                          : (myl[n] == m[n] ? 1.0 : exp((double)myl[n] - (double)m[n])) / z[n];
     if (!filled) s = 0.0;
     if (renorm) {
       const double t = sum8_f64(s);
@@ -825,7 +827,7 @@ __global__ __launch_bounds__(256) void gate_dlogits_kernel(int Tn, int E, int k,
       m = wave_max_dpp(m);
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
-        p[q] = p[q] > -INFINITY ? expf(p[q] - m) : 0.f;
+        p[q] = p[q] > -INFINITY ? (p[q] == m ? 1.f : expf(p[q] - m)) : 0.f;
         zp += p[q];
       }
       const float z = wave_sum(zp);
