@@ -35,3 +35,16 @@ def test_outputs_are_rounded_once(case):
     off = float((y[valid] != ref[valid].bfloat16().double()).double().mean())
     log(f"[q4] rounding {off:.4f} of the outputs differ from the rounded fp64 result")
     assert off <= 0.04, off
+
+
+@pytest.mark.parametrize("hosted,shared", [(256, 70), (256, 255), (3, 317)])
+def test_more_than_256_groups(hosted, shared):
+    """Hosted and shared experts together, up to the most that a call takes; most of them without a row."""
+    T, k = 2, 4
+    counts = [0] * hosted
+    for g in (0, hosted // 2, hosted - 1):
+        counts[g] = 2
+    log(f"[q4] groups {hosted} + {shared}")
+    y, ref, valid, _ = run(T, 128, 128, counts, min(k, hosted), 256, shared, 64, "bf16")
+    off = float((y[valid] != ref[valid].bfloat16().double()).double().mean())
+    assert off <= 0.04 and bool((y[~valid] == 77).all()), off
