@@ -51,6 +51,8 @@ moe_status moe_route_gated(const moe_desc* desc, const moe_gate* gate, const voi
  *                  softmax: dlogits[t, e] = s_te (c g_te - sum_e' s_te' c g_te'), g scattered onto E
  * and 0 elsewhere; slots of MOE_NO_EXPERT give nothing, whatever their dgate holds.
  *   dw_router = dlogits^T x and the other arguments: moe_route_bwd, whose conditions hold here too. logits is always needed.
+ *   For bf16 x, dlogits is multiplied as three bf16 numbers that add up to it: an infinite x can give NaN in place of an
+ *   infinity.
  */
 moe_status moe_route_gated_bwd(const moe_desc* desc, const moe_gate* gate, const void* x, const float* logits,
                                const int32_t* topk_idx, const float* topk_w, const float* dgate, float* dlogits,

@@ -1077,7 +1077,7 @@ size_t route_bwd_ws_bytes(const moe_desc& d) {
 //   tokens as K: lane (q, i) loads 16 bytes of tokens 8 q .. 8 q + 7 and turns the 8 x 8 block into operands of its columns
 //   8 i + s, s = 0 .. 7, by byte permutes; row i of expert tile m is expert NET i + m, so that a token's gradients of a
 //   lane's NET experts are one load. Tokens and experts past the end read as zeros.
-// An infinite gradient makes NaN (inf - inf in the split) where the fp32 contraction might make an infinity.
+// An infinite x makes NaN where a part of the gradient is 0; the fp32 contraction makes it only where the gradient is.
 constexpr int GDW_W = 8;
 template <int NET, bool VEC>
 __global__ __launch_bounds__(64 * GDW_W, 2) void gate_dw_kernel(int Tn, int d, int E, int tok_per_chunk,
@@ -1126,7 +1126,10 @@ __global__ __launch_bounds__(64 * GDW_W, 2) void gate_dw_kernel(int Tn, int d, i
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
           hi[b] = g[2 * p + b][m];
-          mid[b] = __float_as_uint(__uint_as_float(hi[b]) - __uint_as_float(hi[b] & 0xffff0000u));
+          // an infinity or a NaN is all in the first part (of a NaN the upper half might be an infinity's)
+          const bool special = (hi[b] & 0x7f800000u) == 0x7f800000u;
+          if (special && (hi[b] & 0x7fffffu)) hi[b] = 0x7fc00000u;
+          mid[b] = special ? 0u : __float_as_uint(__uint_as_float(hi[b]) - __uint_as_float(hi[b] & 0xffff0000u));
           low[b] = __float_as_uint(__uint_as_float(mid[b]) - __uint_as_float(mid[b] & 0xffff0000u));
         }
         a[m][0].w[p] = __builtin_amdgcn_perm(hi[1], hi[0], 0x07060302u);

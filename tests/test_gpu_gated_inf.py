@@ -49,3 +49,28 @@ def test_infinite_scores(T, score, renorm):
             ref = gate_formula(finite.double(), idx.long(), dg.double(), gw.double(), score, renorm, 1.5)
             size = np.maximum((gw.double() * dg.double()).abs().amax(1, keepdim=True).numpy(), 1e-30)
             assert np.all(np.abs(dl.cpu().double().numpy() - ref.numpy()) <= 32 * 2.0 ** -24 * size)
+
+
+@pytest.mark.parametrize("case", [(300, 8), (1000, 24), (2100, 64), (700, 66), (4100, 256)], ids=lambda c: "T{}_E{}".format(*c))
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinite_gradients(case, dtype):
+    """dW = dlogits^T x where some of dgate is infinite or NaN: infinities and NaN where the fp64 product has them, with the
+    same signs, and the other experts' rows as without them."""
+    T, n_experts = case
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator().manual_seed(T)
+    log(f"[gated grad] inf {case} {dtype}")
+    gate = P.make_gate("sigmoid")
+    _, logits, idx, gw, desc, x, _ = route(T, 128, n_experts, 2, dtype, gate, False)
+    dg = torch.randn(T, 2, generator=gen)
+    dg[5, 0], dg[T // 2, 1], dg[T - 1, 0] = math.inf, -math.inf, math.nan
+    dl, dw = torch.empty(T, n_experts, device="cuda"), torch.empty(n_experts, 128, device="cuda")
+    ws = torch.empty(max(1, P.moe_workspace_size(desc, P.MOE_WS_ROUTE_BWD)), dtype=torch.uint8, device="cuda")
+    P.moe_route_gated_bwd(desc, gate, x.cuda(), logits.cuda(), idx.cuda(), gw.cuda(), dg.cuda(), dl, dw, ws, ws.numel())
+    torch.cuda.synchronize()
+    got, ref = dw.cpu().double(), dl.cpu().double().t() @ x.double()
+    assert bool(torch.isinf(dl.cpu()).any()) and x.dtype == dt
+    assert torch.equal(torch.isnan(got), torch.isnan(ref)) and torch.equal(got == math.inf, ref == math.inf)
+    assert torch.equal(got == -math.inf, ref == -math.inf)
+    rows = torch.isfinite(ref).all(1)
+    assert float((got[rows] - ref[rows]).norm() / ref[rows].norm()) <= 2e-6
