@@ -60,7 +60,7 @@ moe_status moe_route_gated_bwd(const moe_desc* desc, const moe_gate* gate, const
 
 /*
  * What moe_expert_ffn_fwd saved, kept in 8 bits until the backward: a layer then holds MOE_WS_FFN_CKPT bytes (about 2.06
- * per element of G|U) in place of MOE_WS_FFN_SAVED (6 in bf16, 12 in fp32), and one saved buffer serves all the layers.
+ * per element of H) in place of MOE_WS_FFN_SAVED (6 in bf16, 12 in fp32), and one saved buffer serves all the layers.
  *   moe_ffn_checkpoint  reads saved after the forward and writes ckpt;
  *   moe_ffn_restore     writes saved for the moe_expert_ffn_bwd of the same call shape and offsets.
  * 32 consecutive columns of a row of G|U share a power of two 2^e, the smallest with max|v| <= 127 2^e (-126 <= e <= 121); a

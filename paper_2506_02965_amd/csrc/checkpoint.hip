@@ -16,9 +16,9 @@ namespace {
 
 constexpr int QB = 32;         // columns of a block
 constexpr int CK_THREADS = 256;
-// 16-byte chunks in flight per thread. Both kernels are bound by the memory (T = 8192, f = 14,336, 2 slots: 1.4 GB in 246 us,
-// 1.9 GB in 324 us, 5.8 TB/s each). What they read is read for the last time until its buffer is written again, so it is read
-// non-temporally (280 and 340 us without). us of both at 1 / 2 / 4 / 8 chunks: 654 / 567 / 595 / 608.
+// 16-byte chunks in flight per thread. Both kernels are bound by the memory (T = 8192, f = 14,336, 2 slots: 1.4 GB in 297 us
+// and 1.9 GB in 323 us in turn, 4.8 and 5.9 TB/s; the first 249 us at best). What they read is read for the last time until its buffer is written again, so it is read
+// non-temporally (34 and 16 us less). us of both at 1 / 2 / 4 / 8 chunks: 654 / 567 / 595 / 608.
 constexpr int CK_UNROLL = 2;
 
 struct CkptArgs {

@@ -611,7 +611,7 @@ __global__ __launch_bounds__(256, 2) void q4_rows_kernel(Q4Args p) {
 // p.walk blocks of 64 NF columns, the next block's weights loading meanwhile. Nothing is shared after the rows are there:
 // each wavefront turns its outputs in LDS of its own. In q4_rows_kernel, whose workgroup ends after one block, finding the
 // tile and waiting for the first loads were most of such a workgroup's time (771 tokens, d = 128, f = 5888, 24 experts, top-8:
-// gate/up 70 us there).
+// gate/up 70 us there, 50 here; with the second part of H 84 and 65).
 template <typename T, bool GU, int MT, int NF, int SG, int U>
 __global__ __launch_bounds__(256, 2) void q4_short_kernel(Q4Args p) {
   typedef Acts<T, GU ? 1 : 2> X;
@@ -789,8 +789,9 @@ hipError_t q4_run_short(const moe_desc& d, Q4Args a, hipStream_t s) {
 // The second part of H is a second array written and read: with one part (2.3e-3 of the outputs' norm off in place of 1.7e-3)
 // both projections of 24, 4096, 14336, 8, 2 took 134 us in place of 146, of 777, 1024, 2816, 16, 2 51 in place of 59, of 771,
 // 128, 5888, 24, 8 the gate/up 50 in place of 65.
-// Measured and not kept: 64- and 128-row chunks (777 rows: 36.8 and 49 us of gate/up), four wavefronts of a split, deeper
-// prefetch in the split, non-temporal loads of the codes (equal, and worse where calls follow each other), and the walking
+// Measured and not kept: 32- / 64- / 128-row chunks of gate/up (groups of 32: 777, 1024, 2816, 16, 2 37.2 / 38.3 / 43.2, 1000,
+// 4096, 4096, 8, 2 188 / 178 / 211; groups of 64: the first 32.6 / 38.4 / 84.2), and, with H in one part, four wavefronts of a
+// split, deeper prefetch in the split, non-temporal loads of the codes (equal, and worse where calls follow each other), the walking
 // kernel for K of up to 1024 with a chunk's rows held in LDS whole (rows 32 / walking, gate/up: 777, 1024, 2816, 16, 2 37.7 /
 // 39.6; 1500, 1024, 4096, 8, 2 83.9 / 81.3; 777, 512, 2048, 32, 4 29.7 / 25.8; down 777, 2048, 768, 64, 6 32.8 / 36.5), four
 // steps in flight of 32-row chunks (gate/up of the first 49.5 against 38.7), a group's scalings among the next one's products

@@ -768,7 +768,7 @@ __global__ __launch_bounds__(256) void route_dlogits_kernel(int Tn, int E, int k
 //   sigmoid:      dl_j = w_j (1 - s_j) g_j;       softmax: dl_e = p_e (c g_e - sum_i c p_i g_i) over all the experts.
 // 1 - s is formed as sigmoid(-l), which does not cancel. Slots that no expert fills give nothing.
 // A wavefront takes 8 tokens: first a lane per slot (lane 8 n + j has slot j of token n), so that the loads' latencies are
-// paid once for all of them, then the rows one by one, a lane per expert (T = 16,384, E = 64, top-6: 6.3 us, 8.2 with a
+// paid once for all of them, then the rows one by one, a lane per expert (T = 16,384, E = 64, top-6: 6.6 us, 8.2 with a
 // wavefront per token). DENSE, which reads whole rows of scores: one token (T = 1500, E = 8: 3.9 us, 10 with eight).
 template <bool DENSE>
 __global__ __launch_bounds__(256) void gate_dlogits_kernel(int Tn, int E, int k, int renorm, int sigmoid, float scale,
@@ -1070,9 +1070,9 @@ size_t route_bwd_ws_bytes(const moe_desc& d) {
 }
 
 // dW_router = dlogits^T x of bf16 tokens on v_mfma_f32_16x16x32_bf16: the gradients of the scores as three bf16 numbers that
-// add up to each fp32 one exactly (8 + 8 + 8 bits), so the products are those of the fp32 contraction at five times its rate
-// (T = 16,384, E = 64, d = 2048: 4.3 GFLOP, 28 us on the fp32 matrix cores, 11 for three bf16 products; the tokens' 67 MB take
-// 14). A workgroup holds 128 columns x 16 NET experts; its wavefronts take the chunk's tokens 32 at a time in turn, with
+// add up to each fp32 one exactly (8 + 8 + 8 bits), so the products are those of the fp32 contraction. Three of them take a
+// third of its time by the rates of large products, 1,586 and 154 TFLOP/s (T = 16,384, E = 64, d = 2048: 4.3 GFLOP, 28 us in
+// fp32, 8 for three bf16 products; the tokens' 67 MB take 14; 21.7 us measured). A workgroup holds 128 columns x 16 NET experts; its wavefronts take the chunk's tokens 32 at a time in turn, with
 // accumulators of their own, which meet in LDS half the columns at a time and are added in wavefront order.
 //   tokens as K: lane (q, i) loads 16 bytes of tokens 8 q .. 8 q + 7 and turns the 8 x 8 block into operands of its columns
 //   8 i + s, s = 0 .. 7, by byte permutes; row i of expert tile m is expert NET i + m, so that a token's gradients of a

@@ -168,7 +168,7 @@ class MoELayer:
 
     def forward_q4(self, w: LayerWeights, q: Q4Experts):
         """The forward with the experts' 4-bit weights (inference: nothing is saved, no backward can
-        follow; w's expert weights are not read)."""
+        follow; w's expert weights are not read and may be None)."""
         if self.ws_q4 is None:
             self.ws_q4 = torch.empty(P.moe_workspace_size(self.desc, P.MOE_WS_FFN_Q4), dtype=torch.uint8,
                                      device=self.device)
