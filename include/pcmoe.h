@@ -76,7 +76,7 @@ typedef struct {
   int32_t dtype;        /* moe_dtype */
 } moe_desc;
 
-/* moe_workspace_size(which) selectors (the last two belong to calls of pcmoe_ext.h) */
+/* moe_workspace_size(which) selectors (those from MOE_WS_FFN_Q4 on belong to calls of pcmoe_ext.h) */
 enum {
   MOE_WS_PERMUTE = 0,     /* scratch of moe_permute */
   MOE_WS_FFN_SAVED = 1,   /* activations saved by moe_expert_ffn_fwd for the backward */
@@ -84,7 +84,11 @@ enum {
   MOE_WS_FFN_BWD = 3,     /* scratch of moe_expert_ffn_bwd */
   MOE_WS_ROUTE_BWD = 4,   /* scratch of moe_route_bwd and moe_route_gated_bwd */
   MOE_WS_FFN_Q4 = 5,      /* scratch of moe_expert_ffn_q4 */
-  MOE_WS_FFN_CKPT = 6     /* the 8-bit checkpoint that moe_ffn_checkpoint writes */
+  MOE_WS_FFN_CKPT = 6,    /* the 8-bit checkpoint that moe_ffn_checkpoint writes */
+  MOE_WS_FFN_Q8 = 7,      /* scratch of moe_expert_ffn_q8 */
+  MOE_WS_NORM_BWD = 8,    /* scratch of moe_residual_norm_bwd */
+  MOE_WS_UPDATE_MUON = 9, /* scratch of moe_expert_update_muon ... */
+  MOE_WS_UPDATE_MUON_PRECISE = 10 /* ... in its precise form */
 };
 
 /* Bytes of device memory the selected buffer needs for this shape (0 if none). */

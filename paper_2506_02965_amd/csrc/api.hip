@@ -114,6 +114,53 @@ moe_status check_q4(int32_t n, int32_t rows, int32_t cols, int32_t group, int32_
   return MOE_OK;
 }
 
+moe_status check_q8(int32_t n, int32_t rows, int32_t cols, int32_t dtype) {
+  if (dtype != MOE_F32 && dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARGUMENT, "dtype %d", dtype);
+  if (n < 1 || rows < 1 || cols < 1)
+    return fail(MOE_ERR_INVALID_ARGUMENT, "non-positive shape n=%d rows=%d cols=%d", n, rows, cols);
+  if (cols % 128) return fail(MOE_ERR_UNSUPPORTED, "cols=%d must be a multiple of 128", cols);
+  if ((double)n * rows * cols >= (double)((int64_t)1 << 40))
+    return fail(MOE_ERR_UNSUPPORTED, "%d matrices of %d x %d are too many weights", n, rows, cols);
+  return MOE_OK;
+}
+
+// The settings of a call between two blocks; has_y and has_gate: its arguments.
+moe_status check_norm(const moe_desc& d, const moe_norm* n, bool has_y, bool has_gate, bool w_post, bool w_pre) {
+  if (!n) return fail(MOE_ERR_INVALID_ARGUMENT, "norm is NULL");
+  for (int kind : {n->pre, n->post})
+    if (kind != MOE_NORM_NONE && kind != MOE_NORM_RMS && kind != MOE_NORM_LAYER)
+      return fail(MOE_ERR_INVALID_ARGUMENT, "norm kind %d", kind);
+  if (!(n->eps > 0.f) || !std::isfinite(n->eps)) return fail(MOE_ERR_INVALID_ARGUMENT, "eps must be > 0");
+  if (!std::isfinite(n->residual_scale)) return fail(MOE_ERR_INVALID_ARGUMENT, "residual_scale must be finite");
+  if (has_gate && (n->gate_groups < 1 || d.T % n->gate_groups))
+    return fail(MOE_ERR_INVALID_ARGUMENT, "gate_groups=%d must divide T=%d", n->gate_groups, d.T);
+  if (w_post && n->post == MOE_NORM_NONE) return fail(MOE_ERR_INVALID_ARGUMENT, "w_post without a post norm");
+  if (w_pre && n->pre == MOE_NORM_NONE) return fail(MOE_ERR_INVALID_ARGUMENT, "w_pre without a pre norm");
+  if (!has_y && (has_gate || n->post != MOE_NORM_NONE || n->residual_scale != 1.f || n->pre == MOE_NORM_NONE))
+    return fail(MOE_ERR_INVALID_ARGUMENT,
+                "without y there is no post norm and no gate, residual_scale is 1 and there is a pre norm");
+  return MOE_OK;
+}
+
+moe_status check_muon(const moe_muon* o) {
+  if (!o) return fail(MOE_ERR_INVALID_ARGUMENT, "opt is NULL");
+  if (!(o->lr > 0.f) || !std::isfinite(o->lr)) return fail(MOE_ERR_INVALID_ARGUMENT, "lr must be > 0");
+  if (!(o->momentum >= 0.f && o->momentum < 1.f)) return fail(MOE_ERR_INVALID_ARGUMENT, "momentum must lie in [0, 1)");
+  if (!(o->weight_decay >= 0.f) || !std::isfinite(o->weight_decay))
+    return fail(MOE_ERR_INVALID_ARGUMENT, "weight_decay must be >= 0");
+  if (!(o->scale > 0.f) || !std::isfinite(o->scale)) return fail(MOE_ERR_INVALID_ARGUMENT, "scale must be > 0");
+  if (!(o->eps > 0.f) || !std::isfinite(o->eps)) return fail(MOE_ERR_INVALID_ARGUMENT, "eps must be > 0");
+  if ((o->nesterov != 0 && o->nesterov != 1) || (o->precise != 0 && o->precise != 1))
+    return fail(MOE_ERR_INVALID_ARGUMENT, "nesterov and precise must be 0 or 1");
+  if (o->steps < 1 || o->steps > 16) return fail(MOE_ERR_INVALID_ARGUMENT, "steps=%d outside [1, 16]", o->steps);
+  if (!std::isfinite(o->a) || !std::isfinite(o->b) || !std::isfinite(o->c))
+    return fail(MOE_ERR_INVALID_ARGUMENT, "coefficients must be finite");
+  if (!(muon_growth(*o) <= 16.0))
+    return fail(MOE_ERR_UNSUPPORTED, "a singular value can grow to %g in %d steps with these coefficients",
+                muon_growth(*o), o->steps);
+  return MOE_OK;
+}
+
 // Every buffer is read and written in 16-byte vectors.
 #define NEED(p)                                                                         \
   do {                                                                                  \
@@ -207,6 +254,10 @@ size_t moe_workspace_size(const moe_desc* d, int which) {
     case MOE_WS_ROUTE_BWD: return route_bwd_ws_bytes(*d);
     case MOE_WS_FFN_Q4: return ffn_q4_ws_bytes(*d);
     case MOE_WS_FFN_CKPT: return ffn_ckpt_bytes(*d);
+    case MOE_WS_FFN_Q8: return d->dtype == MOE_BF16 ? ffn_q8_ws_bytes(*d) : 0;
+    case MOE_WS_NORM_BWD: return norm_bwd_ws_bytes(*d);
+    case MOE_WS_UPDATE_MUON: return update_muon_ws_bytes(*d, false);
+    case MOE_WS_UPDATE_MUON_PRECISE: return update_muon_ws_bytes(*d, true);
   }
   return 0;
 }
@@ -429,6 +480,103 @@ moe_status moe_expert_update(const moe_desc* d, const moe_opt* opt, void* w_gate
   return hip_status(launch_expert_update(*d, *opt, w_gate, w_up, w_down, dw_gate, dw_up, dw_down, master, m, v,
                                          stream),
                     "moe_expert_update");
+}
+
+moe_status moe_q8_pack(int32_t n, int32_t rows, int32_t cols, int32_t dtype, const void* w, void* codes, void* scales,
+                       hipStream_t stream) {
+  if (moe_status st = check_q8(n, rows, cols, dtype)) return st;
+  NEED(w); NEED(codes); NEED(scales);
+  return hip_status(launch_q8_pack(n, rows, cols, dtype, w, codes, scales, stream), "moe_q8_pack");
+}
+
+moe_status moe_q8_unpack(int32_t n, int32_t rows, int32_t cols, int32_t dtype, const void* codes, const void* scales,
+                         void* w, hipStream_t stream) {
+  if (moe_status st = check_q8(n, rows, cols, dtype)) return st;
+  NEED(codes); NEED(scales); NEED(w);
+  return hip_status(launch_q8_unpack(n, rows, cols, dtype, codes, scales, w, stream), "moe_q8_unpack");
+}
+
+moe_status moe_expert_ffn_q8(const moe_desc* d, const void* x, const void* x_perm, const int32_t* offsets,
+                             const void* gate_codes, const void* gate_scales, const void* up_codes, const void* up_scales,
+                             const void* down_codes, const void* down_scales, void* y_perm, void* ws, size_t ws_bytes,
+                             hipStream_t stream) {
+  moe_status st = check_desc(d);
+  if (st) return st;
+  if (d->dtype != MOE_BF16) return fail(MOE_ERR_UNSUPPORTED, "experts in 8-bit integers are for bf16 layers");
+  if (d->n_shared > 0) NEED(x);
+  NEED(x_perm); NEED(offsets); NEED(gate_codes); NEED(gate_scales); NEED(up_codes); NEED(up_scales);
+  NEED(down_codes); NEED(down_scales); NEED(y_perm);
+  NEED_WS(ws_bytes, ffn_q8_ws_bytes(*d));
+  return hip_status(launch_ffn_q8(*d, x, x_perm, offsets, {gate_codes, gate_scales}, {up_codes, up_scales},
+                                  {down_codes, down_scales}, y_perm, ws, stream),
+                    "moe_expert_ffn_q8");
+}
+
+moe_status moe_residual_norm(const moe_desc* d, const moe_norm* norm, const void* x, const void* y, const void* w_post,
+                             const void* gate, const void* w_pre, void* r, void* h, hipStream_t stream) {
+  moe_status st = check_desc(d);
+  if (st || (st = check_norm(*d, norm, y, gate, w_post, w_pre))) return st;
+  NEED(x);
+  if (y) {
+    NEED(y); NEED(r);
+  } else if (r) {
+    return fail(MOE_ERR_INVALID_ARGUMENT, "without y, r is x and is not written");
+  }
+  if (w_post) NEED(w_post);
+  if (gate) NEED(gate);
+  if (w_pre) NEED(w_pre);
+  if (norm->pre != MOE_NORM_NONE) NEED(h);
+  else if (h) return fail(MOE_ERR_INVALID_ARGUMENT, "h without a pre norm");
+  return hip_status(launch_residual_norm(*d, *norm, x, y, w_post, gate, w_pre, r, h, stream), "moe_residual_norm");
+}
+
+moe_status moe_residual_norm_bwd(const moe_desc* d, const moe_norm* norm, const void* dr, const void* dh, const void* y,
+                                 const void* r, const void* w_post, const void* gate, const void* w_pre, void* dx, void* dy,
+                                 float* dw_post, float* dgate, float* dw_pre, void* ws, size_t ws_bytes,
+                                 hipStream_t stream) {
+  moe_status st = check_desc(d);
+  if (st || (st = check_norm(*d, norm, dy, gate, w_post, w_pre))) return st;
+  const bool pre = norm->pre != MOE_NORM_NONE;
+  if (dr) NEED(dr);
+  else if (!pre) return fail(MOE_ERR_INVALID_ARGUMENT, "neither dr nor a pre norm's dh");
+  if (pre) {
+    NEED(dh); NEED(r);
+  } else if (dh) {
+    return fail(MOE_ERR_INVALID_ARGUMENT, "dh without a pre norm");
+  }
+  if (norm->post != MOE_NORM_NONE || gate || y) {
+    NEED(y); NEED(dy);
+  }
+  NEED(dx);
+  if (dy) NEED(dy);
+  if (w_post) {
+    NEED(w_post); NEED(dw_post);
+  }
+  if (gate) {
+    NEED(gate); NEED(dgate);
+  }
+  if (w_pre) {
+    NEED(w_pre); NEED(dw_pre);
+  }
+  if ((dw_post && !w_post) || (dgate && !gate) || (dw_pre && !w_pre))
+    return fail(MOE_ERR_INVALID_ARGUMENT, "the gradient of a weight or gate that is not there");
+  NEED_WS(ws_bytes, norm_bwd_ws_bytes(*d));
+  return hip_status(launch_residual_norm_bwd(*d, *norm, dr, dh, y, r, w_post, gate, w_pre, dx, dy, dw_post, dgate, dw_pre,
+                                             ws, stream),
+                    "moe_residual_norm_bwd");
+}
+
+moe_status moe_expert_update_muon(const moe_desc* d, const moe_muon* opt, void* w_gate, void* w_up, void* w_down,
+                                  const void* dw_gate, const void* dw_up, const void* dw_down, float* master, float* m,
+                                  void* ws, size_t ws_bytes, hipStream_t stream) {
+  moe_status st = check_desc(d);
+  if (st || (st = check_muon(opt))) return st;
+  NEED(w_gate); NEED(w_up); NEED(w_down); NEED(dw_gate); NEED(dw_up); NEED(dw_down); NEED(m);
+  if (master) NEED(master);
+  NEED_WS(ws_bytes, update_muon_ws_bytes(*d, opt->precise != 0));
+  return hip_status(launch_expert_update_muon(*d, *opt, w_gate, w_up, w_down, dw_gate, dw_up, dw_down, master, m, ws,
+                                              stream),
+                    "moe_expert_update_muon");
 }
 
 moe_status moe_kernel_timing(int enable) {

@@ -1,4 +1,4 @@
-// Launchers of the gated routing, the 4-bit experts and the 8-bit activation checkpoints (private to the library).
+// Launchers of the calls around the layer: gated routing, 4-bit and 8-bit experts, activation checkpoints, norms, updates (private to the library).
 #pragma once
 #include "pcmoe_internal.h"
 #include "../../include/pcmoe_ext.h"
@@ -32,5 +32,31 @@ hipError_t launch_q4_unpack(int n, int rows, int cols, int group, int dtype, con
 hipError_t launch_ffn_q4(const moe_desc& d, int group, const void* x, const void* xp, const int32_t* offsets,
                          const Q4Weights& gate, const Q4Weights& up, const Q4Weights& down, void* yp, void* ws,
                          hipStream_t s);
+
+// 8-bit weights (experts_q8.hip).
+struct Q8Weights {
+  const void* codes;
+  const void* scales;
+};
+size_t ffn_q8_ws_bytes(const moe_desc& d);
+hipError_t launch_q8_pack(int n, int rows, int cols, int dtype, const void* w, void* codes, void* scales, hipStream_t s);
+hipError_t launch_q8_unpack(int n, int rows, int cols, int dtype, const void* codes, const void* scales, void* w,
+                            hipStream_t s);
+hipError_t launch_ffn_q8(const moe_desc& d, const void* x, const void* xp, const int32_t* offsets, const Q8Weights& gate,
+                         const Q8Weights& up, const Q8Weights& down, void* yp, void* ws, hipStream_t s);
+
+// Norms around a block with its gate and residual (norm.hip).
+size_t norm_bwd_ws_bytes(const moe_desc& d);
+hipError_t launch_residual_norm(const moe_desc& d, const moe_norm& n, const void* x, const void* y, const void* w_post,
+                                const void* gate, const void* w_pre, void* r, void* h, hipStream_t s);
+hipError_t launch_residual_norm_bwd(const moe_desc& d, const moe_norm& n, const void* dr, const void* dh, const void* y,
+                                    const void* r, const void* w_post, const void* gate, const void* w_pre, void* dx,
+                                    void* dy, float* dw_post, float* dgate, float* dw_pre, void* ws, hipStream_t s);
+
+// Orthogonalised updates (muon.hip). muon_growth: the largest value that the coefficients let a singular value take.
+size_t update_muon_ws_bytes(const moe_desc& d, bool precise);
+double muon_growth(const moe_muon& o);
+hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void* wg, void* wu, void* wd, const void* gg,
+                                     const void* gu, const void* gd, float* master, float* m, void* ws, hipStream_t s);
 
 }  // namespace pcmoe

@@ -16,7 +16,8 @@ LIB_PATH = os.path.join(HERE, "libpcmoe.so")
 MOE_OK, MOE_ERR_INVALID_ARGUMENT, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE_TOO_SMALL, MOE_ERR_HIP = range(5)
 MOE_F32, MOE_BF16 = 0, 1
 (MOE_WS_PERMUTE, MOE_WS_FFN_SAVED, MOE_WS_FFN_FWD, MOE_WS_FFN_BWD, MOE_WS_ROUTE_BWD, MOE_WS_FFN_Q4,
- MOE_WS_FFN_CKPT) = range(7)
+ MOE_WS_FFN_CKPT, MOE_WS_FFN_Q8, MOE_WS_NORM_BWD, MOE_WS_UPDATE_MUON, MOE_WS_UPDATE_MUON_PRECISE) = range(11)
+MOE_NORM_NONE, MOE_NORM_RMS, MOE_NORM_LAYER = 0, 1, 2
 MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID = 0, 1
 MOE_NO_EXPERT = 0x7fffffff
 
@@ -26,7 +27,8 @@ EXPORTS = ("moe_workspace_size", "moe_route", "moe_permute", "moe_permute_noallo
            "moe_kernel_timing_select", "moe_kernel_timing_report", "moe_status_string", "moe_last_error")
 # ... and include/pcmoe_ext.h
 EXPORTS_EXT = ("moe_route_gated", "moe_route_gated_bwd", "moe_ffn_checkpoint", "moe_ffn_restore", "moe_q4_pack",
-               "moe_q4_unpack", "moe_expert_ffn_q4")
+               "moe_q4_unpack", "moe_expert_ffn_q4", "moe_q8_pack", "moe_q8_unpack", "moe_expert_ffn_q8", "moe_residual_norm",
+               "moe_residual_norm_bwd", "moe_expert_update_muon")
 MOE_OPT_SGD, MOE_OPT_ADAMW = 0, 1
 
 
@@ -57,6 +59,31 @@ def make_gate(score="softmax", n_groups=1, topk_groups=1, group_top=1, scale=1.0
 
 def make_opt(kind="adamw", lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, step=1) -> moe_opt:
     return moe_opt(MOE_OPT_ADAMW if kind == "adamw" else MOE_OPT_SGD, lr, beta1, beta2, eps, weight_decay, step)
+
+
+class moe_norm(ctypes.Structure):
+    _fields_ = [("pre", ctypes.c_int32), ("post", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("residual_scale", ctypes.c_float), ("gate_groups", ctypes.c_int32)]
+
+
+class moe_muon(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float), ("nesterov", ctypes.c_int32),
+                ("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float),
+                ("precise", ctypes.c_int32)]
+
+
+def make_norm(pre="rms", post="none", eps=1e-6, residual_scale=1.0, gate_groups=1) -> moe_norm:
+    kinds = {"none": MOE_NORM_NONE, "rms": MOE_NORM_RMS, "layer": MOE_NORM_LAYER}
+    for kind in (pre, post):
+        if kind not in kinds:
+            raise ValueError(f"norm {kind!r} is not one of {sorted(kinds)}")
+    return moe_norm(kinds[pre], kinds[post], eps, residual_scale, gate_groups)
+
+
+def make_muon(lr=2e-2, momentum=0.95, weight_decay=0.0, scale=1.0, eps=1e-7, nesterov=True, steps=5,
+              coefficients=(3.4445, -4.7750, 2.0315), precise=False) -> moe_muon:
+    return moe_muon(lr, momentum, weight_decay, scale, eps, int(bool(nesterov)), steps, *coefficients, int(bool(precise)))
 
 
 class MoeError(RuntimeError):
@@ -96,6 +123,12 @@ def lib():
             "moe_q4_pack": (_INT, [_I32] * 5 + [_VP] * 4),
             "moe_q4_unpack": (_INT, [_I32] * 5 + [_VP] * 4),
             "moe_expert_ffn_q4": (_INT, [D, _I32] + [_VP] * 11 + [_SZ, _VP]),
+            "moe_q8_pack": (_INT, [_I32] * 4 + [_VP] * 4),
+            "moe_q8_unpack": (_INT, [_I32] * 4 + [_VP] * 4),
+            "moe_expert_ffn_q8": (_INT, [D] + [_VP] * 11 + [_SZ, _VP]),
+            "moe_residual_norm": (_INT, [D, ctypes.POINTER(moe_norm)] + [_VP] * 8),
+            "moe_residual_norm_bwd": (_INT, [D, ctypes.POINTER(moe_norm)] + [_VP] * 13 + [_SZ, _VP]),
+            "moe_expert_update_muon": (_INT, [D, ctypes.POINTER(moe_muon)] + [_VP] * 9 + [_SZ, _VP]),
             "moe_kernel_timing": (_INT, [_INT]),
             "moe_kernel_timing_select": (_INT, [ctypes.c_char_p]),
             "moe_kernel_timing_report": (_SZ, [ctypes.c_char_p, _SZ]),
@@ -264,6 +297,42 @@ def moe_expert_ffn_q4(desc, group, x, x_perm, offsets, gate_codes, gate_scales, 
         ctypes.byref(desc), group, _ptr(x), _ptr(x_perm), _ptr(offsets), _ptr(gate_codes), _ptr(gate_scales),
         _ptr(up_codes), _ptr(up_scales), _ptr(down_codes), _ptr(down_scales), _ptr(y_perm), _ptr(ws), ws_bytes,
         _stream(stream)))
+
+
+def moe_q8_pack(n, rows, cols, dtype, w, codes, scales, stream=None):
+    _check("moe_q8_pack", lib().moe_q8_pack(n, rows, cols, _dtype(dtype), _ptr(w), _ptr(codes), _ptr(scales),
+                                            _stream(stream)))
+
+
+def moe_q8_unpack(n, rows, cols, dtype, codes, scales, w, stream=None):
+    _check("moe_q8_unpack", lib().moe_q8_unpack(n, rows, cols, _dtype(dtype), _ptr(codes), _ptr(scales), _ptr(w),
+                                                _stream(stream)))
+
+
+def moe_expert_ffn_q8(desc, x, x_perm, offsets, gate_codes, gate_scales, up_codes, up_scales, down_codes, down_scales,
+                      y_perm, ws, ws_bytes, stream=None):
+    _check("moe_expert_ffn_q8", lib().moe_expert_ffn_q8(
+        ctypes.byref(desc), _ptr(x), _ptr(x_perm), _ptr(offsets), _ptr(gate_codes), _ptr(gate_scales), _ptr(up_codes),
+        _ptr(up_scales), _ptr(down_codes), _ptr(down_scales), _ptr(y_perm), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_residual_norm(desc, norm, x, y, w_post, gate, w_pre, r, h, stream=None):
+    _check("moe_residual_norm", lib().moe_residual_norm(
+        ctypes.byref(desc), ctypes.byref(norm), _ptr(x), _ptr(y), _ptr(w_post), _ptr(gate), _ptr(w_pre), _ptr(r), _ptr(h),
+        _stream(stream)))
+
+
+def moe_residual_norm_bwd(desc, norm, dr, dh, y, r, w_post, gate, w_pre, dx, dy, dw_post, dgate, dw_pre, ws, ws_bytes,
+                          stream=None):
+    _check("moe_residual_norm_bwd", lib().moe_residual_norm_bwd(
+        ctypes.byref(desc), ctypes.byref(norm), _ptr(dr), _ptr(dh), _ptr(y), _ptr(r), _ptr(w_post), _ptr(gate), _ptr(w_pre),
+        _ptr(dx), _ptr(dy), _ptr(dw_post), _ptr(dgate), _ptr(dw_pre), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def moe_expert_update_muon(desc, opt, w_gate, w_up, w_down, dw_gate, dw_up, dw_down, master, m, ws, ws_bytes, stream=None):
+    _check("moe_expert_update_muon", lib().moe_expert_update_muon(
+        ctypes.byref(desc), ctypes.byref(opt), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(dw_gate), _ptr(dw_up),
+        _ptr(dw_down), _ptr(master), _ptr(m), _ptr(ws), ws_bytes, _stream(stream)))
 
 
 def moe_kernel_timing(enable: bool):

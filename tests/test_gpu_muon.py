@@ -1,0 +1,209 @@
+"""moe_expert_update_muon against 64 bits.
+
+Tolerances are on the 2-norm of an update matrix. With u the relative rounding of X, A and B (2^-11, half a step of fp16;
+2^-21 where each is held in two parts) and products that sum K terms in fp32 (K / 16 + 8 roundings of 2^-24), a step adds
+u |X| to X, and through A and B their errors times what they multiply; a later step passes an error of X on by at most
+slope = max |p'| (or the largest quotient of differences), which a bounds. All of it is formed from the 64-bit run itself."""
+import pytest
+import torch
+
+from paper_2506_02965_amd import pcmoe as P
+
+pytestmark = pytest.mark.gpu
+COEF = (3.4445, -4.7750, 2.0315)
+U32 = 2.0 ** -24
+
+
+def orthogonalise(u, eps, steps, coef, unit):
+    """X after the steps in 64 bits, and a bound of the 2-norm (Frobenius) of what rounding does to it."""
+    a, b, c = coef
+    flip = u.shape[0] > u.shape[1]
+    x = (u.t() if flip else u).contiguous()
+    x = x / (x.norm() + eps)
+    m, n = x.shape
+    # elements below fp16's normal range (2^-14, of numbers scaled to 2^14 at least) are off by 2^-25 of that scale at most
+    tiny = 2.0 ** -39 * (m * n) ** 0.5
+    err = unit * x.norm() + tiny
+    for _ in range(steps):
+        gram = x @ x.t()
+        big = float(torch.linalg.matrix_norm(x, 2))
+        sums_n, sums_m = (n / 16 + 8) * U32, (m / 16 + 8) * U32
+        e_gram = unit * gram.norm() + sums_n * x.norm() ** 2
+        poly = b * gram + c * gram @ gram
+        e_poly = unit * poly.norm() + (abs(b) + 2 * abs(c) * big ** 2) * e_gram + sums_m * abs(c) * gram.norm() ** 2
+        new = a * x + poly @ x
+        slope = max(abs(a), 2.0)
+        err = slope * err + big * e_poly + sums_m * poly.norm() * x.norm() + unit * new.norm() + 4 * U32 * new.norm() + tiny
+        x = new
+    return (x.t() if flip else x), float(err)
+
+
+class Run:
+    def __init__(self, d, f, E, shared=0, dtype="bf16", master=False, seed=0, local=None, **opt):
+        self.G = (E if local is None else local) + shared
+        self.d, self.f, self.dt = d, f, torch.bfloat16 if dtype == "bf16" else torch.float32
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed + d + 31 * f)
+        self.sides = ((f, d), (f, d), (d, f))
+
+        def normal(*s, std=1.0, dtype=None):
+            return (torch.randn(*s, device="cuda", generator=g) * std).to(dtype or self.dt)
+        self.w = [normal(self.G, a, b, std=b ** -0.5) for a, b in self.sides]
+        self.g = [normal(self.G, a, b, std=1e-3) for a, b in self.sides]
+        self.m = normal(3 * self.G * f * d, std=2e-3, dtype=torch.float32)
+        self.master = torch.cat([t.reshape(-1).float() for t in self.w]) + 1e-5 if master else None
+        o = dict(lr=0.02, momentum=0.95, weight_decay=0.1, scale=0.2 * max(d, f) ** 0.5, coefficients=COEF)
+        o.update(opt)
+        self.opt = P.make_muon(**o)
+        self.desc = P.make_desc(1, d, f, max(E, 1), 1, 0, local, shared, dtype=dtype)
+        which = P.MOE_WS_UPDATE_MUON_PRECISE if self.opt.precise else P.MOE_WS_UPDATE_MUON
+        self.ws = torch.empty(P.moe_workspace_size(self.desc, which), dtype=torch.uint8, device="cuda")
+
+    def step(self):
+        P.moe_expert_update_muon(self.desc, self.opt, *self.w, *self.g, self.master, self.m, self.ws, self.ws.numel())
+
+    def state(self):
+        return [t.clone() for t in (*self.w, self.m)] + ([] if self.master is None else [self.master.clone()])
+
+    def check(self):
+        o = self.opt
+        w0, m0 = [t.clone() for t in self.w], self.m.clone()
+        p0 = None if self.master is None else self.master.clone()
+        self.step()
+        n = self.d * self.f
+        unit = 2.0 ** -21 if o.precise else 2.0 ** -11
+        for t in range(3):
+            for i in range(self.G):
+                at = (t * self.G + i) * n
+                shape = self.sides[t]
+                old, g = m0[at:at + n].view(shape).double(), self.g[t][i].double()
+                m = float(o.momentum) * old + g
+                got = self.m[at:at + n].view(shape).double()
+                tol = 2 * U32 * (old.abs() + g.abs())
+                assert ((got - m).abs() <= tol).all()
+                u = g + float(o.momentum) * got if o.nesterov else got
+                x, err = orthogonalise(u, float(o.eps), o.steps, (float(o.a), float(o.b), float(o.c)), unit)
+                err += 4 * U32 * float(x.norm())        # u and its norm
+                p = w0[t][i].double() if p0 is None else p0[at:at + n].view(shape).double()
+                want = p * (1 - float(o.lr) * float(o.weight_decay)) - float(o.lr) * float(o.scale) * x
+                bound = float(o.lr) * float(o.scale) * err + 4 * U32 * float(p.norm() + want.norm())
+                if p0 is not None:
+                    new = self.master[at:at + n].view(shape)
+                    assert float((new.double() - want).norm()) <= bound, (t, i)
+                    assert torch.equal(self.w[t][i], new.to(self.dt))
+                else:
+                    off = float((self.w[t][i].double() - want).norm())
+                    bound += torch.finfo(self.dt).eps / 2 * float(want.norm() + bound)
+                    assert off <= bound, (t, i, off, bound)
+
+
+SIZES = [(128, 128, 1), (128, 384, 2), (384, 128, 1), (256, 640, 3), (640, 256, 1), (512, 512, 2), (1024, 384, 1),
+         (1408, 256, 1)]
+
+
+@pytest.mark.parametrize("precise", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,f,E", SIZES)
+def test_update(d, f, E, dtype, precise):
+    Run(d, f, E, dtype=dtype, precise=precise).check()
+
+
+@pytest.mark.parametrize("opt", [dict(steps=1), dict(steps=2), dict(steps=9), dict(nesterov=False), dict(momentum=0.0),
+                                 dict(weight_decay=0.0), dict(coefficients=(1.5, -0.5, 0.0)), dict(coefficients=(2.0, -1.5, 0.5)),
+                                 dict(coefficients=(1.0, 0.0, 0.0)), dict(eps=0.5)], ids=str)
+@pytest.mark.parametrize("precise", [False, True])
+def test_settings(opt, precise):
+    Run(256, 384, 2, shared=1, precise=precise, **opt).check()
+
+
+@pytest.mark.parametrize("precise", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_master_copy_and_shards(dtype, precise):
+    Run(384, 256, 8, shared=1, local=3, dtype=dtype, master=True, precise=precise).check()
+
+
+def test_larger_matrices():
+    """Several tiles of every size each way, and many matrices in one launch."""
+    Run(1024, 1280, 2, dtype="bf16").check()
+    Run(640, 2176, 1, dtype="f32", precise=True).check()
+    Run(256, 256, 24, dtype="bf16").check()
+
+
+def test_zero_tiny_huge_and_broken_gradients():
+    for precise in (False, True):
+        r = Run(256, 384, 6, precise=precise, dtype="f32")
+        n = r.d * r.f
+        for t in range(3):
+            for i, k in enumerate((0.0, 1e-25, 1e25)):
+                r.g[t][i] *= k
+                r.m[(t * 6 + i) * n:(t * 6 + i + 1) * n] *= k
+            r.g[t][4][3, 5] = float("nan")
+            r.g[t][5][100, 7] = float("inf")
+        before = [w.clone() for w in r.w]
+        r2 = Run(256, 384, 6, precise=precise, dtype="f32")      # the same without the broken ones
+        r.step()
+        r2.step()
+        for t in range(3):
+            keep = before[t][0].double() * (1 - float(r.opt.lr) * float(r.opt.weight_decay))
+            assert ((r.w[t][0].double() - keep).abs() <= 2 * U32 * keep.abs()).all()      # nothing to follow
+            for i in (1, 2):     # the direction does not depend on the size (1e-25: its norm is near eps, 1e25: it is far)
+                assert torch.isfinite(r.w[t][i]).all()
+            gone = 0.02 * float(r.opt.scale)
+            off = (r.w[t][2] - r2.w[t][2]).norm() / gone
+            # both runs round X apart: twice the bound of one
+            _, err = orthogonalise(r2.g[t][2].double() + 0.95 * r2.m[(t * 6 + 2) * n:(t * 6 + 3) * n].view(r.sides[t]).double(),
+                                   1e-7, 5, COEF, 2.0 ** -21 if precise else 2.0 ** -11)
+            assert float(off) <= 2 * err + 1e-5 * float(r2.w[t][2].norm()) / gone
+            assert torch.equal(r.w[t][3], r2.w[t][3])     # no other matrix is touched by a broken one
+            assert torch.isnan(r.w[t][4]).all() and torch.isnan(r.w[t][5]).all()
+
+
+def test_many_steps_make_singular_values_alike():
+    """The definition's purpose: of a full-rank update every singular value ends between 0.6 and 1.25 (the range into which the
+    polynomial takes values of 0.003 and more in five steps)."""
+    r = Run(256, 256, 1, dtype="f32", precise=True, weight_decay=0.0, lr=1.0, scale=1.0)
+    for t in range(3):
+        q, _ = torch.linalg.qr(torch.randn(256, 256, device="cuda", dtype=torch.float64))
+        v, _ = torch.linalg.qr(torch.randn(256, 256, device="cuda", dtype=torch.float64))
+        s = torch.linspace(0.05, 1.0, 256, device="cuda", dtype=torch.float64)
+        r.g[t][0] = (q * s @ v).float()
+    r.m.zero_()
+    before = [w.clone() for w in r.w]
+    r.step()
+    for t in range(3):
+        s = torch.linalg.svdvals((before[t][0] - r.w[t][0]).double())
+        assert 0.6 < float(s.min()) and float(s.max()) < 1.25
+
+
+def test_equal_calls_and_graph_replays():
+    a, b = Run(256, 384, 2, seed=4), Run(256, 384, 2, seed=4)
+    a.step()
+    b.step()
+    assert all(torch.equal(x, y) for x, y in zip(a.state(), b.state()))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        b.step()
+    for k in range(3):
+        for t in range(3):
+            new = torch.randn_like(a.g[t], dtype=torch.float32) * 1e-3
+            a.g[t].copy_(new)
+            b.g[t].copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        a.step()
+        assert all(torch.equal(x, y) for x, y in zip(a.state(), b.state())), k
+
+
+def test_nothing_behind_the_workspace_or_state_is_written():
+    r = Run(128, 256, 2)
+    guard = 4096
+    for name in ("ws", "m"):
+        t = getattr(r, name)
+        pad = guard // t.element_size()
+        whole = torch.full((t.numel() + pad,), 3, dtype=t.dtype, device="cuda")
+        whole[:t.numel()].copy_(t)
+        setattr(r, name + "_whole", whole)
+        setattr(r, name, whole[:t.numel()])
+    r.check()
+    assert (r.ws_whole[r.ws.numel():] == 3).all() and (r.m_whole[r.m.numel():] == 3).all()
