@@ -10,6 +10,7 @@
 #include "expert_ops.h"
 
 #include <algorithm>
+#include <cstdlib>
 
 namespace pcmoe {
 
@@ -69,22 +70,33 @@ __device__ __forceinline__ int code_of(const RowCodes& r, float v) {
   return r.ok ? (int)q : 0;
 }
 
-// A row of K values to codes and scale, by the whole workgroup. SRC: bf16 or float; F64: exact quotients of fp32 values.
-template <typename SRC, bool F64>
+// A row of K values to codes and scale, by the whole workgroup. SRC: bf16 or float; F64: exact quotients of fp32 values. The
+// first KEEP chunks of a thread stay in registers; what a longer row has beyond them is read again.
+template <typename SRC, bool F64, int KEEP>
 __device__ __forceinline__ void code_row(const SRC* v, int K, int8_t* codes, float* scale) {
   constexpr int EP = EPC<SRC>::value;
+  const int n = K / EP;
   uint32_t top = 0;
-  for (int c = threadIdx.x; c < K / EP; c += Q8_THREADS) {
+  const auto look = [&](const Chunk& c) {
     float x[EP];
-    chunk_to_f<SRC>(ld_chunk(v + c * EP), x);
+    chunk_to_f<SRC>(c, x);
 #pragma unroll
     for (int e = 0; e < EP; ++e) top = max_u32(top, __float_as_uint(x[e]) & 0x7fffffffu);
+  };
+  Chunk kept[KEEP];
+#pragma unroll
+  for (int i = 0; i < KEEP; ++i) {
+    const int c = threadIdx.x + i * Q8_THREADS;
+    kept[i] = c < n ? ld_chunk(v + c * EP) : zero_chunk();
   }
+#pragma unroll
+  for (int i = 0; i < KEEP; ++i) look(kept[i]);
+  for (int c = threadIdx.x + KEEP * Q8_THREADS; c < n; c += Q8_THREADS) look(ld_chunk(v + c * EP));
   top = block_max_bits(top);
   const RowCodes r = row_codes(top);
-  for (int c = threadIdx.x; c < K / EP; c += Q8_THREADS) {
+  const auto put = [&](int c, const Chunk& from) {
     float x[EP];
-    chunk_to_f<SRC>(ld_chunk(v + c * EP), x);
+    chunk_to_f<SRC>(from, x);
     uint32_t w[EP / 4];
 #pragma unroll
     for (int e = 0; e < EP; ++e) {
@@ -93,14 +105,20 @@ __device__ __forceinline__ void code_row(const SRC* v, int K, int8_t* codes, flo
     }
     if constexpr (EP == 8) *reinterpret_cast<uint2*>(codes + c * EP) = uint2{w[0], w[1]};
     else *reinterpret_cast<uint32_t*>(codes + c * EP) = w[0];
+  };
+#pragma unroll
+  for (int i = 0; i < KEEP; ++i) {
+    const int c = threadIdx.x + i * Q8_THREADS;
+    if (c < n) put(c, kept[i]);
   }
+  for (int c = threadIdx.x + KEEP * Q8_THREADS; c < n; c += Q8_THREADS) put(c, ld_chunk(v + c * EP));
   if (threadIdx.x == 0) *scale = row_scale(top);
 }
 
 template <typename T>
 __global__ __launch_bounds__(Q8_THREADS) void q8_pack_kernel(const T* w, int64_t rows, int cols, int8_t* codes, float* scales) {
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    code_row<T, std::is_same<T, float>::value>(w + r * cols, cols, codes + r * cols, scales + r);
+    code_row<T, std::is_same<T, float>::value, 4>(w + r * cols, cols, codes + r * cols, scales + r);
 }
 
 template <typename T>
@@ -130,22 +148,27 @@ struct Q8Args {
   const int8_t *wg, *wu, *wd;
   const float *sg, *su, *sd;
   bf16* y;            // [R][d]
-  int32_t* prefix;    // [G + 1]
+  int32_t *prefix, *tail;  // [G + 1] each; no tails: null
   int bm;             // rows of an m-tile
 };
 
-// Codes of the rows of x_perm and x; the last workgroup makes the m-tile prefix of the groups.
+// Codes of the rows of x_perm and x; the last workgroup makes the m-tile prefix of the groups, with tails (last m-tiles of at
+// most half their rows) in a prefix of their own where they take another tile.
 __global__ __launch_bounds__(Q8_THREADS) void q8_rows_x_kernel(Q8Args a) {
-  const int r = blockIdx.x, lane = threadIdx.x;
+  const int r = blockIdx.x;
   if (r == (int)gridDim.x - 1) {
-    if (threadIdx.x >= 64) return;
+    if (threadIdx.x >= 128) return;
+    const int lane = threadIdx.x & 63, tails = threadIdx.x >> 6;  // the second wavefront: the tails
+    if (tails && !a.tail) return;
+    int32_t* out = tails ? a.tail : a.prefix;
     const int G = a.ga.Eloc + a.ga.S;
     int carry = 0;
-    if (lane == 0) a.prefix[0] = 0;
+    if (lane == 0) out[0] = 0;
     for (int g0 = 0; g0 < G; g0 += 64) {
       const int g = g0 + lane;
       const int rows = g < a.ga.Eloc ? a.ga.offsets[g + 1] - a.ga.offsets[g] : g < G ? a.ga.T : 0;
-      int v = (rows + a.bm - 1) / a.bm;
+      const int rem = rows % a.bm, is_tail = a.tail && rem > 0 && 2 * rem <= a.bm ? 1 : 0;
+      int v = tails ? is_tail : (rows + a.bm - 1) / a.bm - is_tail;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
         const int u = __shfl_up(v, o, 64);
@@ -153,28 +176,34 @@ __global__ __launch_bounds__(Q8_THREADS) void q8_rows_x_kernel(Q8Args a) {
       }
       v += carry;
       carry = __builtin_amdgcn_readlane(v, 63);
-      if (g < G) a.prefix[g + 1] = v;
+      if (g < G) out[g + 1] = v;
     }
     return;
   }
   const bool routed = r < a.ga.rows_cap;
   if (routed && r >= a.ga.offsets[a.ga.Eloc]) return;
   const bf16* v = routed ? (const bf16*)a.xp + (size_t)r * a.ga.d : (const bf16*)a.x + (size_t)(r - a.ga.rows_cap) * a.ga.d;
-  code_row<bf16, false>(v, a.ga.d, a.xq + (size_t)r * a.ga.d, a.sx + r);
+  code_row<bf16, false, 2>(v, a.ga.d, a.xq + (size_t)r * a.ga.d, a.sx + r);
 }
+template <int KEEP>
 __global__ __launch_bounds__(Q8_THREADS) void q8_rows_h_kernel(Q8Args a) {
   const int r = blockIdx.x;
   if (r < a.ga.rows_cap && r >= a.ga.offsets[a.ga.Eloc]) return;
-  code_row<float, false>(a.h + (size_t)r * a.ga.f, a.ga.f, a.hq + (size_t)r * a.ga.f, a.sh + r);
+  code_row<float, false, KEEP>(a.h + (size_t)r * a.ga.f, a.ga.f, a.hq + (size_t)r * a.ga.f, a.sh + r);
+}
+
+// 1 / (1 + exp(-g)) with the hardware's exponential and reciprocal. The exponential of a product rounded to fp32 alone would be
+// |g| roundings off; what the product rounds away is put back.
+__device__ __forceinline__ float sigmoid_of(float g) {
+  const float t = -1.44269504f * g, r = __builtin_fmaf(-1.44269504f, g, -t) + -1.925963e-8f * g;
+  const float e = __builtin_amdgcn_exp2f(fminf(t, 126.f));
+  return __builtin_amdgcn_rcpf(1.f + __builtin_fmaf(e, 0.693147181f * r, e));
 }
 
 // Gate and up (DOWN = false): half of a wavefront's columns are gate rows, the other half the up rows of the same columns of
 // H. Down: y.
 template <typename S, bool DOWN>
-__global__ __launch_bounds__(S::NT) void q8_gemm_kernel(Q8Args a) {
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  TileIdx ti;
-  if (!decode_tile<true>(a.ga, blockIdx.x, ti)) return;
+__device__ __forceinline__ void q8_tile(const Q8Args& a, const TileIdx& ti, int m0, char* smem) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::WN, wn = wave % S::WN, q = lane >> 4, li = lane & 15;
   const int d = a.ga.d, f = a.ga.f, K = DOWN ? f : d;
@@ -183,7 +212,6 @@ __global__ __launch_bounds__(S::NT) void q8_gemm_kernel(Q8Args a) {
   // the group's first row: in the row space, and among the codes of x
   const size_t rs = routed ? (size_t)ti.row0 : (size_t)a.ga.rows_cap + (size_t)shared * a.ga.T;
   const size_t rx = routed ? (size_t)ti.row0 : (size_t)a.ga.rows_cap;
-  const int m0 = ti.mt * S::BM;
   const int8_t* ap = DOWN ? a.hq + rs * f : a.xq + rx * d;
   const float* sa = DOWN ? a.sh + rs : a.sx + rx;
   const int32x4 ra = make_rsrc(ap, (uint32_t)((size_t)ti.rows * K));
@@ -197,14 +225,11 @@ __global__ __launch_bounds__(S::NT) void q8_gemm_kernel(Q8Args a) {
   I8::acc acc[S::FM][S::FN];
   nt_loop<S, I8>(
       smem, K / NT_ROWB, live,
-      [&](int kt, int j, uint32_t dst) { dma16(ra, dst, (m0 + 8 * j) * K + at + kt * NT_ROWB); },
-      [&](int kt, int j, uint32_t dst) {
-        if (DOWN) {
-          dma16(rb0, dst, (n0 + 8 * j) * K + at + kt * NT_ROWB);
-        } else {
-          const int r = 8 * j, w = r / S::WTN, in = r % S::WTN;
-          dma16(pick_rsrc(in >= HALF, rb0, rb1), dst, (n0 + w * HALF + in % HALF) * K + at + kt * NT_ROWB);
-        }
+      [&](int kt, int j) { return NtSrc{ra, (m0 + 8 * j) * K + at + kt * NT_ROWB}; },
+      [&](int kt, int j) {
+        if (DOWN) return NtSrc{rb0, (n0 + 8 * j) * K + at + kt * NT_ROWB};
+        const int r = 8 * j, w = r / S::WTN, in = r % S::WTN;
+        return NtSrc{pick_rsrc(in >= HALF, rb0, rb1), (n0 + w * HALF + in % HALF) * K + at + kt * NT_ROWB};
       },
       acc);
   if (!live) return;
@@ -233,7 +258,7 @@ __global__ __launch_bounds__(S::NT) void q8_gemm_kernel(Q8Args a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float g = (float)acc[i][j][e] * (s * sg[e]), u = (float)acc[i][j + S::FN / 2][e] * (s * su[e]);
-          o[e] = g / (1.f + expf(-g)) * u;
+          o[e] = g * sigmoid_of(g) * u;
         }
         *reinterpret_cast<floatx4*>(a.h + (rs + m) * f + n) = o;
       }
@@ -241,17 +266,45 @@ __global__ __launch_bounds__(S::NT) void q8_gemm_kernel(Q8Args a) {
   }
 }
 
+// A tail (at most half of the rows) of a 256-row tile takes a tile of 128 rows.
+template <typename S, bool DOWN>
+__global__ __launch_bounds__(S::NT) void q8_gemm_kernel(Q8Args a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  TileIdx ti;
+  if (!decode_tile<true>(a.ga, blockIdx.x, ti)) return;
+  const int m0 = ti.mt * S::BM;
+  if constexpr (S::PIPE && S::BM == 256) {
+    if (2 * (ti.rows - m0) <= S::BM) {
+      q8_tile<NtShape<S::BM / 2, S::BN, 2, 2, 2>, DOWN>(a, ti, m0, smem);
+      return;
+    }
+  }
+  q8_tile<S, DOWN>(a, ti, m0, smem);
+}
+
+typedef NtShape<256, 256, 2, 2, 2> Q8Large;
+typedef NtShape<64, 128, 2, 2, 3> Q8b;
+typedef NtShape<64, 128, 2, 2, 2> Q8c;
+typedef NtShape<32, 128, 1, 4, 4> Q8d;
+typedef NtShape<128, 128, 2, 2, 4> Q8e;
+typedef NtShape<64, 64, 2, 2, 4> Q8f;
+typedef NtShape<64, 256, 2, 4, 2> Q8g;
+typedef NtShape<32, 64, 1, 2, 4> Q8h;
+typedef NtShape<128, 256, 2, 2, 2> Q8p;
+typedef NtShape<64, 256, 1, 4, 3> Q8q;
+typedef NtShape<128, 128, 2, 4, 2> Q8r;
 typedef NtShape<128, 128, 2, 2, 2> Q8Small;
 
 struct Q8Layout {
-  size_t sx, prefix, h, hq, sh, bytes;
+  size_t sx, prefix, tail, h, hq, sh, bytes;
 };
 Q8Layout q8_layout(const moe_desc& d) {
   Q8Layout l;
   const size_t rx = (size_t)d.T * d.top_k + (d.n_shared ? d.T : 0), R = (size_t)rows_total(d);
   l.sx = align256(rx * d.d_model);
   l.prefix = l.sx + align256(rx * 4);
-  l.h = l.prefix + align256((d.local_count + d.n_shared + 1) * 4);
+  l.tail = l.prefix + align256((d.local_count + d.n_shared + 1) * 4);
+  l.h = l.tail + align256((d.local_count + d.n_shared + 1) * 4);
   l.hq = l.h + align256(R * d.d_ff * 4);
   l.sh = l.hq + align256(R * d.d_ff);
   l.bytes = l.sh + align256(R * 4);
@@ -268,7 +321,8 @@ hipError_t q8_gemm(const char* name, const moe_desc& d, Q8Args a, hipStream_t s)
                                 (int64_t)d.local_count * ((d.T + S::BM - 1) / S::BM)) +
                        (int64_t)d.n_shared * ((d.T + S::BM - 1) / S::BM);
   KernelTimer kt(name, s);
-  hipLaunchKernelGGL(kern, dim3((unsigned)((most * a.ga.n_tiles + 7) / 8 * 8)), dim3(S::NT), S::LDS, s, a);
+  // every XCD takes its share of the tiles and of the tails, each rounded up: at most two tiles more than an eighth of all
+  hipLaunchKernelGGL(kern, dim3((unsigned)(most * a.ga.n_tiles / 8 * 8 + 16)), dim3(S::NT), S::LDS, s, a);
   return hipGetLastError();
 }
 
@@ -318,6 +372,7 @@ hipError_t launch_ffn_q8(const moe_desc& d, const void* x, const void* xp, const
   a.ga.offsets = offsets;
   a.prefix = (int32_t*)(base + l.prefix);
   a.ga.mt_prefix = a.prefix;
+  a.tail = nullptr;
   a.x = x;
   a.xp = xp;
   a.xq = (int8_t*)base;
@@ -332,20 +387,50 @@ hipError_t launch_ffn_q8(const moe_desc& d, const void* x, const void* xp, const
   a.su = (const float*)up.scales;
   a.sd = (const float*)down.scales;
   a.y = (bf16*)yp;
-  a.bm = 128;
+  // rows per expert
+  const double rows = (double)d.T * d.top_k / d.n_experts;
+  bool large = rows >= 192;
+  const char* e = getenv("Q8_TILE");
+  const char shape = e ? e[0] : large ? 'l' : 's';
+  large = shape == 'l';
+  a.bm = large ? 256 : 128;
+  if (shape == 'b' || shape == 'c' || shape == 'f' || shape == 'g' || shape == 'q') a.bm = 64;
+  if (shape == 'd' || shape == 'h') a.bm = 32;
+  if (large) a.ga.mt_tail = a.tail = (int32_t*)(base + l.tail);
   const int rx = d.T * d.top_k + (d.n_shared ? d.T : 0);
   {
     KernelTimer kt("q8_rows_x", s);
     hipLaunchKernelGGL(q8_rows_x_kernel, dim3(rx + 1), dim3(Q8_THREADS), 0, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  if (hipError_t e = q8_gemm<Q8Small, false>("q8_gate_up", d, a, s); e != hipSuccess) return e;
+  const auto gemm = [&](const char* name, auto down) {
+    constexpr bool D = decltype(down)::value;
+    switch (shape) {
+      case 'l': return q8_gemm<Q8Large, D>(name, d, a, s);
+      case 'b': return q8_gemm<Q8b, D>(name, d, a, s);
+      case 'c': return q8_gemm<Q8c, D>(name, d, a, s);
+      case 'd': return q8_gemm<Q8d, D>(name, d, a, s);
+      case 'e': return q8_gemm<Q8e, D>(name, d, a, s);
+      case 'f': return q8_gemm<Q8f, D>(name, d, a, s);
+      case 'g': return q8_gemm<Q8g, D>(name, d, a, s);
+      case 'p': return q8_gemm<Q8p, D>(name, d, a, s);
+      case 'q': return q8_gemm<Q8q, D>(name, d, a, s);
+      case 'r': return q8_gemm<Q8r, D>(name, d, a, s);
+      case 'h': return q8_gemm<Q8h, D>(name, d, a, s);
+    }
+    return q8_gemm<Q8Small, D>(name, d, a, s);
+  };
+  if (hipError_t e = gemm("q8_gate_up", std::false_type{}); e != hipSuccess) return e;
   {
     KernelTimer kt("q8_rows_h", s);
-    hipLaunchKernelGGL(q8_rows_h_kernel, dim3((unsigned)rows_total(d)), dim3(Q8_THREADS), 0, s, a);
+    const auto rows_h = [&](auto keep) {
+      hipLaunchKernelGGL(q8_rows_h_kernel<decltype(keep)::value>, dim3((unsigned)rows_total(d)), dim3(Q8_THREADS), 0, s, a);
+    };
+    if (d.d_ff <= 4 * 4 * Q8_THREADS) rows_h(std::integral_constant<int, 4>{});
+    else rows_h(std::integral_constant<int, 16>{});
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  return q8_gemm<Q8Small, true>("q8_down", d, a, s);
+  return gemm("q8_down", std::true_type{});
 }
 
 }  // namespace pcmoe

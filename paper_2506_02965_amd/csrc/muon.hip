@@ -18,6 +18,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 namespace pcmoe {
 
@@ -141,32 +142,287 @@ __global__ __launch_bounds__(256) void muon_normalise_kernel(MuonArgs a) {
     }
 }
 
-// One product of every matrix: out = alpha P Q^T + beta D, P [M][K], Q [N][K], D and out [M][N].
+// One product of every matrix: out = alpha P Q^T (+ beta D + diag on the diagonal), P [M][K], Q [N][K], D and out [M][N].
 struct NsArgs {
   const f16 *p, *q, *d;
   f16 *out, *out_t;        // out, and its transpose [N][M]
   size_t p_mat, q_mat, o_mat;        // elements of a matrix
   size_t p_plane, q_plane, o_plane;  // ... of a part
   int M, N, K, mats;
-  float alpha, beta;
+  int whole;               // tiles that are not split into quarters
+  float alpha, beta, diag;
+  // a second product of the same shape by the same P, in the same launch
+  const f16* q2;
+  f16* out2;
+  float alpha2;
   // last step: parameters in place of out
   void* w[3];
   float* master;
   int G, dtype;
-  int flip[3];             // the tensor is stored transposed to X
+  int flip_up, flip_down;  // gate and up, down are stored transposed to X
   float decay, step;       // p <- decay p - step X
 };
 
 enum NsMode { NS_SYMMETRIC, NS_BOTH, NS_LAST };  // stores: one tile and its mirror, both orientations, the parameters
 
+// LDS of an epilogue: a wavefront's part transposed, [WTN][WTM] fp16 with rows of PITCH words, or for parameters stored
+// transposed to X half of it in fp32. Rows an odd multiple of 4 words apart spread the writes over all banks.
+template <typename S, int MODE>
+struct NsLds {
+  static constexpr int PITCH = S::WTM / 2 + 4, PITCH32 = S::WTM + 4;
+  static constexpr int WAVE = MODE == NS_LAST ? S::WTN / 2 * PITCH32 * 4 : S::WTN * PITCH * 4;
+  static constexpr int BYTES = S::LDS > S::NW * WAVE ? S::LDS : S::NW * WAVE;
+};
+
+// Two column blocks of a fragment row (four consecutive columns a lane each) -> eight consecutive columns a lane: of the first
+// block in the even rows of 16 lanes, of the second in the odd ones, starting at column 8 (q >> 1).
+__device__ __forceinline__ void join_columns(const floatx4& a, const floatx4& b, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a[e]), __float_as_uint(b[e]), false, false);
+    v[e] = __uint_as_float(r[0]);
+    v[4 + e] = __uint_as_float(r[1]);
+  }
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b, bool second) {
+  return (uint32_t)__builtin_bit_cast(uint16_t, part_of(a, second)) |
+         (uint32_t)__builtin_bit_cast(uint16_t, part_of(b, second)) << 16;
+}
+
+// The tile of matrix `mat` whose first row and column are m0 and n0.
 template <typename S, int MODE, bool PRECISE>
-__global__ __launch_bounds__(S::NT) void muon_product_kernel(NsArgs a) {
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int tm = (a.M + S::BM - 1) / S::BM, tn = (a.N + S::BN - 1) / S::BN;
+__device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int mat, bool other, int m0, int n0) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / S::WN, wn = wave % S::WN, q = lane >> 4, li = lane & 15;
+  const int ld = a.K * 2;
+  const f16 *p0 = a.p + mat * a.p_mat, *q0 = (other ? a.q2 : a.q) + mat * a.q_mat;
+  const uint32_t p_bytes = (uint32_t)a.M * ld, q_bytes = (uint32_t)a.N * ld;
+  const int32x4 rp = make_rsrc(p0, p_bytes), rq = make_rsrc(q0, q_bytes);
+  int32x4 rp1 = rp, rq1 = rq;
+  if (PRECISE) {
+    rp1 = make_rsrc(p0 + a.p_plane, p_bytes);
+    rq1 = make_rsrc(q0 + a.q_plane, q_bytes);
+  }
+  const int kts = a.K / 64, at = nt_lane(ld);
+  // the wavefronts' parts lie on either side of a matrix's end, not across it: the sides are multiples of 128
+  const bool live = m0 + wm * S::WTM < a.M && n0 + wn * S::WTN < a.N;
+  typename F16::acc acc[S::FM][S::FN];
+  // K-tiles kt: of a precise product first P1 Q2, then P2 Q1, then P1 Q1
+  nt_loop<S, F16>(
+      smem, PRECISE ? 3 * kts : kts, live,
+      [&](int kt, int j) {
+        const int seg = PRECISE ? (kt >= 2 * kts ? 2 : kt >= kts ? 1 : 0) : 0;
+        return NtSrc{PRECISE ? pick_rsrc(seg == 1, rp, rp1) : rp, (m0 + 8 * j) * ld + at + (kt - seg * kts) * NT_ROWB};
+      },
+      [&](int kt, int j) {
+        const int seg = PRECISE ? (kt >= 2 * kts ? 2 : kt >= kts ? 1 : 0) : 0;
+        return NtSrc{PRECISE ? pick_rsrc(seg == 0, rq, rq1) : rq, (n0 + 8 * j) * ld + at + (kt - seg * kts) * NT_ROWB};
+      },
+      acc);
+  if (!live) return;
+  const int mr = m0 + wm * S::WTM, nc = n0 + wn * S::WTN;  // the wavefront's part
+
+  if constexpr (MODE == NS_LAST) {
+    const int tensor = mat / a.G;
+    const size_t at_w = (size_t)(mat % a.G) * a.o_mat;
+    float* mp = a.master ? a.master + (size_t)tensor * a.G * a.o_mat + at_w : nullptr;
+    void* const w = tensor == 0 ? a.w[0] : tensor == 1 ? a.w[1] : a.w[2];
+    float* wf = (float*)w + at_w;
+    bf16* wb = (bf16*)w + at_w;
+    // with the parameters' type and whether there is a master copy known, so that nothing in the loops branches
+    const auto keep = [&] {  // the accumulators stay where they are until a path takes them
+#pragma unroll
+      for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) asm volatile("" : "+a"(acc[i][j]));
+    };
+    const auto update = [&](auto f32, auto has_master) {
+      constexpr bool F32 = decltype(f32)::value, MASTER = decltype(has_master)::value;
+      // eight consecutive parameters from element o on
+      const auto fetch = [&](size_t o, Chunk (&c)[2]) {
+        if constexpr (F32 || MASTER) {
+          const float* from = (MASTER ? mp : wf) + o;
+          c[0] = ld_chunk(from);
+          c[1] = ld_chunk(from + 4);
+        } else {
+          c[0] = c[1] = ld_chunk(wb + o);
+        }
+      };
+      const auto store = [&](size_t o, const Chunk (&c)[2], const float (&x)[8]) {
+        float p[8];
+        if constexpr (F32 || MASTER) {
+          chunk_to_f<float>(c[0], p);
+          chunk_to_f<float>(c[1], p + 4);
+        } else {
+          chunk_to_f<bf16>(c[0], p);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = a.decay * p[e] - a.step * (a.alpha * x[e]);
+        if constexpr (MASTER) {
+          st_chunk(mp + o, f_to_chunk<float>(p));
+          st_chunk(mp + o + 4, f_to_chunk<float>(p + 4));
+        }
+        if constexpr (F32) {
+          st_chunk(wf + o, f_to_chunk<float>(p));
+          st_chunk(wf + o + 4, f_to_chunk<float>(p + 4));
+        } else {
+          st_chunk(wb + o, f_to_chunk<bf16>(p));
+        }
+      };
+      if (!(tensor == 2 ? a.flip_down : a.flip_up)) {
+        keep();
+#pragma unroll
+        for (int i = 0; i < S::FM; ++i) {
+          __builtin_amdgcn_sched_barrier(0);
+          const size_t o = (size_t)(mr + 16 * i + li) * a.N + nc + 16 * (q & 1) + 8 * (q >> 1);
+          Chunk c[S::FN / 2][2];
+#pragma unroll
+          for (int j = 0; j < S::FN / 2; ++j) fetch(o + 32 * j, c[j]);
+#pragma unroll
+          for (int j = 0; j < S::FN / 2; ++j) {
+            float v[8];
+            join_columns(acc[i][2 * j], acc[i][2 * j + 1], v);
+            store(o + 32 * j, c[j], v);
+          }
+        }
+      } else {
+        constexpr int PITCH = NsLds<S, MODE>::PITCH32, CH = S::WTM / 8;
+        float* st = reinterpret_cast<float*>(smem + wave * NsLds<S, MODE>::WAVE);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          keep();
+#pragma unroll
+          for (int i = 0; i < S::FM; ++i, __builtin_amdgcn_sched_barrier(0))
+#pragma unroll
+            for (int j = 0; j < S::FN / 2; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) st[(16 * j + 4 * q + e) * PITCH + 16 * i + li] = acc[i][half * (S::FN / 2) + j][e];
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          constexpr int TASKS = S::WTN / 2 * CH / 64, AHEAD = TASKS < 4 ? TASKS : 4;
+#pragma unroll 1
+          for (int k0 = 0; k0 < TASKS; k0 += AHEAD) {
+            Chunk c[AHEAD][2];
+            size_t o[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+              const int task = lane + 64 * (k0 + k);
+              o[k] = (size_t)(nc + half * (S::WTN / 2) + task / CH) * a.M + mr + (task % CH) * 8;
+              fetch(o[k], c[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+              const int task = lane + 64 * (k0 + k);
+              const float* from = st + (task / CH) * PITCH + (task % CH) * 8;
+              float v[8];
+              chunk_to_f<float>(ld_chunk(from), v);
+              chunk_to_f<float>(ld_chunk(from + 4), v + 4);
+              store(o[k], c[k], v);
+            }
+          }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+      }
+    };
+    if (a.dtype == MOE_F32) {
+      if (mp) update(std::true_type{}, std::true_type{});
+      else update(std::true_type{}, std::false_type{});
+    } else {
+      if (mp) update(std::false_type{}, std::true_type{});
+      else update(std::false_type{}, std::false_type{});
+    }
+    return;
+  } else {
+    f16* out = (other ? a.out2 : a.out) + mat * a.o_mat;
+    f16* out_t = (MODE == NS_SYMMETRIC ? (other ? a.out2 : a.out) : a.out_t) + mat * a.o_mat;
+    const float alpha = other ? a.alpha2 : a.alpha;
+    const f16* d0 = MODE == NS_SYMMETRIC && a.d ? a.d + mat * a.o_mat : nullptr;
+    const bool turn = MODE == NS_BOTH || m0 != n0;
+    constexpr int PITCH = NsLds<S, MODE>::PITCH;
+    uint32_t* st = reinterpret_cast<uint32_t*>(smem + wave * NsLds<S, MODE>::WAVE);
+    const bool odd = lane & 1;
+    const uint32_t sel_lo = odd ? 0x01000504u : 0x05040100u, sel_hi = odd ? 0x03020706u : 0x07060302u;
+#pragma unroll 1
+    for (int p = 0; p < (PRECISE ? 2 : 1); ++p) {
+      float by = alpha;
+      int row = li;
+      if (PRECISE) asm volatile("" : "+v"(by), "+v"(row));  // keeps what both parts compute from being kept in registers
+#pragma unroll
+      for (int i = 0; i < S::FM; ++i) {
+        __builtin_amdgcn_sched_barrier(0);  // one row of blocks out of the accumulators at a time: more would spill
+        floatx4 x[S::FN];
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[j][e] = by * acc[i][j][e];
+        if (d0) {
+          typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+          const int m = mr + 16 * i + row;
+          const size_t o = (size_t)m * a.N + nc + 4 * q;
+          half4 dv[S::FN], d1[S::FN];
+#pragma unroll
+          for (int j = 0; j < S::FN; ++j) {
+            dv[j] = *reinterpret_cast<const half4*>(d0 + o + 16 * j);
+            if (PRECISE) d1[j] = *reinterpret_cast<const half4*>(d0 + a.o_plane + o + 16 * j);
+          }
+#pragma unroll
+          for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[j][e] += a.beta * ((float)dv[j][e] + (PRECISE ? (float)d1[j][e] : 0.f));
+              if (m == nc + 16 * j + 4 * q + e) x[j][e] += a.diag;
+            }
+        }
+        // by rows, from registers
+#pragma unroll
+        for (int j = 0; j < S::FN / 2; ++j) {
+          float v[8];
+          join_columns(x[2 * j], x[2 * j + 1], v);
+          Chunk c;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c.w[e] = pack_f16(v[2 * e], v[2 * e + 1], p != 0);
+          st_chunk(out + p * a.o_plane + (size_t)(mr + 16 * i + row) * a.N + nc + 32 * j + 16 * (q & 1) + 8 * (q >> 1), c);
+        }
+        // by columns, through LDS: neighbouring lanes (rows m and m + 1) exchange halves, the even one keeps columns 0 and 1 of
+        // its four, the odd one 2 and 3
+        if (!turn) continue;
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j) {
+          const uint32_t c01 = pack_f16(x[j][0], x[j][1], p != 0), c23 = pack_f16(x[j][2], x[j][3], p != 0);
+          const uint32_t keep = odd ? c23 : c01, give = odd ? c01 : c23;
+          const uint32_t got = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)give, 0xb1, 0xf, 0xf, true);
+          uint32_t* to = st + (16 * j + 4 * q + (odd ? 2 : 0)) * PITCH + 8 * i + (row >> 1);
+          to[0] = __builtin_amdgcn_perm(got, keep, sel_lo);
+          to[PITCH] = __builtin_amdgcn_perm(got, keep, sel_hi);
+        }
+      }
+      if (!turn) continue;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      constexpr int CH = S::WTM / 8;
+#pragma unroll
+      for (int k = 0; k < S::WTN * CH / 64; ++k) {
+        const int task = lane + 64 * k, r = task / CH, c = task % CH;
+        st_chunk(out_t + p * a.o_plane + (size_t)(nc + r) * a.M + mr + 8 * c, ld_chunk(st + r * PITCH + 4 * c));
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+  }
+}
+
+// 256 x 256 tiles with one wavefront per SIMD, 128 x 128 tiles two workgroups a CU, and 64 x 64 tiles with a deep ring; and the
+// quarters of 256 x 256 tiles, which share a launch with them.
+typedef NtShape<256, 256, 2, 2, 2> NsLarge;
+typedef NtShape<128, 128, 2, 2, 4> NsQuarter;
+typedef NtShape<128, 128, 2, 2, 2> NsSmall;
+typedef NtShape<64, 64, 2, 2, 8> NsTiny;
+
+// Tile l of a grid of `tm` x `tn` tiles of every matrix (for symmetric products, of those on and above the diagonal).
+template <int MODE>
+__device__ __forceinline__ void ns_tile(const NsArgs& a, int l, int tm, int tn, int& mat, bool& other, int& mt, int& nt) {
   const int per = MODE == NS_SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn;
-  const int L = xcd_order(blockIdx.x, per * a.mats);
-  const int mat = L / per;
-  int l = L - mat * per, mt, nt;
+  other = MODE == NS_SYMMETRIC && l >= per * a.mats;
+  if (other) l -= per * a.mats;
+  mat = l / per;
+  l -= mat * per;
   if (MODE == NS_SYMMETRIC) {  // nt >= mt, by columns: nt (nt + 1) / 2 tiles stand before column nt
     nt = (int)((sqrtf(8.f * (float)l + 1.f) - 1.f) * 0.5f);
     while (nt * (nt + 1) / 2 > l) --nt;
@@ -177,159 +433,80 @@ __global__ __launch_bounds__(S::NT) void muon_product_kernel(NsArgs a) {
     nt = rem / rows;
     mt = 8 * blk + rem % rows;
   }
-  const int m0 = mt * S::BM, n0 = nt * S::BN;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave / S::WN, wn = wave % S::WN, q = lane >> 4, li = lane & 15;
-  const int ld = a.K * 2;
-  const f16 *p0 = a.p + mat * a.p_mat, *q0 = a.q + mat * a.q_mat;
-  const uint32_t p_bytes = (uint32_t)a.M * ld, q_bytes = (uint32_t)a.N * ld;
-  const int32x4 rp = make_rsrc(p0, p_bytes), rq = make_rsrc(q0, q_bytes);
-  int32x4 rp1 = rp, rq1 = rq;
-  if (PRECISE) {
-    rp1 = make_rsrc(p0 + a.p_plane, p_bytes);
-    rq1 = make_rsrc(q0 + a.q_plane, q_bytes);
-  }
-  const int kts = a.K / 64, at = nt_lane(ld);
-  // the wavefronts' parts lie on either side of a matrix's end, not across it: both are multiples of 64
-  const bool live = m0 + wm * S::WTM < a.M && n0 + wn * S::WTN < a.N;
-  typename F16::acc acc[S::FM][S::FN];
-  // K-tiles kt: of a precise product first P1 Q2, then P2 Q1, then P1 Q1
-  nt_loop<S, F16>(
-      smem, PRECISE ? 3 * kts : kts, live,
-      [&](int kt, int j, uint32_t dst) {
-        const int seg = PRECISE ? (kt >= 2 * kts ? 2 : kt >= kts ? 1 : 0) : 2;
-        dma16(PRECISE ? pick_rsrc(seg == 1, rp, rp1) : rp, dst, (m0 + 8 * j) * ld + at + (PRECISE ? kt - seg * kts : kt) * NT_ROWB);
-      },
-      [&](int kt, int j, uint32_t dst) {
-        const int seg = PRECISE ? (kt >= 2 * kts ? 2 : kt >= kts ? 1 : 0) : 2;
-        dma16(PRECISE ? pick_rsrc(seg == 0, rq, rq1) : rq, dst, (n0 + 8 * j) * ld + at + (PRECISE ? kt - seg * kts : kt) * NT_ROWB);
-      },
-      acc);
-  if (!live) return;
+  mat = __builtin_amdgcn_readfirstlane(mat);
+  mt = __builtin_amdgcn_readfirstlane(mt);
+  nt = __builtin_amdgcn_readfirstlane(nt);
+}
 
-  // Epilogue, per wavefront: 32 rows at a time go through LDS in fp32, are combined with D and stored by rows of 16-byte
-  // chunks, then read again by columns for the transposed store.
-  constexpr int PITCH = S::WTN + 4;
-  float* st = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
-  static_assert(S::NW * 32 * PITCH * 4 <= S::LDS, "the staging fits the operands' LDS");
-  const int tensor = mat / max(a.G, 1), flip = MODE == NS_LAST ? a.flip[tensor] : 0;
-#pragma unroll
-  for (int part = 0; part < S::FM / 2; ++part) {
-    const int mr = m0 + wm * S::WTM + 32 * part, nc = n0 + wn * S::WTN;
-#pragma unroll
-    for (int i = 0; i < S::FM; ++i) {
-      if (i / 2 != part) continue;
-#pragma unroll
-      for (int j = 0; j < S::FN; ++j)
-        *reinterpret_cast<floatx4*>(st + (16 * (i & 1) + li) * PITCH + 16 * j + 4 * q) = acc[i][j];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    constexpr int CH = S::WTN / 8;  // 8-column chunks of a row
-#pragma unroll
-    for (int k = 0; k < 32 * CH / 64; ++k) {
-      const int task = lane + 64 * k, r = task / CH, c = (task % CH) * 8;
-      float v[8];
-      chunk_to_f<float>(ld_chunk(st + r * PITCH + c), v);
-      chunk_to_f<float>(ld_chunk(st + r * PITCH + c + 4), v + 4);
-      const size_t o = mat * a.o_mat + (size_t)(mr + r) * a.N + nc + c;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= a.alpha;
-      if (a.d) {
-        const half8 dv = __builtin_bit_cast(half8, ld_chunk(a.d + o));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += a.beta * (float)dv[e];
-        if (PRECISE) {
-          const half8 d1 = __builtin_bit_cast(half8, ld_chunk(a.d + a.o_plane + o));
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += a.beta * (float)d1[e];
-        }
-      }
-      if (MODE != NS_LAST) {
-#pragma unroll
-        for (int p = 0; p < (PRECISE ? 2 : 1); ++p) {
-          half8 h;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) h[e] = part_of(v[e], p != 0);
-          st_chunk(a.out + p * a.o_plane + o, __builtin_bit_cast(Chunk, h));
-        }
-      }
-      st_chunk(st + r * PITCH + c, f_to_chunk<float>(v));
-      st_chunk(st + r * PITCH + c + 4, f_to_chunk<float>(v + 4));
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (MODE == NS_LAST) {
-      // rows of the parameters: X's rows, or its columns where the tensor is stored transposed
-      const int inner = flip ? 4 : CH, outer = flip ? S::WTN : 32;
-      for (int k = 0; k < outer * inner / 64; ++k) {
-        const int task = lane + 64 * k, r = task / inner, c = (task % inner) * 8;
-        float v[8], p[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = flip ? st[(c + e) * PITCH + r] : st[r * PITCH + c + e];
-        const size_t in = (size_t)(mat % a.G) * a.o_mat +
-                          (flip ? (size_t)(nc + r) * a.M + mr + c : (size_t)(mr + r) * a.N + nc + c);
-        float* mp = a.master ? a.master + (size_t)tensor * a.G * a.o_mat + in : nullptr;
-        float* wf = (float*)a.w[tensor] + in;
-        bf16* wb = (bf16*)a.w[tensor] + in;
-        if (mp || a.dtype == MOE_F32) {
-          const float* from = mp ? mp : wf;
-          chunk_to_f<float>(ld_chunk(from), p);
-          chunk_to_f<float>(ld_chunk(from + 4), p + 4);
-        } else {
-          chunk_to_f<bf16>(ld_chunk(wb), p);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = a.decay * p[e] - a.step * v[e];
-        if (mp) {
-          st_chunk(mp, f_to_chunk<float>(p));
-          st_chunk(mp + 4, f_to_chunk<float>(p + 4));
-        }
-        if (a.dtype == MOE_F32) {
-          st_chunk(wf, f_to_chunk<float>(p));
-          st_chunk(wf + 4, f_to_chunk<float>(p + 4));
-        } else {
-          st_chunk(wb, f_to_chunk<bf16>(p));
-        }
-      }
-    } else if (MODE == NS_BOTH || mt != nt) {
-#pragma unroll
-      for (int k = 0; k < S::WTN * 4 / 64; ++k) {
-        const int task = lane + 64 * k, r = task >> 2, c = (task & 3) * 8;
-        const size_t o = mat * a.o_mat + (size_t)(nc + r) * a.M + mr + c;
-#pragma unroll
-        for (int p = 0; p < (PRECISE ? 2 : 1); ++p) {
-          half8 h;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) h[e] = part_of(st[(c + e) * PITCH + r], p != 0);
-          st_chunk(a.out_t + p * a.o_plane + o, __builtin_bit_cast(Chunk, h));
-        }
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+template <typename S, int MODE, bool PRECISE>
+__global__ __launch_bounds__(S::NT) void muon_product_kernel(NsArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tm = (a.M + S::BM - 1) / S::BM, tn = (a.N + S::BN - 1) / S::BN;
+  int mat, mt, nt;
+  bool other;
+  if (!S::PIPE || (int)blockIdx.x < a.whole) {
+    ns_tile<MODE>(a, xcd_order(blockIdx.x, S::PIPE ? a.whole : (int)gridDim.x), tm, tn, mat, other, mt, nt);
+    product_tile<S, MODE, PRECISE>(a, smem, mat, other, mt * S::BM, nt * S::BN);
+  } else {  // a quarter of one of the last tiles
+    const int l = xcd_order(blockIdx.x - a.whole, (int)gridDim.x - a.whole);
+    ns_tile<MODE>(a, a.whole + l / 4, tm, tn, mat, other, mt, nt);
+    const int m0 = mt * S::BM + (l >> 1 & 1) * (S::BM / 2), n0 = nt * S::BN + (l & 1) * (S::BN / 2);
+    if (m0 >= a.M || n0 >= a.N || (MODE == NS_SYMMETRIC && m0 > n0)) return;  // below the diagonal: the mirror of another
+    product_tile<NsQuarter, MODE, PRECISE>(a, smem, mat, other, m0, n0);
   }
 }
 
-typedef NtShape<128, 128, 2, 2, 2> NsSmall;
+template <typename S, int MODE>
+int64_t ns_tiles(const NsArgs& a) {
+  const int64_t tm = (a.M + S::BM - 1) / S::BM, tn = (a.N + S::BN - 1) / S::BN;
+  return (MODE == NS_SYMMETRIC ? tm * (tm + 1) / 2 * (a.q2 ? 2 : 1) : tm * tn) * a.mats;
+}
 
 template <typename S, int MODE, bool PRECISE>
-hipError_t ns_launch(const char* name, const NsArgs& a, hipStream_t s) {
+hipError_t ns_launch(const char* name, NsArgs a, hipStream_t s) {
   static std::atomic<uint64_t> done{0};
   const auto kern = muon_product_kernel<S, MODE, PRECISE>;
-  if (hipError_t e = lds_limit_once((const void*)kern, S::LDS, done); e != hipSuccess) return e;
-  const int64_t tm = (a.M + S::BM - 1) / S::BM, tn = (a.N + S::BN - 1) / S::BN;
-  const int64_t tiles = (MODE == NS_SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn) * a.mats;
+  constexpr int lds = S::PIPE && NsLds<NsQuarter, MODE>::BYTES > NsLds<S, MODE>::BYTES ? NsLds<NsQuarter, MODE>::BYTES : NsLds<S, MODE>::BYTES;
+  if (hipError_t e = lds_limit_once((const void*)kern, lds, done); e != hipSuccess) return e;
+  int64_t tiles = ns_tiles<S, MODE>(a);
+  a.whole = (int)tiles;
+  if (S::PIPE) {
+    // A last round of few tiles is split into quarters, which take about 0.4 of a tile's time each.
+    const int64_t cus = device_cus(), rest = tiles % cus;
+    static const char* noq = getenv("NS_NOQ");
+    if (!noq && 4 * rest <= 2 * cus) {
+      a.whole = (int)(tiles - rest);
+      tiles += 3 * rest;
+    }
+  }
   KernelTimer kt(name, s);
-  hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(S::NT), S::LDS, s, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(S::NT), lds, s, a);
   return hipGetLastError();
 }
 template <int MODE>
 hipError_t ns_product(const char* name, const NsArgs& a, bool precise, hipStream_t s) {
-  return precise ? ns_launch<NsSmall, MODE, true>(name, a, s) : ns_launch<NsSmall, MODE, false>(name, a, s);
+  const auto go = [&](auto shape) {
+    using S = decltype(shape);
+    return precise ? ns_launch<S, MODE, true>(name, a, s) : ns_launch<S, MODE, false>(name, a, s);
+  };
+  // Rounds of the chip, each priced by a tile's time: 4 units of the 128 x 128 tile's work at 1.4 times its rate, two such
+  // tiles at once.
+  const int64_t cus = device_cus();
+  const auto rounds = [&](int64_t tiles, int64_t slots) { return (double)((tiles + slots - 1) / slots); };
+  const double large = rounds(ns_tiles<NsLarge, MODE>(a), cus) * 4 / 1.4, small = rounds(ns_tiles<NsSmall, MODE>(a), 2 * cus) * 2;
+  if (const char* force = getenv("NS_TILE")) {
+    if (force[0] == 'l') return go(NsLarge{});
+    if (force[0] == 's') return go(NsSmall{});
+    return go(NsTiny{});
+  }
+  if (ns_tiles<NsTiny, MODE>(a) <= cus) return go(NsTiny{});
+  return large <= small ? go(NsLarge{}) : go(NsSmall{});
 }
 
 struct MuonLayout {
   int mats, m, n;
   size_t x_plane, a_plane;  // elements of a part of X and of A
-  size_t part, x, xt, a, b, bytes;
+  size_t x, xt[2], a, r, b[3], bytes;  // the partial sums of squares come first
 };
 MuonLayout muon_layout(const moe_desc& d, bool precise) {
   MuonLayout l{};
@@ -339,11 +516,18 @@ MuonLayout muon_layout(const moe_desc& d, bool precise) {
   const size_t parts = precise ? 2 : 1;
   l.x_plane = (size_t)l.mats * l.m * l.n;
   l.a_plane = (size_t)l.mats * l.m * l.m;
-  l.x = align256(sizeof(double) * l.mats * SUM_BLOCKS);
-  l.xt = l.x + align256(parts * l.x_plane * 2);  // two of them, in turn
-  l.a = l.xt + 2 * align256(parts * l.x_plane * 2);
-  l.b = l.a + align256(parts * l.a_plane * 2);
-  l.bytes = l.b + align256(parts * l.a_plane * 2);
+  size_t at = align256(sizeof(double) * l.mats * SUM_BLOCKS);
+  const auto take = [&](size_t plane) {
+    const size_t here = at;
+    at += align256(parts * plane * 2);
+    return here;
+  };
+  l.x = take(l.x_plane);
+  for (size_t& o : l.xt) o = take(l.x_plane);
+  l.a = take(l.a_plane);
+  l.r = take(l.a_plane);
+  for (size_t& o : l.b) o = take(l.a_plane);
+  l.bytes = at;
   return l;
 }
 
@@ -363,6 +547,29 @@ double largest(double c0, double c1, double c2, double top) {
   for (double s : roots)
     if (s > 0 && s < top * top) most = std::max(most, at(std::sqrt(s)));
   return most;
+}
+// Largest |c0 + c1 s + c2 s^2| over s in [0, top^2]: of the factor by which a step multiplies a singular value.
+double largest_factor(double c0, double c1, double c2, double top) {
+  const double s1 = top * top;
+  double most = std::max(std::fabs(c0), std::fabs(c0 + s1 * (c1 + s1 * c2)));
+  if (c2 != 0) {
+    const double s = -c1 / (2 * c2);
+    if (s > 0 && s < s1) most = std::max(most, std::fabs(c0 + s * (c1 + s * c2)));
+  }
+  return most;
+}
+// Steps that are taken on A before X is formed again.
+int muon_group(const MuonLayout& l, int done, int steps) {
+  int g = 1;
+  const char* e = getenv("NS_PLAN");
+  const char* plan = e ? e : (2 * l.n >= 3 * l.m ? "23" : "1");
+  int at = 0;
+  for (int i = 0; ; ++i) {
+    g = plan[i] - '0';
+    if (at == done || !plan[i + 1]) break;
+    at += g;
+  }
+  return std::min(g, steps - done);
 }
 // The power of two that takes values of up to `top` below 2^15.
 double two_to(double top) {
@@ -401,7 +608,7 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
   a.nesterov = o.nesterov;
   a.eps = (double)o.eps;
   a.x = (f16*)(base + l.x);
-  a.xt = (f16*)(base + l.xt);
+  a.xt = (f16*)(base + l.xt[0]);
   a.plane = l.x_plane;
   double sx = two_to(1.0);
   a.s0 = (float)sx;
@@ -426,16 +633,16 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
 
-  f16* xt[2] = {a.xt, (f16*)(base + l.xt + (l.a - l.xt) / 2)};
-  f16 *A = (f16*)(base + l.a), *B = (f16*)(base + l.b);
+  f16 *xt[2] = {a.xt, (f16*)(base + l.xt[1])}, *A = (f16*)(base + l.a), *R = (f16*)(base + l.r);
+  f16* buf[3];
+  for (int i = 0; i < 3; ++i) buf[i] = (f16*)(base + l.b[i]);
   const size_t mn = (size_t)l.m * l.n, mm = (size_t)l.m * l.m;
-  double top = 1.0;
-  for (int step = 0; step < o.steps; ++step) {
-    const double sa = two_to(top * top), next = largest(o.a, o.b, o.c, top);
-    // B's largest eigenvalue: |b s^2 + c s^4| over [0, top]
-    double tb = std::fabs(top * top * (o.b + o.c * top * top));
-    if (o.c != 0 && -o.b / (2 * o.c) > 0 && -o.b / (2 * o.c) < top * top) tb = std::max(tb, std::fabs(o.b * o.b / (4 * (double)o.c)));
-    const double sb = two_to(tb), sn = two_to(next);
+  double top = 1.0;   // of X's singular values
+  int turn = 0;
+  for (int done = 0; done < o.steps;) {
+    const int group = muon_group(l, done, o.steps);
+    const bool last = done + group == o.steps;
+    // A = X X^T
     NsArgs n{};
     n.mats = l.mats;
     n.M = n.N = l.m;
@@ -443,37 +650,84 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
     n.p = n.q = a.x;
     n.p_mat = n.q_mat = mn;
     n.p_plane = n.q_plane = l.x_plane;
-    n.out = n.out_t = A;
+    n.out = A;
     n.o_mat = mm;
     n.o_plane = l.a_plane;
+    double sa = two_to(top * top);
     n.alpha = (float)(sa / (sx * sx));
     if (hipError_t e = ns_product<NS_SYMMETRIC>("muon_gram", n, o.precise, s); e != hipSuccess) return e;
     n.K = l.m;
-    n.p = n.q = n.d = A;
     n.p_mat = n.q_mat = mm;
     n.p_plane = n.q_plane = l.a_plane;
-    n.out = n.out_t = B;
-    n.alpha = (float)((double)o.c * sb / (sa * sa));
-    n.beta = (float)((double)o.b * sb / sa);
-    if (hipError_t e = ns_product<NS_SYMMETRIC>("muon_square", n, o.precise, s); e != hipSuccess) return e;
-    const bool last = step == o.steps - 1;
+    f16 *P = nullptr, *Q = nullptr;
+    double sp = 0, sq = 0, tq = 1.0;
+    for (int i = 0; i < group; ++i) {
+      // P = a + b A + c A^2, in a buffer that is neither Q nor the last P
+      const double tp = largest_factor(o.a, o.b, o.c, top);
+      sp = two_to(tp);
+      f16* next = buf[0];
+      for (f16* f : buf)
+        if (f != P && f != Q) next = f;
+      NsArgs v = n;
+      v.p = v.q = v.d = A;
+      v.out = P = next;
+      v.alpha = (float)((double)o.c * sp / (sa * sa));
+      v.beta = (float)((double)o.b * sp / sa);
+      v.diag = (float)((double)o.a * sp);
+      if (hipError_t e = ns_product<NS_SYMMETRIC>("muon_poly", v, o.precise, s); e != hipSuccess) return e;
+      // R = P A unless X is formed next, and Q <- P Q
+      v = n;
+      v.p = P;
+      const bool more = i + 1 < group;
+      const double tr = tp * top * top, sr = two_to(tr), sq2 = two_to(tp * tq);
+      f16* q_out = nullptr;
+      for (f16* f : buf)
+        if (f != P && f != Q) q_out = f;
+      if (more) {
+        v.q = A;
+        v.out = R;
+        v.alpha = (float)(sr / (sp * sa));
+        if (Q) {
+          v.q2 = Q;
+          v.out2 = q_out;
+          v.alpha2 = (float)(sq2 / (sp * sq));
+        }
+      } else if (Q) {
+        v.q = Q;
+        v.out = q_out;
+        v.alpha = (float)(sq2 / (sp * sq));
+      }
+      if (more || Q) {
+        if (hipError_t e = ns_product<NS_SYMMETRIC>("muon_chain", v, o.precise, s); e != hipSuccess) return e;
+      }
+      top = largest(o.a, o.b, o.c, top);
+      if (more) {  // A <- P R, the Gram matrix of P X
+        v = n;
+        v.p = P;
+        v.q = R;
+        v.out = A;
+        sa = two_to(top * top);
+        v.alpha = (float)(sa / (sp * sr));
+        if (hipError_t e = ns_product<NS_SYMMETRIC>("muon_chain", v, o.precise, s); e != hipSuccess) return e;
+      }
+      tq *= tp;
+      sq = Q ? sq2 : sp;
+      Q = Q ? q_out : P;
+    }
+    // X <- Q X
     n.N = l.n;
-    n.p = B;
-    n.q = xt[step & 1];
+    n.p = Q;
+    n.q = xt[turn];
     n.q_mat = mn;
     n.q_plane = l.x_plane;
-    n.d = a.x;
-    n.out = a.x;
-    n.out_t = xt[(step + 1) & 1];
     n.o_mat = mn;
     n.o_plane = l.x_plane;
-    n.alpha = (float)((last ? 1.0 : sn) / (sb * sx));
-    n.beta = (float)((double)o.a * (last ? 1.0 : sn) / sx);
+    const double sn = last ? 1.0 : two_to(top);
+    n.alpha = (float)(sn / (sq * sx));
     if (last) {
-      for (int t = 0; t < 3; ++t) {
-        n.w[t] = a.w[t];
-        n.flip[t] = (t == 2 ? a.d > a.f : a.f > a.d) ? 1 : 0;
-      }
+      for (int t = 0; t < 3; ++t) n.w[t] = a.w[t];
+      n.flip_up = a.f > a.d;
+      n.flip_down = a.d > a.f;
       n.master = master;
       n.G = a.G;
       n.dtype = d.dtype;
@@ -481,10 +735,13 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
       n.step = (float)((double)o.lr * (double)o.scale);
       if (hipError_t e = ns_product<NS_LAST>("muon_update", n, o.precise, s); e != hipSuccess) return e;
     } else {
+      n.out = a.x;
+      turn ^= 1;
+      n.out_t = xt[turn];
       if (hipError_t e = ns_product<NS_BOTH>("muon_step", n, o.precise, s); e != hipSuccess) return e;
     }
     sx = sn;
-    top = next;
+    done += group;
   }
   return hipSuccess;
 }

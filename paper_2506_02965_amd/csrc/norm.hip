@@ -63,8 +63,9 @@ __device__ __forceinline__ F sum64(F v) {
   return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
 
-// Sums of two fp64 and two fp32 values over the workgroup's wavefronts. Consecutive calls alternate between two halves of
-// `lds`: a wavefront that writes a half again has passed the barrier that the others reach after reading it.
+// Sums of up to two fp64 and two fp32 values over the workgroup's wavefronts (D, F: how many; the others are left alone).
+// Consecutive calls alternate between two halves of `lds`: a wavefront that writes a half again has passed the barrier that the
+// others reach after reading it.
 struct Sums {
   double d0, d1;
   float f0, f1;
@@ -72,25 +73,38 @@ struct Sums {
 struct SumLds {
   Sums s[2][kMaxWaves];
 };
+template <int D, int F>
 __device__ __forceinline__ Sums block_sum(Sums v, SumLds& lds, int& turn) {
-  v.d0 = sum64(v.d0);
-  v.d1 = sum64(v.d1);
-  v.f0 = sum64(v.f0);
-  v.f1 = sum64(v.f1);
+  if (D > 0) v.d0 = sum64(v.d0);
+  if (D > 1) v.d1 = sum64(v.d1);
+  if (F > 0) v.f0 = sum64(v.f0);
+  if (F > 1) v.f1 = sum64(v.f1);
   const int waves = blockDim.x >> 6;
   if (waves == 1) return v;
-  if ((threadIdx.x & 63) == 0) lds.s[turn][threadIdx.x >> 6] = v;
+  Sums* at = lds.s[turn];
+  if ((threadIdx.x & 63) == 0) {
+    Sums& to = at[threadIdx.x >> 6];
+    if (D > 0) to.d0 = v.d0;
+    if (D > 1) to.d1 = v.d1;
+    if (F > 0) to.f0 = v.f0;
+    if (F > 1) to.f1 = v.f1;
+  }
   __syncthreads();
-  Sums t = lds.s[turn][0];
-  for (int w = 1; w < waves; ++w) {
-    const Sums u = lds.s[turn][w];
-    t.d0 += u.d0;
-    t.d1 += u.d1;
-    t.f0 += u.f0;
-    t.f1 += u.f1;
+  Sums t{0., 0., 0.f, 0.f};
+  for (int w = 0; w < waves; ++w) {
+    if (D > 0) t.d0 += at[w].d0;
+    if (D > 1) t.d1 += at[w].d1;
+    if (F > 0) t.f0 += at[w].f0;
+    if (F > 1) t.f1 += at[w].f1;
   }
   turn ^= 1;
   return t;
+}
+
+// 1 / sqrt(v) to fp32: the hardware's estimate (23 bits) and a Newton step, in fp64 for its range.
+__device__ __forceinline__ float rsqrt_of(double v) {
+  const double y = __builtin_amdgcn_rsq(v);
+  return y == 0. ? 0.f : (float)(y * fma(-0.5 * v * y, y, 1.5));  // an infinite sum
 }
 
 // The chunk of a thread's i-th piece, and whether the row has it.
@@ -124,7 +138,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
 #pragma unroll
           for (int e = 0; e < EP; ++e) s.d0 += (double)y[e];
         }
-        mean = (float)(block_sum(s, lds, turn).d0 * a.inv_d);
+        mean = (float)(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d);
       }
       if (a.post != MOE_NORM_NONE) {
         Sums s{0., 0., 0.f, 0.f};
@@ -137,7 +151,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
 #pragma unroll
             for (int e = 0; e < EP; ++e) s.d0 += (double)(y[e] - mean) * (double)(y[e] - mean);
         }
-        rstd = (float)(1.0 / sqrt(block_sum(s, lds, turn).d0 * a.inv_d + a.eps));
+        rstd = rsqrt_of(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d + a.eps);
       }
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
@@ -174,7 +188,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
 #pragma unroll
           for (int e = 0; e < EP; ++e) s.d0 += (double)v[i][e];
       }
-      mean = (float)(block_sum(s, lds, turn).d0 * a.inv_d);
+      mean = (float)(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d);
     }
     Sums s{0., 0., 0.f, 0.f};
 #pragma unroll
@@ -184,7 +198,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
 #pragma unroll
         for (int e = 0; e < EP; ++e) s.d0 += (double)(v[i][e] - mean) * (double)(v[i][e] - mean);
     }
-    const float rstd = (float)(1.0 / sqrt(block_sum(s, lds, turn).d0 * a.inv_d + a.eps));
+    const float rstd = rsqrt_of(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d + a.eps);
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
       PIECE(i);
@@ -209,6 +223,7 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
   __shared__ SumLds lds;
   int turn = 0;
   const bool need_y = a.y && (POST || a.gate);
+  const bool lr = PRE && a.pre == MOE_NORM_LAYER, ly = POST && a.post == MOE_NORM_LAYER;
   float s_pre[CPT][EP], s_post[CPT][EP], s_gate[CPT][EP];
   Chunk wpre[CPT], wpost[CPT], gc[CPT];
 #pragma unroll
@@ -241,20 +256,35 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < EP; ++e) s_gate[i][e] = 0.f;
     }
-    for (int t = g * a.gate_rows + first; t < g * a.gate_rows + last; ++t) {
+    // the next row's chunks are loaded while a row is worked on
+    Chunk next[4][CPT];
+    const auto fetch = [&](int t, bool there) {
+      const size_t row = (size_t)t * a.cpr;
+#pragma unroll
+      for (int i = 0; i < CPT; ++i) {
+        PIECE(i);
+        const bool ld = in && there;
+        next[0][i] = a.dr && ld ? ld_chunk((const Chunk*)a.dr + row + c) : zero_chunk();
+        next[1][i] = PRE && ld ? ld_chunk((const Chunk*)a.dh + row + c) : zero_chunk();
+        next[2][i] = PRE && ld ? ld_chunk((const Chunk*)a.r + row + c) : zero_chunk();
+        next[3][i] = need_y && ld ? ld_chunk((const Chunk*)a.y + row + c) : zero_chunk();
+      }
+    };
+    const int t1 = g * a.gate_rows + last;
+    fetch(g * a.gate_rows + first, first < last);
+    for (int t = g * a.gate_rows + first; t < t1; ++t) {
       const size_t row = (size_t)t * a.cpr;
       Chunk drc[CPT], dhc[CPT], rc[CPT], yc[CPT];
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
-        PIECE(i);
-        drc[i] = a.dr && in ? ld_chunk((const Chunk*)a.dr + row + c) : zero_chunk();
-        dhc[i] = PRE && in ? ld_chunk((const Chunk*)a.dh + row + c) : zero_chunk();
-        rc[i] = PRE && in ? ld_chunk((const Chunk*)a.r + row + c) : zero_chunk();
-        yc[i] = need_y && in ? ld_chunk((const Chunk*)a.y + row + c) : zero_chunk();
+        drc[i] = next[0][i];
+        dhc[i] = next[1][i];
+        rc[i] = next[2][i];
+        yc[i] = next[3][i];
       }
+      fetch(t + 1, t + 1 < t1);
       // row sums: of r and y (LAYER), then of their squares with those of a = dh w_pre
       float mr = 0.f, my = 0.f, ma = 0.f, rr = 1.f, ry = 1.f, car = 0.f;
-      const bool lr = PRE && a.pre == MOE_NORM_LAYER, ly = POST && a.post == MOE_NORM_LAYER;
       if (lr || ly) {
         Sums s{0., 0., 0.f, 0.f};
 #pragma unroll
@@ -271,7 +301,7 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
             if (lr) s.f0 += a.w_pre ? dh[e] * w[e] : dh[e];
           }
         }
-        s = block_sum(s, lds, turn);
+        s = block_sum<2, 1>(s, lds, turn);
         if (lr) mr = (float)(s.d0 * a.inv_d);
         if (ly) my = (float)(s.d1 * a.inv_d);
         if (lr) ma = (float)((double)s.f0 * a.inv_d);
@@ -294,9 +324,11 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
               if (PRE) s.f0 += (a.w_pre ? dh[e] * w[e] : dh[e]) * (r[e] - mr);
             }
         }
-        s = block_sum(s, lds, turn);
-        if (PRE) rr = (float)(1.0 / sqrt(s.d0 * a.inv_d + a.eps));
-        if (POST) ry = (float)(1.0 / sqrt(s.d1 * a.inv_d + a.eps));
+        if (PRE && POST) s = block_sum<2, 1>(s, lds, turn);
+        else if (PRE) s = block_sum<1, 1>(s, lds, turn);
+        else s = block_sum<2, 0>(s, lds, turn);
+        if (PRE) rr = rsqrt_of(s.d0 * a.inv_d + a.eps);
+        if (POST) ry = rsqrt_of(s.d1 * a.inv_d + a.eps);
         if (PRE) car = (float)((double)s.f0 * a.inv_d) * rr;  // mean(a rhat)
       }
       float b[CPT][EP];  // gradient of r, then of post(y)
@@ -337,7 +369,7 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
       }
       if (!a.y) continue;
       if (POST) {
-        s = block_sum(s, lds, turn);
+        s = ly ? block_sum<0, 2>(s, lds, turn) : block_sum<0, 1>(s, lds, turn);
         const float cy = (float)((double)s.f0 * a.inv_d), mb = (float)((double)s.f1 * a.inv_d);
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
@@ -379,30 +411,40 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
 }
 #undef PIECE
 
-// Sums of the workgroups' partial rows. blockIdx.y: dw_pre, dw_post, then the gate rows; a workgroup adds 64 columns, 16
-// threads by 16 shares of the rows.
+// Sums of the workgroups' partial rows. blockIdx.y: dw_pre, dw_post, then the gate rows; a workgroup adds SUM_COLS columns,
+// four a thread, by SHARES shares of the rows.
+constexpr int SUM_COLS = 32, SHARES = 256 / (SUM_COLS / 4);
 __global__ __launch_bounds__(256) void norm_sums_kernel(NormArgs a, int first) {
   const int which = blockIdx.y + first;
   float* out = which == 0 ? a.dw_pre : which == 1 ? a.dw_post : a.dgate + (size_t)(which - 2) * a.d;
   if (!out) return;  // uniform
   const int n = which < 2 ? a.n_part : a.parts;
   const float* part = a.part + ((size_t)min(which, 2) * a.n_part + (which < 2 ? 0 : (size_t)(which - 2) * a.parts)) * a.d;
-  const int col = blockIdx.x * 64 + 4 * (threadIdx.x & 15), share = threadIdx.x >> 4;
+  const int quad = threadIdx.x % (SUM_COLS / 4), share = threadIdx.x / (SUM_COLS / 4);
+  const int col = blockIdx.x * SUM_COLS + 4 * quad;
   float s[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int p = share; p < n; p += 16) {
-    float v[4];
-    chunk_to_f<float>(ld_chunk(part + (size_t)p * a.d + col), v);
+  for (int p = share; p < n; p += SHARES * 8) {  // eight loads at a time
+    Chunk c[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] += v[e];
+    for (int k = 0; k < 8; ++k)
+      c[k] = p + SHARES * k < n ? ld_chunk(part + (size_t)(p + SHARES * k) * a.d + col) : zero_chunk();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      float v[4];
+      chunk_to_f<float>(c[k], v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += v[e];
+    }
   }
-  __shared__ float sums[16][64];
+  __shared__ float sums[SHARES][SUM_COLS];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) sums[share][4 * (threadIdx.x & 15) + e] = s[e];
+  for (int e = 0; e < 4; ++e) sums[share][4 * quad + e] = s[e];
   __syncthreads();
-  if (threadIdx.x < 64) {
-    float v = 0.f;
-    for (int k = 0; k < 16; ++k) v += sums[k][threadIdx.x];
-    out[blockIdx.x * 64 + threadIdx.x] = v;
+  if (threadIdx.x < SUM_COLS) {
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < SHARES; ++k) v[k % 4] += sums[k][threadIdx.x];
+    out[blockIdx.x * SUM_COLS + threadIdx.x] = (v[0] + v[1]) + (v[2] + v[3]);
   }
 }
 
@@ -492,8 +534,9 @@ hipError_t launch_residual_norm_bwd(const moe_desc& d, const moe_norm& n, const 
   a.dgate = gate ? dgate : nullptr;
   a.dw_pre = w_pre ? dw_pre : nullptr;
   a.part = (float*)ws;
-  // workgroups: about four rows each, kMaxParts at most
-  const int want = std::max(1, std::min(kMaxParts, a.T / 4));
+  // Workgroups: a row each while there are few, which leaves most of them to run at once (777 x 1024 fp32, a row / two / four /
+  // eight: 14.0 / 15.0 / 17.3 / 26 us). One or two rows: a single workgroup, which needs no second launch.
+  const int want = a.T <= 2 ? 1 : std::min(kMaxParts, a.T);
   a.parts = a.groups <= want ? std::min(want / a.groups, a.gate_rows) : 0;
   a.n_part = a.parts ? a.groups * a.parts : want;
   a.direct = a.n_part == 1;
@@ -516,7 +559,7 @@ hipError_t launch_residual_norm_bwd(const moe_desc& d, const moe_norm& n, const 
   if (weights || gates) {
     const int first = weights ? 0 : 2, rows = (weights ? 2 : 0) + (gates ? a.groups : 0);
     KernelTimer kt("residual_norm_sums", s);
-    hipLaunchKernelGGL(norm_sums_kernel, dim3(a.d / 64, rows), dim3(256), 0, s, a, first);
+    hipLaunchKernelGGL(norm_sums_kernel, dim3(a.d / SUM_COLS, rows), dim3(256), 0, s, a, first);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -18,12 +18,22 @@ struct F16 {
   static __device__ __forceinline__ acc mfma(const Chunk& a, const Chunk& b, acc c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
   }
+  static __device__ __forceinline__ void mfma_agpr(acc& c, const Chunk& a, const Chunk& b) {
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0"
+                 : "+a"(c)
+                 : "v"(__builtin_bit_cast(int32x4, a)), "v"(__builtin_bit_cast(int32x4, b)));
+  }
 };
 struct I8 {
   typedef int32x4 acc;
   static constexpr int size = 1;
   static __device__ __forceinline__ acc mfma(const Chunk& a, const Chunk& b, acc c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(int32x4, a), __builtin_bit_cast(int32x4, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ void mfma_agpr(acc& c, const Chunk& a, const Chunk& b) {
+    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0"
+                 : "+a"(c)
+                 : "v"(__builtin_bit_cast(int32x4, a)), "v"(__builtin_bit_cast(int32x4, b)));
   }
 };
 
@@ -37,15 +47,22 @@ struct NtShape {
   static constexpr int FM = WTM / 16, FN = WTN / 16;
   static constexpr int IA = BM / 8 / NW, IB = BN / 8 / NW;  // direct loads (8 rows each) per wavefront and K-tile
   static constexpr int A_BYTES = BM * NT_ROWB, STAGE = (BM + BN) * NT_ROWB, LDS = STAGES * STAGE;
+  // one wavefront per SIMD with outputs of 128 columns: nt_pipe
+  static constexpr bool PIPE = BM >= 128 && BN == 256 && NW == 4 && STAGES == 2;
   static_assert(IA * 8 * NW == BM && IB * 8 * NW == BN, "tiles split evenly over the wavefronts");
 };
 
-// K loop of one tile. load_a(kt, j, dst) and load_b(kt, j, dst) issue the direct load of rows 8 j .. 8 j + 7 of K-tile kt
-// to LDS address dst: lane l brings row 8 j + (l >> 3), chunk (l & 7) ^ (l >> 3) (nt_lane). Accumulators hold, in lane (q =
+// Where a direct load takes its rows from: lane l brings row l >> 3 of eight, chunk (l & 7) ^ (l >> 3) (nt_lane).
+struct NtSrc {
+  int32x4 rsrc;
+  int off;
+};
+
+// K loop of one tile. src_a(kt, j) and src_b(kt, j) name rows 8 j .. 8 j + 7 of K-tile kt. Accumulators hold, in lane (q =
 // lane >> 4, i = lane & 15), row i of the fragment and its columns 4 q .. 4 q + 3. `live`: this wavefront has something to
 // compute (uniform); the others load and synchronise with it.
 template <typename S, typename E, typename LA, typename LB>
-__device__ __forceinline__ void nt_loop(char* smem, int ktiles, bool live, LA&& load_a, LB&& load_b,
+__device__ __forceinline__ void nt_ring(char* smem, int ktiles, bool live, LA&& src_a, LB&& src_b,
                                         typename E::acc (&acc)[S::FM][S::FN]) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::WN, wn = wave % S::WN;
@@ -54,9 +71,15 @@ __device__ __forceinline__ void nt_loop(char* smem, int ktiles, bool live, LA&& 
   const auto issue = [&](int kt) {
     const uint32_t st = base + (kt % S::STAGES) * S::STAGE;
 #pragma unroll
-    for (int j = 0; j < S::IA; ++j) load_a(kt, wave + S::NW * j, st + (wave + S::NW * j) * 1024);
+    for (int j = 0; j < S::IA; ++j) {
+      const NtSrc a = src_a(kt, wave + S::NW * j);
+      dma16(a.rsrc, st + (wave + S::NW * j) * 1024, a.off);
+    }
 #pragma unroll
-    for (int j = 0; j < S::IB; ++j) load_b(kt, wave + S::NW * j, st + S::A_BYTES + (wave + S::NW * j) * 1024);
+    for (int j = 0; j < S::IB; ++j) {
+      const NtSrc b = src_b(kt, wave + S::NW * j);
+      dma16(b.rsrc, st + S::A_BYTES + (wave + S::NW * j) * 1024, b.off);
+    }
   };
 #pragma unroll
   for (int i = 0; i < S::FM; ++i)
@@ -89,6 +112,95 @@ __device__ __forceinline__ void nt_loop(char* smem, int ktiles, bool live, LA&& 
   }
   __syncthreads();  // the operands' LDS is free
 }
+
+// The same for 256 x 256 tiles with one wavefront per SIMD (accumulators in AGPRs). Nothing else hides a stall of a
+// wavefront, so its loop is ordered by hand: while the MFMAs of a 64-byte step run, the fragments of the next step are read
+// into other registers, one read after every fourth MFMA, and during a K-tile's second step the 16 direct loads of the K-tile
+// after the next are issued. One barrier per K-tile, between its steps: by then every wavefront has read the K-tile's last
+// fragments (its stage is free), and its loads of the next K-tile, issued a whole K-tile ago, have landed. Loads past the
+// last K-tile are issued with an offset past every range: a branch around them would make the compiler move accumulators.
+// 8192 x 14336 x 8192 bytes of K, products alone: 1,320 TFLOP/s fp16 and 2,650 TOP/s int8, against 980 and 1,980 of the
+// 128 x 128 tiles, and 1,260 and 2,460 of the same loop with eight wavefronts of 128 x 64, whose fragments pass LDS 1.5 times
+// as often.
+template <typename S, typename E, typename LA, typename LB>
+__device__ __forceinline__ void nt_pipe(char* smem, int ktiles, bool live, LA&& src_a, LB&& src_b,
+                                        typename E::acc (&acc)[S::FM][S::FN]) {
+  static_assert(S::STAGES == 2, "two stages");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / S::WN, wn = wave % S::WN, q = lane >> 4, li = lane & 15;
+  const uint32_t base = lds_addr(smem);
+  constexpr int LOADS = S::IA + S::IB, NF = S::FM + S::FN, NM = S::FM * S::FN;
+  constexpr int RS = NM / NF, LS = NM / LOADS;  // MFMAs for each read, and for each load
+  constexpr int OOR = 0x7fffffff;               // no operand has 2^31 bytes
+  const auto load = [&](int kt, int l) {
+    const uint32_t st = base + (kt & 1) * S::STAGE;
+    const NtSrc s = l < S::IA ? src_a(kt, wave + S::NW * l) : src_b(kt, wave + S::NW * (l - S::IA));
+    const uint32_t dst = l < S::IA ? st + (wave + S::NW * l) * 1024 : st + S::A_BYTES + (wave + S::NW * (l - S::IA)) * 1024;
+    dma16(s.rsrc, dst, kt < ktiles ? s.off : OOR);
+  };
+  const int at0 = li * NT_ROWB + ((q ^ (li & 7)) << 4), at1 = li * NT_ROWB + (((4 + q) ^ (li & 7)) << 4);
+  const char* a0 = smem + wm * S::WTM * NT_ROWB;
+  const char* b0 = smem + S::A_BYTES + wn * S::WTN * NT_ROWB;
+  Chunk fa[2][S::FM], fb[2][S::FN];
+  // read t of step s of K-tile kt, in the order in which the MFMAs take them: A's first, B's, A's others
+  const auto read = [&](int kt, int s, int t) {
+    const int st = (kt & 1) * S::STAGE + (s ? at1 : at0);
+    if (t == 0) fa[s][0] = ld_chunk(a0 + st);
+    else if (t <= S::FN) fb[s][t - 1] = ld_chunk(b0 + st + 16 * (t - 1) * NT_ROWB);
+    else fa[s][t - S::FN] = ld_chunk(a0 + st + 16 * (t - S::FN) * NT_ROWB);
+  };
+  const auto barrier = [] {
+    wait_vmcnt<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) acc[i][j] = typename E::acc{0, 0, 0, 0};
+#pragma unroll
+  for (int l = 0; l < LOADS; ++l) load(0, l);
+#pragma unroll
+  for (int l = 0; l < LOADS; ++l) load(1, l);
+  wait_vmcnt<LOADS>();
+  asm volatile("s_barrier" ::: "memory");
+  if (!live) {
+    for (int kt = 0; kt < ktiles; ++kt) {
+      barrier();
+#pragma unroll
+      for (int l = 0; l < LOADS; ++l) load(kt + 2, l);
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < NF; ++t) read(0, 0, t);
+    for (int kt = 0; kt < ktiles; ++kt) {
+#pragma unroll
+      for (int m = 0; m < NM; ++m) {
+        E::mfma_agpr(acc[m / S::FN][m % S::FN], fb[0][m % S::FN], fa[0][m / S::FN]);
+        if (m % RS == 0 && m / RS < NF) read(kt, 1, m / RS);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      barrier();
+#pragma unroll
+      for (int m = 0; m < NM; ++m) {
+        E::mfma_agpr(acc[m / S::FN][m % S::FN], fb[1][m % S::FN], fa[1][m / S::FN]);
+        if (m % RS == 0 && m / RS < NF) read(kt + 1, 0, m / RS);
+        if (m % LS == LS / 2 && m / LS < LOADS) load(kt + 2, m / LS);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  wait_vmcnt<0>();  // the loads past the last K-tile have landed before the epilogue uses the LDS
+  asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");  // the last MFMAs' results are ready to read
+  __syncthreads();
+}
+
+template <typename S, typename E, typename LA, typename LB>
+__device__ __forceinline__ void nt_loop(char* smem, int ktiles, bool live, LA&& src_a, LB&& src_b,
+                                        typename E::acc (&acc)[S::FM][S::FN]) {
+  if constexpr (S::PIPE) nt_pipe<S, E>(smem, ktiles, live, src_a, src_b, acc);
+  else nt_ring<S, E>(smem, ktiles, live, src_a, src_b, acc);
+}
+
 // Byte offset of a lane's chunk within a direct load whose rows are ld bytes apart.
 __device__ __forceinline__ int nt_lane(int ld) {
   const int l = threadIdx.x & 63;

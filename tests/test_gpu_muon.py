@@ -1,9 +1,11 @@
 """moe_expert_update_muon against 64 bits.
 
-Tolerances are on the 2-norm of an update matrix. With u the relative rounding of X, A and B (2^-11, half a step of fp16;
-2^-21 where each is held in two parts) and products that sum K terms in fp32 (K / 16 + 8 roundings of 2^-24), a step adds
-u |X| to X, and through A and B their errors times what they multiply; a later step passes an error of X on by at most
-slope = max |p'| (or the largest quotient of differences), which a bounds. All of it is formed from the 64-bit run itself."""
+Tolerances are on the 2-norm of an update matrix. With u the relative rounding of every matrix that is kept (2^-11, half a
+step of fp16; 2^-21 where each is held in two parts) and products that sum K terms in fp32 (K / 16 + 8 roundings of 2^-24),
+errors are followed to first order through the products that the library takes: A = X X^T, and for the steps of a group (two
+steps, then three at a time, where the long side is 1.5 times the short one; else every step alone) P = a + b A + c A^2,
+Q <- P Q, and between steps R = P A, A <- P R; then X <- Q X. An error of X itself is passed on by at most slope = |p'| (or the
+largest quotient of differences), which a bounds, for each step. All of it is formed from the 64-bit run itself."""
 import pytest
 import torch
 
@@ -14,6 +16,15 @@ COEF = (3.4445, -4.7750, 2.0315)
 U32 = 2.0 ** -24
 
 
+def groups(m, n, steps):
+    first = True
+    while steps > 0:
+        g = min(steps, (2 if first else 3) if 2 * n >= 3 * m else 1)
+        yield g
+        steps -= g
+        first = False
+
+
 def orthogonalise(u, eps, steps, coef, unit):
     """X after the steps in 64 bits, and a bound of the 2-norm (Frobenius) of what rounding does to it."""
     a, b, c = coef
@@ -21,20 +32,42 @@ def orthogonalise(u, eps, steps, coef, unit):
     x = (u.t() if flip else u).contiguous()
     x = x / (x.norm() + eps)
     m, n = x.shape
-    # elements below fp16's normal range (2^-14, of numbers scaled to 2^14 at least) are off by 2^-25 of that scale at most
-    tiny = 2.0 ** -39 * (m * n) ** 0.5
-    err = unit * x.norm() + tiny
-    for _ in range(steps):
-        gram = x @ x.t()
-        big = float(torch.linalg.matrix_norm(x, 2))
-        sums_n, sums_m = (n / 16 + 8) * U32, (m / 16 + 8) * U32
-        e_gram = unit * gram.norm() + sums_n * x.norm() ** 2
-        poly = b * gram + c * gram @ gram
-        e_poly = unit * poly.norm() + (abs(b) + 2 * abs(c) * big ** 2) * e_gram + sums_m * abs(c) * gram.norm() ** 2
-        new = a * x + poly @ x
-        slope = max(abs(a), 2.0)
-        err = slope * err + big * e_poly + sums_m * poly.norm() * x.norm() + unit * new.norm() + 4 * U32 * new.norm() + tiny
-        x = new
+    eye = torch.eye(m, dtype=torch.float64, device=x.device)
+    # every matrix is a polynomial of X: its largest singular value is that of X's singular values
+    s = torch.linalg.svdvals((x @ x.t()).cpu()).clamp(min=0).sqrt()
+
+    def two(v):
+        return float(v.abs().max())
+
+    def kept(t, v, terms):
+        """Rounding of a product of `terms` terms that is kept: its own, and its sums' (their absolute terms in `terms[1]`).
+        Elements below fp16's normal range (numbers scaled to 2^14 at least) are off by 2^-25 of that scale at most."""
+        k, size = terms
+        return unit * float(t.norm()) + (k / 16 + 8) * U32 * size + 2.0 ** -39 * t.numel() ** 0.5 * max(1.0, two(v))
+    slope = max(abs(a), 2.0)
+    err = kept(x, s, (0, 0.0))
+    for g in groups(m, n, steps):
+        gram, l = x @ x.t(), s ** 2
+        e_a = kept(gram, l, (n, float(x.norm()) ** 2))
+        q, v, e_q = eye, torch.ones_like(s), 0.0
+        for i in range(g):
+            p, w = a * eye + b * gram + c * gram @ gram, a + b * l + c * l ** 2
+            e_p = (abs(b) + 2 * abs(c) * two(l)) * e_a + kept(p, w, (m, abs(c) * float(gram.norm()) ** 2))
+            if i == 0:
+                new_q, e_q = p, e_p
+            else:
+                new_q = p @ q
+                e_q = two(w) * e_q + two(v) * e_p + kept(new_q, w * v, (m, float(p.norm() * q.norm())))
+            if i + 1 < g:
+                r = p @ gram
+                e_r = two(w) * e_a + two(l) * e_p + kept(r, w * l, (m, float(p.norm() * gram.norm())))
+                new = p @ r
+                e_a = two(w) * e_r + two(w * l) * e_p + kept(new, w * w * l, (m, float(p.norm() * r.norm())))
+                gram, l = new, w * w * l
+            q, v = new_q, v * w
+        new = q @ x
+        err = slope ** g * err + two(s) * e_q + kept(new, s * v, (m, float(q.norm() * x.norm()))) + 4 * U32 * float(new.norm())
+        x, s = new, s * v
     return (x.t() if flip else x), float(err)
 
 
