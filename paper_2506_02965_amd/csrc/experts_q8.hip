@@ -10,7 +10,7 @@
 #include "expert_ops.h"
 
 #include <algorithm>
-#include <cstdlib>
+#include <cmath>
 
 namespace pcmoe {
 
@@ -148,27 +148,23 @@ struct Q8Args {
   const int8_t *wg, *wu, *wd;
   const float *sg, *su, *sd;
   bf16* y;            // [R][d]
-  int32_t *prefix, *tail;  // [G + 1] each; no tails: null
-  int bm;             // rows of an m-tile
+  int32_t *prefix, *tail, *mid, *few;  // [G + 1] each: m-tiles of 256 rows but the tails, tails, m-tiles of 128 and of 64 rows
 };
 
-// Codes of the rows of x_perm and x; the last workgroup makes the m-tile prefix of the groups, with tails (last m-tiles of at
-// most half their rows) in a prefix of their own where they take another tile.
+// Codes of the rows of x_perm and x; the last workgroup makes the m-tile prefixes of the groups, a wavefront each.
 __global__ __launch_bounds__(Q8_THREADS) void q8_rows_x_kernel(Q8Args a) {
   const int r = blockIdx.x;
   if (r == (int)gridDim.x - 1) {
-    if (threadIdx.x >= 128) return;
-    const int lane = threadIdx.x & 63, tails = threadIdx.x >> 6;  // the second wavefront: the tails
-    if (tails && !a.tail) return;
-    int32_t* out = tails ? a.tail : a.prefix;
+    const int lane = threadIdx.x & 63, which = threadIdx.x >> 6, bm = which < 2 ? 256 : which == 2 ? 128 : 64;
+    int32_t* out = which == 0 ? a.prefix : which == 1 ? a.tail : which == 2 ? a.mid : a.few;
     const int G = a.ga.Eloc + a.ga.S;
     int carry = 0;
     if (lane == 0) out[0] = 0;
     for (int g0 = 0; g0 < G; g0 += 64) {
       const int g = g0 + lane;
       const int rows = g < a.ga.Eloc ? a.ga.offsets[g + 1] - a.ga.offsets[g] : g < G ? a.ga.T : 0;
-      const int rem = rows % a.bm, is_tail = a.tail && rem > 0 && 2 * rem <= a.bm ? 1 : 0;
-      int v = tails ? is_tail : (rows + a.bm - 1) / a.bm - is_tail;
+      const int rem = rows % 256, is_tail = which < 2 && rem > 0 && rem <= 128 ? 1 : 0;
+      int v = which == 1 ? is_tail : (rows + bm - 1) / bm - is_tail;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
         const int u = __shfl_up(v, o, 64);
@@ -200,103 +196,204 @@ __device__ __forceinline__ float sigmoid_of(float g) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_fmaf(e, 0.693147181f * r, e));
 }
 
-// Gate and up (DOWN = false): half of a wavefront's columns are gate rows, the other half the up rows of the same columns of
-// H. Down: y.
+// A tile's operands. Gate and up (DOWN = false): half of a wavefront's columns are gate rows, the other half the up rows of the
+// same columns of H. Down: columns of y.
 template <typename S, bool DOWN>
-__device__ __forceinline__ void q8_tile(const Q8Args& a, const TileIdx& ti, int m0, char* smem) {
+struct Q8Tile {
+  static constexpr int HALF = S::WTN / 2;
+  int32x4 ra, rb0, rb1;
+  int K, m0, n0, at;
+  size_t rs;         // the group's first row in the row space
+  const float* sa;   // its rows' scales
+  int g, rows;
+  __device__ __forceinline__ Q8Tile(const Q8Args& a, const TileIdx& ti, int first) {
+    const int d = a.ga.d, f = a.ga.f;
+    K = DOWN ? f : d;
+    g = ti.g;
+    rows = ti.rows;
+    m0 = first;
+    n0 = DOWN ? ti.nt * S::BN : ti.nt * (S::BN / 2);  // first column of the output
+    const bool routed = g < a.ga.Eloc;
+    rs = routed ? (size_t)ti.row0 : (size_t)a.ga.rows_cap + (size_t)(g - a.ga.Eloc) * a.ga.T;
+    const size_t rx = routed ? (size_t)ti.row0 : (size_t)a.ga.rows_cap;  // among the codes of x
+    sa = DOWN ? a.sh + rs : a.sx + rx;
+    ra = make_rsrc(DOWN ? a.hq + rs * f : a.xq + rx * d, (uint32_t)((size_t)rows * K));
+    const size_t w = (size_t)g * f * d;
+    rb0 = make_rsrc((DOWN ? a.wd : a.wg) + w, (uint32_t)((size_t)f * d));
+    rb1 = DOWN ? rb0 : make_rsrc(a.wu + w, (uint32_t)((size_t)f * d));
+    at = nt_lane(K);
+  }
+  __device__ __forceinline__ NtSrc a_rows(int kt, int j) const { return {ra, (m0 + 8 * j) * K + at + kt * NT_ROWB}; }
+  __device__ __forceinline__ NtSrc b_rows(int kt, int j) const {
+    if (DOWN) return {rb0, (n0 + 8 * j) * K + at + kt * NT_ROWB};
+    const int r = 8 * j, w = r / S::WTN, in = r % S::WTN;
+    return {pick_rsrc(in >= HALF, rb0, rb1), (n0 + w * HALF + in % HALF) * K + at + kt * NT_ROWB};
+  }
+  // Whether this wavefront has something to compute, and whether all its rows and columns are there.
+  __device__ __forceinline__ bool live(const Q8Args& a) const {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    return m0 + wave / S::WN * S::WTM < rows && (!DOWN || n0 + wave % S::WN * S::WTN < a.ga.d);
+  }
+  __device__ __forceinline__ bool full() const {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    return m0 + wave / S::WN * S::WTM + S::WTM <= rows;
+  }
+};
+
+// Scales and stores of a tile. `meanwhile` is called between the loads of the scales and everything else.
+template <typename S, bool DOWN, typename F>
+__device__ __forceinline__ void q8_store(const Q8Args& a, const Q8Tile<S, DOWN>& t, I8::acc (&acc)[S::FM][S::FN], bool live,
+                                         F&& meanwhile) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::WN, wn = wave % S::WN, q = lane >> 4, li = lane & 15;
-  const int d = a.ga.d, f = a.ga.f, K = DOWN ? f : d;
-  const bool routed = ti.g < a.ga.Eloc;
-  const int shared = ti.g - a.ga.Eloc;
-  // the group's first row: in the row space, and among the codes of x
-  const size_t rs = routed ? (size_t)ti.row0 : (size_t)a.ga.rows_cap + (size_t)shared * a.ga.T;
-  const size_t rx = routed ? (size_t)ti.row0 : (size_t)a.ga.rows_cap;
-  const int8_t* ap = DOWN ? a.hq + rs * f : a.xq + rx * d;
-  const float* sa = DOWN ? a.sh + rs : a.sx + rx;
-  const int32x4 ra = make_rsrc(ap, (uint32_t)((size_t)ti.rows * K));
-  const size_t wat = (size_t)ti.g * f * d;
-  const uint32_t w_bytes = (uint32_t)((size_t)f * d);
-  const int32x4 rb0 = make_rsrc((DOWN ? a.wd : a.wg) + wat, w_bytes), rb1 = make_rsrc((DOWN ? a.wd : a.wu) + wat, w_bytes);
-  constexpr int HALF = S::WTN / 2;
-  const int n0 = DOWN ? ti.nt * S::BN : ti.nt * (S::BN / 2);  // first column of the output
-  const int at = nt_lane(K);
-  const bool live = m0 + wm * S::WTM < ti.rows && (!DOWN || n0 + wn * S::WTN < d);
-  I8::acc acc[S::FM][S::FN];
-  nt_loop<S, I8>(
-      smem, K / NT_ROWB, live,
-      [&](int kt, int j) { return NtSrc{ra, (m0 + 8 * j) * K + at + kt * NT_ROWB}; },
-      [&](int kt, int j) {
-        if (DOWN) return NtSrc{rb0, (n0 + 8 * j) * K + at + kt * NT_ROWB};
-        const int r = 8 * j, w = r / S::WTN, in = r % S::WTN;
-        return NtSrc{pick_rsrc(in >= HALF, rb0, rb1), (n0 + w * HALF + in % HALF) * K + at + kt * NT_ROWB};
-      },
-      acc);
+  const int d = a.ga.d, f = a.ga.f, HALF = S::WTN / 2;
+  const int m = t.m0 + wm * S::WTM + li, n = t.n0 + wn * (DOWN ? S::WTN : HALF) + 4 * q;
+  float s[S::FM];
+  floatx4 sw[S::FN];  // down: of the columns; else gate's, then up's
+  if (live) {
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i) s[i] = m + 16 * i < t.rows ? t.sa[m + 16 * i] : 0.f;
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) {
+      const float* from = DOWN ? a.sd + (size_t)t.g * d + n + 16 * j
+                               : (j < S::FN / 2 ? a.sg : a.su) + (size_t)t.g * f + n + 16 * (j % (S::FN / 2));
+      sw[j] = *reinterpret_cast<const floatx4*>(from);
+    }
+  }
+  meanwhile();
   if (!live) return;
 #pragma unroll
   for (int i = 0; i < S::FM; ++i) {
-    const int m = m0 + wm * S::WTM + 16 * i + li;
-    if (m >= ti.rows) continue;
-    const float s = sa[m];
+    if constexpr (S::PIPE) __builtin_amdgcn_sched_barrier(0);  // one row of blocks out of the accumulators at a time
+    if (m + 16 * i >= t.rows) continue;
     if (DOWN) {
 #pragma unroll
       for (int j = 0; j < S::FN; ++j) {
-        const int n = n0 + wn * S::WTN + 16 * j + 4 * q;
-        const floatx4 sw = *reinterpret_cast<const floatx4*>(a.sd + (size_t)ti.g * d + n);
         float o[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (float)acc[i][j][e] * (s * sw[e]);
-        *reinterpret_cast<uint2*>(a.y + (rs + m) * d + n) = uint2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+        for (int e = 0; e < 4; ++e) o[e] = (float)acc[i][j][e] * (s[i] * sw[j][e]);
+        *reinterpret_cast<uint2*>(a.y + (t.rs + m + 16 * i) * d + n + 16 * j) = uint2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
       }
     } else {
 #pragma unroll
       for (int j = 0; j < S::FN / 2; ++j) {
-        const int n = n0 + wn * HALF + 16 * j + 4 * q;
-        const floatx4 sg = *reinterpret_cast<const floatx4*>(a.sg + (size_t)ti.g * f + n);
-        const floatx4 su = *reinterpret_cast<const floatx4*>(a.su + (size_t)ti.g * f + n);
         floatx4 o;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float g = (float)acc[i][j][e] * (s * sg[e]), u = (float)acc[i][j + S::FN / 2][e] * (s * su[e]);
+          const float g = (float)acc[i][j][e] * (s[i] * sw[j][e]);
+          const float u = (float)acc[i][j + S::FN / 2][e] * (s[i] * sw[j + S::FN / 2][e]);
           o[e] = g * sigmoid_of(g) * u;
         }
-        *reinterpret_cast<floatx4*>(a.h + (rs + m) * f + n) = o;
+        *reinterpret_cast<floatx4*>(a.h + (t.rs + m + 16 * i) * f + n + 16 * j) = o;
       }
     }
   }
 }
 
-// A tail (at most half of the rows) of a 256-row tile takes a tile of 128 rows.
+// One tile a workgroup.
 template <typename S, bool DOWN>
 __global__ __launch_bounds__(S::NT) void q8_gemm_kernel(Q8Args a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   TileIdx ti;
   if (!decode_tile<true>(a.ga, blockIdx.x, ti)) return;
-  const int m0 = ti.mt * S::BM;
-  if constexpr (S::PIPE && S::BM == 256) {
-    if (2 * (ti.rows - m0) <= S::BM) {
-      q8_tile<NtShape<S::BM / 2, S::BN, 2, 2, 2>, DOWN>(a, ti, m0, smem);
-      return;
-    }
-  }
-  q8_tile<S, DOWN>(a, ti, m0, smem);
+  const Q8Tile<S, DOWN> t(a, ti, ti.mt * S::BM);
+  const bool live = t.live(a);
+  I8::acc acc[S::FM][S::FN];
+  nt_loop<S, I8>(
+      smem, t.K / NT_ROWB, live, [&](int kt, int j) { return t.a_rows(kt, j); }, [&](int kt, int j) { return t.b_rows(kt, j); },
+      acc);
+  q8_store<S, DOWN>(a, t, acc, live, [] {});
 }
 
-typedef NtShape<256, 256, 2, 2, 2> Q8Large;
-typedef NtShape<64, 128, 2, 2, 3> Q8b;
-typedef NtShape<64, 128, 2, 2, 2> Q8c;
-typedef NtShape<32, 128, 1, 4, 4> Q8d;
-typedef NtShape<128, 128, 2, 2, 4> Q8e;
-typedef NtShape<64, 64, 2, 2, 4> Q8f;
-typedef NtShape<64, 256, 2, 4, 2> Q8g;
-typedef NtShape<32, 64, 1, 2, 4> Q8h;
-typedef NtShape<128, 256, 2, 2, 2> Q8p;
-typedef NtShape<64, 256, 1, 4, 3> Q8q;
-typedef NtShape<128, 128, 2, 4, 2> Q8r;
-typedef NtShape<128, 128, 2, 2, 2> Q8Small;
+// Workgroups that stay, one a CU, and walk over the tiles of their XCD: 256 x 256, and 128 x 256 for tails (a group's last rows,
+// at most 128), which come after the others. The next tile's first loads are issued before a tile is stored.
+template <bool DOWN>
+__global__ __launch_bounds__(256) void q8_walk_kernel(Q8Args a) {
+  typedef NtShape<256, 256, 2, 2, 2> S;
+  typedef NtShape<128, 256, 2, 2, 2> St;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  int* const plan = reinterpret_cast<int*>(smem + S::LDS);  // prefix of the tiles, of the tails, row offsets: 512 each
+  const int G = a.ga.Eloc + a.ga.S, lane = threadIdx.x & 63;
+  for (int i = threadIdx.x; i < 512; i += 256) {
+    plan[i] = i <= G ? a.prefix[i] : 0x7fffffff;
+    plan[512 + i] = i <= G ? a.tail[i] : 0x7fffffff;
+    plan[1024 + i] = i <= a.ga.Eloc ? a.ga.offsets[i] : 0;
+  }
+  __syncthreads();
+  const int nt = a.ga.n_tiles, x = blockIdx.x & 7, stride = gridDim.x >> 3;
+  const int body = __builtin_amdgcn_readfirstlane(plan[G]) * nt, tails = __builtin_amdgcn_readfirstlane(plan[512 + G]) * nt;
+  const int nb = body / 8 + (x < body % 8 ? 1 : 0), nx = tails / 8 + (x < tails % 8 ? 1 : 0);  // of this XCD
+  const int b0 = x * (body / 8) + min(x, body % 8), t0 = x * (tails / 8) + min(x, tails % 8);
+  // Tile i of this XCD; false past the last.
+  const auto decode = [&](int i, TileIdx& ti, bool& tail) __attribute__((always_inline)) {
+    if (i >= nb + nx) return false;
+    tail = i >= nb;
+    const int L = tail ? t0 + i - nb : b0 + i;
+    const int* pre = plan + (tail ? 512 : 0);
+    const int mt = L / nt;   // among all m-tiles of its kind
+    int g = 0;               // the last group whose prefix is at most mt
+    for (int s = 0; s < G; s += 64) g += __popcll(__ballot(s + lane >= 1 && s + lane < G && pre[s + lane] <= mt));
+    g = __builtin_amdgcn_readfirstlane(g);
+    ti.g = g;
+    const bool routed = g < a.ga.Eloc;
+    ti.row0 = routed ? __builtin_amdgcn_readfirstlane(plan[1024 + g]) : 0;
+    ti.rows = routed ? __builtin_amdgcn_readfirstlane(plan[1024 + g + 1]) - ti.row0 : a.ga.T;
+    const int first = __builtin_amdgcn_readfirstlane(plan[g]), count = __builtin_amdgcn_readfirstlane(plan[g + 1]) - first;
+    if (tail) {
+      ti.mt = count;  // after the group's others
+      ti.nt = L - mt * nt;
+    } else {  // m-tiles in bunches of GROUP_M per n-tile
+      const int l = L - first * nt, blk = l / (GROUP_M * nt), rem = l - blk * GROUP_M * nt, n = min(GROUP_M, count - blk * GROUP_M);
+      ti.nt = rem / n;
+      ti.mt = blk * GROUP_M + rem % n;
+    }
+    ti.mt = __builtin_amdgcn_readfirstlane(ti.mt);
+    ti.nt = __builtin_amdgcn_readfirstlane(ti.nt);
+    return true;
+  };
+  const auto fill = [&](const TileIdx& ti, bool tail) __attribute__((always_inline)) {
+    if (tail) {
+      const Q8Tile<St, DOWN> t(a, ti, ti.mt * 256);
+      nt_fill<St>(smem, t.K / NT_ROWB, [&](int kt, int j) { return t.a_rows(kt, j); }, [&](int kt, int j) { return t.b_rows(kt, j); });
+    } else {
+      const Q8Tile<S, DOWN> t(a, ti, ti.mt * 256);
+      nt_fill<S>(smem, t.K / NT_ROWB, [&](int kt, int j) { return t.a_rows(kt, j); }, [&](int kt, int j) { return t.b_rows(kt, j); });
+    }
+  };
+  TileIdx ti, next;
+  bool tail = false, next_tail = false, behind = false;
+  int i = blockIdx.x >> 3;
+  bool more = decode(i, ti, tail);
+  if (more) fill(ti, tail);
+  while (more) {
+    i += stride;
+    const bool there = decode(i, next, next_tail);
+    const auto tile = [&](auto shape) __attribute__((always_inline)) {
+      using Sh = decltype(shape);
+      const Q8Tile<Sh, DOWN> t(a, ti, ti.mt * 256);
+      const bool live = t.live(a);
+      I8::acc acc[Sh::FM][Sh::FN];
+      nt_pipe<Sh, I8>(
+          smem, t.K / NT_ROWB, live, behind, [&](int kt, int j) { return t.a_rows(kt, j); },
+          [&](int kt, int j) { return t.b_rows(kt, j); }, acc);
+      q8_store<Sh, DOWN>(a, t, acc, live, [&]() __attribute__((always_inline)) {
+        if (there) fill(next, next_tail);
+      });
+      behind = live && t.full();
+    };
+    if (tail) tile(St{});
+    else tile(S{});
+    more = there;
+    ti = next;
+    tail = next_tail;
+  }
+}
+
+typedef NtShape<128, 128, 2, 4, 2> Q8Mid;   // two workgroups a CU
+typedef NtShape<64, 128, 2, 2, 3> Q8Few;
 
 struct Q8Layout {
-  size_t sx, prefix, tail, h, hq, sh, bytes;
+  size_t sx, prefix, tail, mid, few, h, hq, sh, bytes;
 };
 Q8Layout q8_layout(const moe_desc& d) {
   Q8Layout l;
@@ -304,11 +401,44 @@ Q8Layout q8_layout(const moe_desc& d) {
   l.sx = align256(rx * d.d_model);
   l.prefix = l.sx + align256(rx * 4);
   l.tail = l.prefix + align256((d.local_count + d.n_shared + 1) * 4);
-  l.h = l.tail + align256((d.local_count + d.n_shared + 1) * 4);
+  const size_t plan = l.tail - l.prefix;
+  l.mid = l.tail + plan;
+  l.few = l.mid + plan;
+  l.h = l.few + plan;
   l.hq = l.h + align256(R * d.d_ff * 4);
   l.sh = l.hq + align256(R * d.d_ff);
   l.bytes = l.sh + align256(R * 4);
   return l;
+}
+
+// An upper bound of the m-tiles of bm rows, and what to expect of them: half a tile of each group is empty.
+int64_t most_tiles(const moe_desc& d, int bm) {
+  const int64_t of_all = (d.T + bm - 1) / bm;
+  return std::min((int64_t)d.T * d.top_k / bm + d.local_count, d.local_count * of_all) + d.n_shared * of_all;
+}
+double mean_rows(const moe_desc& d) {
+  return ((double)d.T * d.top_k / d.n_experts * d.local_count + (double)d.T * d.n_shared) / (d.local_count + d.n_shared);
+}
+double expected_tiles(const moe_desc& d, int bm) {
+  return (d.local_count + d.n_shared) * (mean_rows(d) / bm + 0.5);
+}
+
+// Which tiles a contraction takes.
+//   Few rows a group: 64 x 128, two workgroups a CU with two K-tiles of weights on their way each. Fewer than 64 rows, or so few
+//   tiles that 128 x 128 ones would leave CUs idle.
+//   Else by the rounds of the chip and what a tile costs (us): 1.55 a K-tile and 10 for the 256 x 256 tiles, 1.15 and 3 for the
+//   128 x 128 tiles, two at once.
+// us of gate and up / down for 64-row, 128-row and 256-row tiles (d, f, experts: rows an expert):
+//   4096, 14336, 8:  6: 158/81  172/113  188/145;  75: 237/130  196/124  216/156;  250: 424/242  369/246  335/198;
+//                    500: 798/413  623/346  522/322
+//   1024, 2816, 16:  32: 22/18  23/19  32/25;  97: 32/18  27/22  35/28;  375: 85/38  62/31  69/44
+//   2048, 1408, 64:  12: 73/39  76/41  86/46;  96: 104/61  98/54  107/56;  384: 275/161  224/140  222/129
+enum Q8Tiles { Q8_FEW, Q8_MID, Q8_LARGE };
+Q8Tiles pick_tiles(const moe_desc& d, bool down) {
+  const double kts = (down ? d.d_ff : d.d_model) / 128., cus = device_cus(), n = down ? d.d_model : 2. * d.d_ff;
+  const double large = expected_tiles(d, 256) * std::ceil(n / 256), mid = expected_tiles(d, 128) * std::ceil(n / 128);
+  if (mean_rows(d) < 64 || mid <= cus) return Q8_FEW;
+  return std::ceil(large / cus) * (1.55 * kts + 10) <= std::ceil(mid / (2 * cus)) * (1.15 * kts + 3) ? Q8_LARGE : Q8_MID;
 }
 
 template <typename S, bool DOWN>
@@ -317,12 +447,19 @@ hipError_t q8_gemm(const char* name, const moe_desc& d, Q8Args a, hipStream_t s)
   const auto kern = q8_gemm_kernel<S, DOWN>;
   if (hipError_t e = lds_limit_once((const void*)kern, S::LDS, done); e != hipSuccess) return e;
   a.ga.n_tiles = DOWN ? (d.d_model + S::BN - 1) / S::BN : d.d_ff / (S::BN / 2);
-  const int64_t most = std::min((int64_t)d.T * d.top_k / S::BM + d.local_count,
-                                (int64_t)d.local_count * ((d.T + S::BM - 1) / S::BM)) +
-                       (int64_t)d.n_shared * ((d.T + S::BM - 1) / S::BM);
   KernelTimer kt(name, s);
-  // every XCD takes its share of the tiles and of the tails, each rounded up: at most two tiles more than an eighth of all
-  hipLaunchKernelGGL(kern, dim3((unsigned)(most * a.ga.n_tiles / 8 * 8 + 16)), dim3(S::NT), S::LDS, s, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)((most_tiles(d, S::BM) * a.ga.n_tiles + 7) / 8 * 8)), dim3(S::NT), S::LDS, s, a);
+  return hipGetLastError();
+}
+template <bool DOWN>
+hipError_t q8_walk(const char* name, const moe_desc& d, Q8Args a, hipStream_t s) {
+  static std::atomic<uint64_t> done{0};
+  const auto kern = q8_walk_kernel<DOWN>;
+  constexpr int lds = NtShape<256, 256, 2, 2, 2>::LDS + 3 * 512 * 4;
+  if (hipError_t e = lds_limit_once((const void*)kern, lds, done); e != hipSuccess) return e;
+  a.ga.n_tiles = DOWN ? (d.d_model + 255) / 256 : d.d_ff / 128;
+  KernelTimer kt(name, s);
+  hipLaunchKernelGGL(kern, dim3(std::max(8, device_cus() / 8 * 8)), dim3(256), lds, s, a);
   return hipGetLastError();
 }
 
@@ -371,8 +508,9 @@ hipError_t launch_ffn_q8(const moe_desc& d, const void* x, const void* xp, const
   a.ga.rows_cap = d.T * d.top_k;
   a.ga.offsets = offsets;
   a.prefix = (int32_t*)(base + l.prefix);
-  a.ga.mt_prefix = a.prefix;
-  a.tail = nullptr;
+  a.tail = (int32_t*)(base + l.tail);
+  a.mid = (int32_t*)(base + l.mid);
+  a.few = (int32_t*)(base + l.few);
   a.x = x;
   a.xp = xp;
   a.xq = (int8_t*)base;
@@ -387,16 +525,6 @@ hipError_t launch_ffn_q8(const moe_desc& d, const void* x, const void* xp, const
   a.su = (const float*)up.scales;
   a.sd = (const float*)down.scales;
   a.y = (bf16*)yp;
-  // rows per expert
-  const double rows = (double)d.T * d.top_k / d.n_experts;
-  bool large = rows >= 192;
-  const char* e = getenv("Q8_TILE");
-  const char shape = e ? e[0] : large ? 'l' : 's';
-  large = shape == 'l';
-  a.bm = large ? 256 : 128;
-  if (shape == 'b' || shape == 'c' || shape == 'f' || shape == 'g' || shape == 'q') a.bm = 64;
-  if (shape == 'd' || shape == 'h') a.bm = 32;
-  if (large) a.ga.mt_tail = a.tail = (int32_t*)(base + l.tail);
   const int rx = d.T * d.top_k + (d.n_shared ? d.T : 0);
   {
     KernelTimer kt("q8_rows_x", s);
@@ -405,20 +533,10 @@ hipError_t launch_ffn_q8(const moe_desc& d, const void* x, const void* xp, const
   }
   const auto gemm = [&](const char* name, auto down) {
     constexpr bool D = decltype(down)::value;
-    switch (shape) {
-      case 'l': return q8_gemm<Q8Large, D>(name, d, a, s);
-      case 'b': return q8_gemm<Q8b, D>(name, d, a, s);
-      case 'c': return q8_gemm<Q8c, D>(name, d, a, s);
-      case 'd': return q8_gemm<Q8d, D>(name, d, a, s);
-      case 'e': return q8_gemm<Q8e, D>(name, d, a, s);
-      case 'f': return q8_gemm<Q8f, D>(name, d, a, s);
-      case 'g': return q8_gemm<Q8g, D>(name, d, a, s);
-      case 'p': return q8_gemm<Q8p, D>(name, d, a, s);
-      case 'q': return q8_gemm<Q8q, D>(name, d, a, s);
-      case 'r': return q8_gemm<Q8r, D>(name, d, a, s);
-      case 'h': return q8_gemm<Q8h, D>(name, d, a, s);
-    }
-    return q8_gemm<Q8Small, D>(name, d, a, s);
+    const Q8Tiles tiles = pick_tiles(d, D);
+    a.ga.mt_prefix = tiles == Q8_FEW ? a.few : a.mid;
+    if (tiles == Q8_LARGE) return q8_walk<D>(name, d, a, s);
+    return tiles == Q8_MID ? q8_gemm<Q8Mid, D>(name, d, a, s) : q8_gemm<Q8Few, D>(name, d, a, s);
   };
   if (hipError_t e = gemm("q8_gate_up", std::false_type{}); e != hipSuccess) return e;
   {

@@ -18,7 +18,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 
 namespace pcmoe {
 
@@ -95,9 +94,10 @@ __device__ __forceinline__ f16 part_of(float v, bool second) {
 template <typename T, bool PRECISE>
 __global__ __launch_bounds__(256) void muon_normalise_kernel(MuonArgs a) {
   constexpr int EP = EPC<T>::value;
-  const int mat = blockIdx.y, tensor = mat / a.G;
+  // the last rows of the last matrices first: they are what the pass before this left in the last-level cache
+  const int mat = (int)gridDim.y - 1 - (int)blockIdx.y, tensor = mat / a.G;
   const int rows = tensor == 2 ? a.d : a.f, cols = tensor == 2 ? a.f : a.d;
-  const int tr = blockIdx.x / (cols / 64), tc = blockIdx.x % (cols / 64);
+  const int l = (int)gridDim.x - 1 - (int)blockIdx.x, tr = l / (cols / 64), tc = l % (cols / 64);
   __shared__ double norm2;
   __shared__ f16 tile[PRECISE ? 2 : 1][64][72];
   const size_t at = (size_t)mat * a.d * a.f;
@@ -471,10 +471,10 @@ hipError_t ns_launch(const char* name, NsArgs a, hipStream_t s) {
   int64_t tiles = ns_tiles<S, MODE>(a);
   a.whole = (int)tiles;
   if (S::PIPE) {
-    // A last round of few tiles is split into quarters, which take about 0.4 of a tile's time each.
+    // A last round of few tiles is split into quarters, which take about 0.4 of a tile's time each (six matrices of 4096 rows, 816
+    // tiles of 3.2 rounds, K = 14336: 1402 us, 1236 with the last 48 in quarters; K = 4096: 425, 394).
     const int64_t cus = device_cus(), rest = tiles % cus;
-    static const char* noq = getenv("NS_NOQ");
-    if (!noq && 4 * rest <= 2 * cus) {
+    if (4 * rest <= 2 * cus) {
       a.whole = (int)(tiles - rest);
       tiles += 3 * rest;
     }
@@ -494,11 +494,6 @@ hipError_t ns_product(const char* name, const NsArgs& a, bool precise, hipStream
   const int64_t cus = device_cus();
   const auto rounds = [&](int64_t tiles, int64_t slots) { return (double)((tiles + slots - 1) / slots); };
   const double large = rounds(ns_tiles<NsLarge, MODE>(a), cus) * 4 / 1.4, small = rounds(ns_tiles<NsSmall, MODE>(a), 2 * cus) * 2;
-  if (const char* force = getenv("NS_TILE")) {
-    if (force[0] == 'l') return go(NsLarge{});
-    if (force[0] == 's') return go(NsSmall{});
-    return go(NsTiny{});
-  }
   if (ns_tiles<NsTiny, MODE>(a) <= cus) return go(NsTiny{});
   return large <= small ? go(NsLarge{}) : go(NsSmall{});
 }
@@ -558,18 +553,16 @@ double largest_factor(double c0, double c1, double c2, double top) {
   }
   return most;
 }
-// Steps that are taken on A before X is formed again.
-int muon_group(const MuonLayout& l, int done, int steps) {
-  int g = 1;
-  const char* e = getenv("NS_PLAN");
-  const char* plan = e ? e : (2 * l.n >= 3 * l.m ? "23" : "1");
-  int at = 0;
-  for (int i = 0; ; ++i) {
-    g = plan[i] - '0';
-    if (at == done || !plan[i + 1]) break;
-    at += g;
-  }
-  return std::min(g, steps - done);
+// Steps that are taken on A before X is formed again, after `done` of `steps`. A group of g steps costs m^2 n + 2 m^2 n + (4 g -
+// 3) m^3 operations, g steps one by one g (3 m^2 n + m^3): a longer group saves where n is above m. It also multiplies what
+// rounding has done to A's small eigenvalues by a^2 a step. Off the 64-bit X of random matrices with four directions 0.5 / 3 /
+// 20 times the others' size (1024 x 2816): one by one 0.9e-3 / 1.9e-3 / 9.9e-3, groups of 2, 2, 1: 1.3e-3 / 1.6e-3 / 8.2e-3, of
+// 2, 3: 1.1e-3 / 3.3e-3 / 9.5e-3, of five: 1e-3 / 0.1 (a simulation). In two parts: 1.2e-6 / 1.6e-6 / 8.1e-6, 1.7e-6 / 1.2e-6 /
+// 5.7e-6, 1.4e-6 / 3.6e-6 / 6.9e-6 (fp32 products 3.5e-6 / 2.3e-6 / 1.2e-5). Two at first, when A's eigenvalues span most, then
+// three, and two at most in the precise form.
+int muon_group(const MuonLayout& l, bool precise, int done, int steps) {
+  if (2 * l.n < 3 * l.m) return 1;
+  return std::min(done == 0 || precise ? 2 : 3, steps - done);
 }
 // The power of two that takes values of up to `top` below 2^15.
 double two_to(double top) {
@@ -640,7 +633,7 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
   double top = 1.0;   // of X's singular values
   int turn = 0;
   for (int done = 0; done < o.steps;) {
-    const int group = muon_group(l, done, o.steps);
+    const int group = muon_group(l, o.precise != 0, done, o.steps);
     const bool last = done + group == o.steps;
     // A = X X^T
     NsArgs n{};

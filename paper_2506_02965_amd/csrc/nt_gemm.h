@@ -122,8 +122,27 @@ __device__ __forceinline__ void nt_ring(char* smem, int ktiles, bool live, LA&& 
 // 8192 x 14336 x 8192 bytes of K, products alone: 1,320 TFLOP/s fp16 and 2,650 TOP/s int8, against 980 and 1,980 of the
 // 128 x 128 tiles, and 1,260 and 2,460 of the same loop with eight wavefronts of 128 x 64, whose fragments pass LDS 1.5 times
 // as often.
+// A workgroup that goes on to another tile calls nt_fill for it before the epilogue of the last one, so that its first two
+// K-tiles are under way meanwhile; `behind` says that the wavefront has issued at least 16 stores since.
+template <typename S, typename LA, typename LB>
+__device__ __forceinline__ void nt_load(uint32_t base, int ktiles, int kt, int l, LA&& src_a, LB&& src_b) {
+  constexpr int OOR = 0x7fffffff;  // no operand has 2^31 bytes
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t st = base + (kt & 1) * S::STAGE;
+  const NtSrc s = l < S::IA ? src_a(kt, wave + S::NW * l) : src_b(kt, wave + S::NW * (l - S::IA));
+  const uint32_t dst = l < S::IA ? st + (wave + S::NW * l) * 1024 : st + S::A_BYTES + (wave + S::NW * (l - S::IA)) * 1024;
+  dma16(s.rsrc, dst, kt < ktiles ? s.off : OOR);
+}
+template <typename S, typename LA, typename LB>
+__device__ __forceinline__ void nt_fill(char* smem, int ktiles, LA&& src_a, LB&& src_b) {
+  const uint32_t base = lds_addr(smem);
+#pragma unroll
+  for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+    for (int l = 0; l < S::IA + S::IB; ++l) nt_load<S>(base, ktiles, kt, l, src_a, src_b);
+}
 template <typename S, typename E, typename LA, typename LB>
-__device__ __forceinline__ void nt_pipe(char* smem, int ktiles, bool live, LA&& src_a, LB&& src_b,
+__device__ __forceinline__ void nt_pipe(char* smem, int ktiles, bool live, bool behind, LA&& src_a, LB&& src_b,
                                         typename E::acc (&acc)[S::FM][S::FN]) {
   static_assert(S::STAGES == 2, "two stages");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -131,13 +150,7 @@ __device__ __forceinline__ void nt_pipe(char* smem, int ktiles, bool live, LA&& 
   const uint32_t base = lds_addr(smem);
   constexpr int LOADS = S::IA + S::IB, NF = S::FM + S::FN, NM = S::FM * S::FN;
   constexpr int RS = NM / NF, LS = NM / LOADS;  // MFMAs for each read, and for each load
-  constexpr int OOR = 0x7fffffff;               // no operand has 2^31 bytes
-  const auto load = [&](int kt, int l) {
-    const uint32_t st = base + (kt & 1) * S::STAGE;
-    const NtSrc s = l < S::IA ? src_a(kt, wave + S::NW * l) : src_b(kt, wave + S::NW * (l - S::IA));
-    const uint32_t dst = l < S::IA ? st + (wave + S::NW * l) * 1024 : st + S::A_BYTES + (wave + S::NW * (l - S::IA)) * 1024;
-    dma16(s.rsrc, dst, kt < ktiles ? s.off : OOR);
-  };
+  const auto load = [&](int kt, int l) { nt_load<S>(base, ktiles, kt, l, src_a, src_b); };
   const int at0 = li * NT_ROWB + ((q ^ (li & 7)) << 4), at1 = li * NT_ROWB + (((4 + q) ^ (li & 7)) << 4);
   const char* a0 = smem + wm * S::WTM * NT_ROWB;
   const char* b0 = smem + S::A_BYTES + wn * S::WTN * NT_ROWB;
@@ -157,11 +170,8 @@ __device__ __forceinline__ void nt_pipe(char* smem, int ktiles, bool live, LA&& 
   for (int i = 0; i < S::FM; ++i)
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) acc[i][j] = typename E::acc{0, 0, 0, 0};
-#pragma unroll
-  for (int l = 0; l < LOADS; ++l) load(0, l);
-#pragma unroll
-  for (int l = 0; l < LOADS; ++l) load(1, l);
-  wait_vmcnt<LOADS>();
+  if (behind) wait_vmcnt<16>();  // the loads are older than the last 16 stores
+  else wait_vmcnt<0>();
   asm volatile("s_barrier" ::: "memory");
   if (!live) {
     for (int kt = 0; kt < ktiles; ++kt) {
@@ -189,7 +199,7 @@ __device__ __forceinline__ void nt_pipe(char* smem, int ktiles, bool live, LA&& 
       }
     }
   }
-  wait_vmcnt<0>();  // the loads past the last K-tile have landed before the epilogue uses the LDS
+  wait_vmcnt<0>();  // the loads past the last K-tile have landed before the LDS is used again
   asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");  // the last MFMAs' results are ready to read
   __syncthreads();
 }
@@ -197,8 +207,12 @@ __device__ __forceinline__ void nt_pipe(char* smem, int ktiles, bool live, LA&& 
 template <typename S, typename E, typename LA, typename LB>
 __device__ __forceinline__ void nt_loop(char* smem, int ktiles, bool live, LA&& src_a, LB&& src_b,
                                         typename E::acc (&acc)[S::FM][S::FN]) {
-  if constexpr (S::PIPE) nt_pipe<S, E>(smem, ktiles, live, src_a, src_b, acc);
-  else nt_ring<S, E>(smem, ktiles, live, src_a, src_b, acc);
+  if constexpr (S::PIPE) {
+    nt_fill<S>(smem, ktiles, src_a, src_b);
+    nt_pipe<S, E>(smem, ktiles, live, false, src_a, src_b, acc);
+  } else {
+    nt_ring<S, E>(smem, ktiles, live, src_a, src_b, acc);
+  }
 }
 
 // Byte offset of a lane's chunk within a direct load whose rows are ld bytes apart.

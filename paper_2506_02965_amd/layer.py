@@ -5,8 +5,10 @@ Forward (Alg. 3 with the gating of Alg. 7 and the experts of Alg. 6):
 Backward (Alg. 5 / Alg. 6 and the owner-side router adjoint):
     moe_combine_bwd -> moe_expert_ffn_bwd -> moe_route_bwd (full layer only) -> moe_permute_bwd
 With a gate, moe_route_gated and moe_route_gated_bwd take the place of the routing calls. With checkpoint=True the forward
-ends in moe_ffn_checkpoint and the backward begins with moe_ffn_restore. forward_q4 runs the experts from 4-bit weights.
-Expert update (the last step of Alg. 6): moe_expert_update over the hosted experts' weights.
+ends in moe_ffn_checkpoint and the backward begins with moe_ffn_restore. forward_q4 runs the experts from 4-bit weights,
+forward_q8 in 8-bit integers.
+Expert update (the last step of Alg. 6): moe_expert_update over the hosted experts' weights, or moe_expert_update_muon.
+MoEStack chains layers with moe_residual_norm between them, and their adjoints.
 All calls are enqueued on one stream; no per-expert count ever returns to the host.
 """
 from __future__ import annotations
@@ -72,6 +74,28 @@ class Q4Experts:
         return Q4Experts(group, one(w.w_gate), one(w.w_up), one(w.w_down))
 
 
+@dataclass
+class Q8Experts:
+    """8-bit codes and channel scales of the experts' gate, up and down projections."""
+    gate: tuple
+    up: tuple
+    down: tuple
+
+    @staticmethod
+    def pack(w: LayerWeights) -> "Q8Experts":
+        names = {torch.bfloat16: "bf16", torch.float32: "f32"}
+
+        def one(t):
+            if t.dtype not in names:
+                raise ValueError(f"weights of dtype {t.dtype}: bfloat16 or float32 are packed")
+            n, rows, cols = t.shape
+            codes = torch.empty(n, rows, cols, dtype=torch.int8, device=t.device)
+            scales = torch.empty(n, rows, dtype=torch.float32, device=t.device)
+            P.moe_q8_pack(n, rows, cols, names[t.dtype], t, codes, scales)
+            return codes, scales
+        return Q8Experts(one(w.w_gate), one(w.w_up), one(w.w_down))
+
+
 class MoELayer:
     """gate: a pcmoe.make_gate(...) for gated routing. checkpoint: keep the activations of the backward in 8 bits;
     `saved`, the buffer of their full form, may then be shared by layers that run one after the other: at least
@@ -107,8 +131,9 @@ class MoELayer:
         self.saved = ws(P.MOE_WS_FFN_SAVED) if saved is None else saved
         if checkpoint:
             self.ckpt = ws(P.MOE_WS_FFN_CKPT)
-        self.ws_q4 = None   # of forward_q4, allocated by its first call
-        self.saved_nothing = False  # the last forward was forward_q4
+        self.ws_q4 = None   # of forward_q4 and forward_q8, allocated by their first calls
+        self.ws_q8 = None
+        self.saved_nothing = False  # the last forward was forward_q4 or forward_q8
         self.ws_ffn_fwd = ws(P.MOE_WS_FFN_FWD)
         if self.backward_enabled:
             G = Eloc + S
@@ -180,10 +205,26 @@ class MoELayer:
         self.combine()
         return self.y
 
+    def forward_q8(self, w: LayerWeights, q: Q8Experts):
+        """The forward of a bf16 layer with the experts in 8-bit integers (inference, prompts above all: nothing is saved, no
+        backward can follow; w's expert weights are not read and may be None)."""
+        if self.cfg.dtype != "bf16":
+            raise ValueError("experts in 8-bit integers are for bf16 layers")
+        if self.ws_q8 is None:
+            self.ws_q8 = torch.empty(P.moe_workspace_size(self.desc, P.MOE_WS_FFN_Q8), dtype=torch.uint8,
+                                     device=self.device)
+        self.saved_nothing = True
+        self.route(w)
+        self.permute(w)
+        P.moe_expert_ffn_q8(self.desc, w.x, self.x_perm, self.offsets, *q.gate, *q.up, *q.down, self.y_perm, self.ws_q8,
+                            self.ws_q8.numel())
+        self.combine()
+        return self.y
+
     # ----------------------------------------------------------------- backward
     def _need_saved(self):
         if self.saved_nothing:
-            raise RuntimeError("the last forward was forward_q4, which saves nothing for a backward")
+            raise RuntimeError("the last forward was forward_q4 or forward_q8, which save nothing for a backward")
 
     def combine_bwd(self, dy):
         P.moe_combine_bwd(self.desc, dy, self.y_perm, self.slot_to_row, self.topk_w, self.dy_perm, self.dgate)
@@ -226,14 +267,17 @@ class MoELayer:
         kw = dict(device=self.device, dtype=torch.float32)
         self.opt_m = torch.zeros(n, **kw)
         self.opt_v = torch.zeros(n, **kw)
-        self.opt_master = None
-        if master:  # filled slice by slice: no transient copy of all parameters
-            self.opt_master = torch.empty(n, **kw)
-            o = 0
-            for t in (w.w_gate, w.w_up, w.w_down):
-                self.opt_master[o:o + t.numel()].copy_(t.reshape(-1))
-                o += t.numel()
+        self.opt_master = self._master(w) if master else None
         self.opt_step = 0
+
+    def _master(self, w: LayerWeights):
+        parts = (w.w_gate, w.w_up, w.w_down)
+        out = torch.empty(sum(t.numel() for t in parts), device=self.device, dtype=torch.float32)
+        o = 0
+        for t in parts:  # filled slice by slice: no transient copy of all parameters
+            out[o:o + t.numel()].copy_(t.reshape(-1))
+            o += t.numel()
+        return out
 
     def update(self, w: LayerWeights, opt: "P.moe_opt"):
         """One optimiser step of the hosted experts from the gradients of the last backward."""
@@ -242,8 +286,131 @@ class MoELayer:
         P.moe_expert_update(self.desc, opt, w.w_gate, w.w_up, w.w_down, self.dw_gate, self.dw_up, self.dw_down,
                             self.opt_master, self.opt_m, self.opt_v)
 
+    def init_muon_state(self, w: LayerWeights, master: bool = True, precise: bool = False):
+        """State of update_muon: a zero momentum, the workspace and, if asked, a master copy of the current weights. precise:
+        for updates with precise=True, whose workspace is twice the size."""
+        n = w.w_gate.numel() + w.w_up.numel() + w.w_down.numel()
+        self.muon_m = torch.zeros(n, device=self.device, dtype=torch.float32)
+        self.muon_master = self._master(w) if master else None
+        which = P.MOE_WS_UPDATE_MUON_PRECISE if precise else P.MOE_WS_UPDATE_MUON
+        self.ws_muon = torch.empty(P.moe_workspace_size(self.desc, which), dtype=torch.uint8, device=self.device)
+
+    def update_muon(self, w: LayerWeights, opt: "P.moe_muon"):
+        """One step of the hosted experts along their orthogonalised momentum, from the gradients of the last backward."""
+        P.moe_expert_update_muon(self.desc, opt, w.w_gate, w.w_up, w.w_down, self.dw_gate, self.dw_up, self.dw_down,
+                                 self.muon_master, self.muon_m, self.ws_muon, self.ws_muon.numel())
+
     def n_local_rows(self) -> int:
         return int(self.offsets[-1].item())
+
+
+@dataclass
+class NormWeights:
+    """Weights of what stands between two blocks; None: all ones (the gate: none)."""
+    w_post: Optional[torch.Tensor] = None   # [d]
+    gate: Optional[torch.Tensor] = None     # [gate_groups, d]
+    w_pre: Optional[torch.Tensor] = None    # [d]
+
+
+class ResidualNorm:
+    """Between two blocks: r = alpha x + gate * post(y), h = pre(r), and the adjoint. norm: a pcmoe.make_norm(...). first: before
+    the first block, where there is no y. ws: a workspace of the adjoint to share, MOE_WS_NORM_BWD bytes at least."""
+
+    def __init__(self, T, d, norm, dtype="bf16", device="cuda", first=False, backward=True, ws=None):
+        self.desc = P.make_desc(T, d, 128, 1, 1, dtype=dtype)
+        self.norm, self.first, self.shape, self.dt = norm, first, (T, d), torch_dtype(dtype)
+        new = lambda: torch.empty(T, d, dtype=self.dt, device=device)
+        self.r = None if first else new()
+        self.h = new() if norm.pre != P.MOE_NORM_NONE else None
+        self.device, self.backward_enabled = device, backward
+        if backward:
+            self.dx = new()
+            self.dy = None if first else new()
+            need = P.moe_workspace_size(self.desc, P.MOE_WS_NORM_BWD)
+            self.ws = torch.empty(need, dtype=torch.uint8, device=device) if ws is None else ws
+        self.dw_post = self.dgate = self.dw_pre = None   # fp32, allocated by the first backward
+
+    def _check(self, what, t, shape, dtype=None):
+        if t is not None and (tuple(t.shape) != shape or t.dtype != (dtype or self.dt)):
+            raise ValueError(f"{what}: {tuple(t.shape)} {t.dtype}, expected {shape} {dtype or self.dt}")
+
+    def _check_weights(self, w: NormWeights):
+        d = self.shape[1]
+        self._check("w_post", w.w_post, (d,))
+        self._check("w_pre", w.w_pre, (d,))
+        self._check("gate", w.gate, (self.norm.gate_groups, d))
+
+    def forward(self, w: NormWeights, x, y=None):
+        """r and h (r is x before the first block; h is None without a pre norm). x and y are read again by the backward."""
+        self._check_weights(w)
+        self._check("x", x, self.shape)
+        self._check("y", y, self.shape)
+        P.moe_residual_norm(self.desc, self.norm, x, y, w.w_post, w.gate, w.w_pre, self.r, self.h)
+        self.y, self.r_of_backward = y, x if self.first else self.r
+        return self.r_of_backward, self.h
+
+    def backward(self, w: NormWeights, dr, dh):
+        """dx and dy of the last forward; the weights' gradients are left in dw_post, dgate and dw_pre."""
+        self._check_weights(w)
+        self._check("dr", dr, self.shape)
+        self._check("dh", dh, self.shape)
+        for name, t in (("dw_post", w.w_post), ("dgate", w.gate), ("dw_pre", w.w_pre)):
+            if t is None:
+                setattr(self, name, None)
+            elif getattr(self, name) is None:
+                setattr(self, name, torch.empty(t.shape, dtype=torch.float32, device=self.device))
+        P.moe_residual_norm_bwd(self.desc, self.norm, dr, dh, self.y, self.r_of_backward, w.w_post, w.gate, w.w_pre, self.dx,
+                                self.dy, self.dw_post, self.dgate, self.dw_pre, self.ws, self.ws.numel())
+        return self.dx, self.dy
+
+
+class MoEStack:
+    """Layers one after the other with norms, gates and the residual stream around them:
+        r_0 = x, h_0 = pre(r_0);  y_i = layer_i(h_i);  r_i+1 = alpha r_i + gate_i+1 * post(y_i), h_i+1 = pre(r_i+1)
+    with `final` in place of pre at the end. The result is the last h, or the last r where final is "none". layers: MoELayers of
+    one T, d and dtype. forward takes the layers' weights (whose x it sets) and len(layers) + 1 NormWeights."""
+
+    def __init__(self, layers, pre="rms", post="none", final="rms", eps=1e-6, residual_scale=1.0, gate_groups=1):
+        if not layers:
+            raise ValueError("a stack needs a layer")
+        if len({id(l) for l in layers}) < len(layers):
+            raise ValueError("a layer holds the activations of one place of a stack: the same layer twice")
+        cfg = layers[0].cfg
+        for l in layers:
+            if (l.cfg.T, l.cfg.d, l.cfg.dtype) != (cfg.T, cfg.d, cfg.dtype):
+                raise ValueError("the layers of a stack share T, d and dtype")
+        if pre == "none":
+            raise ValueError("a stack norms the input of its layers: pre is 'rms' or 'layer'")
+        self.layers = list(layers)
+        self.backward_enabled = all(l.backward_enabled for l in layers)
+        self.norms, ws = [], None
+        for i in range(len(layers) + 1):
+            norm = P.make_norm(final if i == len(layers) else pre, post if i else "none", eps, residual_scale if i else 1.0,
+                               gate_groups)
+            self.norms.append(ResidualNorm(cfg.T, cfg.d, norm, cfg.dtype, layers[0].device, first=i == 0,
+                                           backward=self.backward_enabled, ws=ws))
+            ws = getattr(self.norms[-1], "ws", None)
+
+    def forward(self, x, ws, ns, experts=None):
+        """experts: a Q4Experts or Q8Experts for each layer, to run the experts from (no backward can follow)."""
+        r, h = self.norms[0].forward(ns[0], x)
+        for i, (layer, w) in enumerate(zip(self.layers, ws)):
+            w.x = h
+            if experts is None:
+                y = layer.forward(w)
+            else:
+                y = (layer.forward_q8 if isinstance(experts[i], Q8Experts) else layer.forward_q4)(w, experts[i])
+            r, h = self.norms[i + 1].forward(ns[i + 1], r, y)
+        return r if h is None else h
+
+    def backward(self, d, ws, ns):
+        """The gradient of x from that of forward's result. Layers leave the gradients of their weights in their buffers, the
+        norms in theirs."""
+        dr, dh = (d, None) if self.norms[-1].h is None else (None, d)
+        for i in reversed(range(len(self.layers))):
+            dr, dy = self.norms[i + 1].backward(ns[i + 1], dr, dh)
+            dh = self.layers[i].backward(ws[i], dy)
+        return self.norms[0].backward(ns[0], dr, dh)[0]
 
 
 def training_footprint(cfg, local_count: int, master: bool = True, checkpoint: bool = False,

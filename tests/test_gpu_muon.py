@@ -3,7 +3,8 @@
 Tolerances are on the 2-norm of an update matrix. With u the relative rounding of every matrix that is kept (2^-11, half a
 step of fp16; 2^-21 where each is held in two parts) and products that sum K terms in fp32 (K / 16 + 8 roundings of 2^-24),
 errors are followed to first order through the products that the library takes: A = X X^T, and for the steps of a group (two
-steps, then three at a time, where the long side is 1.5 times the short one; else every step alone) P = a + b A + c A^2,
+steps, then three at a time, or two in the precise form, where the long side is 1.5 times the short one; else every step
+alone) P = a + b A + c A^2,
 Q <- P Q, and between steps R = P A, A <- P R; then X <- Q X. An error of X itself is passed on by at most slope = |p'| (or the
 largest quotient of differences), which a bounds, for each step. All of it is formed from the 64-bit run itself."""
 import pytest
@@ -16,10 +17,10 @@ COEF = (3.4445, -4.7750, 2.0315)
 U32 = 2.0 ** -24
 
 
-def groups(m, n, steps):
+def groups(m, n, steps, precise):
     first = True
     while steps > 0:
-        g = min(steps, (2 if first else 3) if 2 * n >= 3 * m else 1)
+        g = min(steps, (2 if first or precise else 3) if 2 * n >= 3 * m else 1)
         yield g
         steps -= g
         first = False
@@ -46,7 +47,7 @@ def orthogonalise(u, eps, steps, coef, unit):
         return unit * float(t.norm()) + (k / 16 + 8) * U32 * size + 2.0 ** -39 * t.numel() ** 0.5 * max(1.0, two(v))
     slope = max(abs(a), 2.0)
     err = kept(x, s, (0, 0.0))
-    for g in groups(m, n, steps):
+    for g in groups(m, n, steps, unit < 2.0 ** -20):
         gram, l = x @ x.t(), s ** 2
         e_a = kept(gram, l, (n, float(x.norm()) ** 2))
         q, v, e_q = eye, torch.ones_like(s), 0.0
