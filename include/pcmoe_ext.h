@@ -217,7 +217,7 @@ typedef struct {
  *   w_*, dw_*, master   as for moe_expert_update;  m  fp32 [P] momentum, updated in place
  *   ws   MOE_WS_UPDATE_MUON bytes of scratch, with precise = 1 MOE_WS_UPDATE_MUON_PRECISE bytes
  * MOE_ERR_INVALID_ARGUMENT for a setting outside the ranges stated in moe_muon; MOE_ERR_UNSUPPORTED for coefficients by which
- * a singular value of [0, 1] can pass 16. Calls that overlap on the same parameters or workspace race.
+ * a singular value of [0, 1] can pass 16, and for precise = 1 with d_model * d_ff >= 2^29. Calls that overlap on the same parameters or workspace race.
  */
 moe_status moe_expert_update_muon(const moe_desc* desc, const moe_muon* opt, void* w_gate, void* w_up, void* w_down,
                                   const void* dw_gate, const void* dw_up, const void* dw_down, float* master, float* m,

@@ -573,6 +573,8 @@ moe_status moe_expert_update_muon(const moe_desc* d, const moe_muon* opt, void* 
   if (st || (st = check_muon(opt))) return st;
   NEED(w_gate); NEED(w_up); NEED(w_down); NEED(dw_gate); NEED(dw_up); NEED(dw_down); NEED(m);
   if (master) NEED(master);
+  if (opt->precise && (int64_t)d->d_model * d->d_ff * 4 >= (int64_t)1 << 31)  // both parts of a matrix are one buffer
+    return fail(MOE_ERR_UNSUPPORTED, "a %d x %d matrix in two fp16 parts exceeds 2 GiB", d->d_ff, d->d_model);
   NEED_WS(ws_bytes, update_muon_ws_bytes(*d, opt->precise != 0));
   return hip_status(launch_expert_update_muon(*d, *opt, w_gate, w_up, w_down, dw_gate, dw_up, dw_down, master, m, ws,
                                               stream),

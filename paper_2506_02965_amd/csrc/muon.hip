@@ -37,8 +37,7 @@ struct MuonArgs {
   float mu;
   int nesterov;
   double eps;
-  f16 *x, *xt;       // [3 G][m][n], [3 G][n][m], then the second parts
-  size_t plane;      // elements of a part
+  f16 *x, *xt;       // [3 G][parts][m][n], [3 G][parts][n][m]
   float s0;          // power of two of the first X
   int wide_first;    // gate and up are wide (f <= d)
 };
@@ -100,7 +99,7 @@ __global__ __launch_bounds__(256) void muon_normalise_kernel(MuonArgs a) {
   const int l = (int)gridDim.x - 1 - (int)blockIdx.x, tr = l / (cols / 64), tc = l % (cols / 64);
   __shared__ double norm2;
   __shared__ f16 tile[PRECISE ? 2 : 1][64][72];
-  const size_t at = (size_t)mat * a.d * a.f;
+  const size_t at = (size_t)mat * a.d * a.f, part = (size_t)a.d * a.f, at_x = at * (PRECISE ? 2 : 1);
   if (threadIdx.x < 64) {
     double s = a.part[(size_t)mat * SUM_BLOCKS + threadIdx.x];
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
@@ -133,21 +132,20 @@ __global__ __launch_bounds__(256) void muon_normalise_kernel(MuonArgs a) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int task = threadIdx.x + 256 * k, r = task >> 3, c = (task & 7) * 8;
-      st_chunk(straight + p * a.plane + at + (size_t)(tr * 64 + r) * cols + tc * 64 + c,
+      st_chunk(straight + at_x + p * part + (size_t)(tr * 64 + r) * cols + tc * 64 + c,
                *reinterpret_cast<const Chunk*>(&tile[p][r][c]));
       half8 v;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = tile[p][c + e][r];
-      st_chunk(turned + p * a.plane + at + (size_t)(tc * 64 + r) * rows + tr * 64 + c, __builtin_bit_cast(Chunk, v));
+      st_chunk(turned + at_x + p * part + (size_t)(tc * 64 + r) * rows + tr * 64 + c, __builtin_bit_cast(Chunk, v));
     }
 }
 
-// One product of every matrix: out = alpha P Q^T (+ beta D + diag on the diagonal), P [M][K], Q [N][K], D and out [M][N].
+// One product of every matrix: out = alpha P Q^T (+ beta D + diag on the diagonal), P [M][K], Q [N][K], D and out [M][N]; in the
+// precise form each matrix is followed by its second part.
 struct NsArgs {
   const f16 *p, *q, *d;
   f16 *out, *out_t;        // out, and its transpose [N][M]
-  size_t p_mat, q_mat, o_mat;        // elements of a matrix
-  size_t p_plane, q_plane, o_plane;  // ... of a part
   int M, N, K, mats;
   int whole;               // tiles that are not split into quarters
   float alpha, beta, diag;
@@ -195,14 +193,12 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::WN, wn = wave % S::WN, q = lane >> 4, li = lane & 15;
   const int ld = a.K * 2;
-  const f16 *p0 = a.p + mat * a.p_mat, *q0 = (other ? a.q2 : a.q) + mat * a.q_mat;
-  const uint32_t p_bytes = (uint32_t)a.M * ld, q_bytes = (uint32_t)a.N * ld;
-  const int32x4 rp = make_rsrc(p0, p_bytes), rq = make_rsrc(q0, q_bytes);
-  int32x4 rp1 = rp, rq1 = rq;
-  if (PRECISE) {
-    rp1 = make_rsrc(p0 + a.p_plane, p_bytes);
-    rq1 = make_rsrc(q0 + a.q_plane, q_bytes);
-  }
+  constexpr int PARTS = PRECISE ? 2 : 1;
+  // Both parts of a matrix are one buffer, so that choosing between them is an offset. (A row past the first part's end, of which
+  // nothing is stored, reads the second's.)
+  const uint32_t p_part = (uint32_t)a.M * ld, q_part = (uint32_t)a.N * ld;
+  const int32x4 rp = make_rsrc(a.p + mat * ((size_t)PARTS * a.M * a.K), PARTS * p_part);
+  const int32x4 rq = make_rsrc((other ? a.q2 : a.q) + mat * ((size_t)PARTS * a.N * a.K), PARTS * q_part);
   const int kts = a.K / 64, at = nt_lane(ld);
   // the wavefronts' parts lie on either side of a matrix's end, not across it: the sides are multiples of 128
   const bool live = m0 + wm * S::WTM < a.M && n0 + wn * S::WTN < a.N;
@@ -212,20 +208,21 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
       smem, PRECISE ? 3 * kts : kts, live,
       [&](int kt, int j) {
         const int seg = PRECISE ? (kt >= 2 * kts ? 2 : kt >= kts ? 1 : 0) : 0;
-        return NtSrc{PRECISE ? pick_rsrc(seg == 1, rp, rp1) : rp, (m0 + 8 * j) * ld + at + (kt - seg * kts) * NT_ROWB};
+        return NtSrc{rp, (m0 + 8 * j) * ld + at + (kt - seg * kts) * NT_ROWB + (PRECISE && seg == 1 ? (int)p_part : 0)};
       },
       [&](int kt, int j) {
         const int seg = PRECISE ? (kt >= 2 * kts ? 2 : kt >= kts ? 1 : 0) : 0;
-        return NtSrc{PRECISE ? pick_rsrc(seg == 0, rq, rq1) : rq, (n0 + 8 * j) * ld + at + (kt - seg * kts) * NT_ROWB};
+        return NtSrc{rq, (n0 + 8 * j) * ld + at + (kt - seg * kts) * NT_ROWB + (PRECISE && seg == 0 ? (int)q_part : 0)};
       },
       acc);
   if (!live) return;
   const int mr = m0 + wm * S::WTM, nc = n0 + wn * S::WTN;  // the wavefront's part
+  const size_t part = (size_t)a.M * a.N;                     // elements of a part of the result
 
   if constexpr (MODE == NS_LAST) {
     const int tensor = mat / a.G;
-    const size_t at_w = (size_t)(mat % a.G) * a.o_mat;
-    float* mp = a.master ? a.master + (size_t)tensor * a.G * a.o_mat + at_w : nullptr;
+    const size_t at_w = (size_t)(mat % a.G) * part;
+    float* mp = a.master ? a.master + (size_t)tensor * a.G * part + at_w : nullptr;
     void* const w = tensor == 0 ? a.w[0] : tensor == 1 ? a.w[1] : a.w[2];
     float* wf = (float*)w + at_w;
     bf16* wb = (bf16*)w + at_w;
@@ -298,7 +295,7 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
 #pragma unroll
               for (int e = 0; e < 4; ++e) st[(16 * j + 4 * q + e) * PITCH + 16 * i + li] = acc[i][half * (S::FN / 2) + j][e];
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-          constexpr int TASKS = S::WTN / 2 * CH / 64, AHEAD = TASKS < 4 ? TASKS : 4;
+          constexpr int ALL = S::WTN / 2 * CH, TASKS = (ALL + 63) / 64, AHEAD = TASKS < 4 ? TASKS : 4;
 #pragma unroll 1
           for (int k0 = 0; k0 < TASKS; k0 += AHEAD) {
             Chunk c[AHEAD][2];
@@ -307,11 +304,12 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
             for (int k = 0; k < AHEAD; ++k) {
               const int task = lane + 64 * (k0 + k);
               o[k] = (size_t)(nc + half * (S::WTN / 2) + task / CH) * a.M + mr + (task % CH) * 8;
-              fetch(o[k], c[k]);
+              if (ALL % 64 == 0 || task < ALL) fetch(o[k], c[k]);
             }
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
               const int task = lane + 64 * (k0 + k);
+              if (ALL % 64 != 0 && task >= ALL) continue;
               const float* from = st + (task / CH) * PITCH + (task % CH) * 8;
               float v[8];
               chunk_to_f<float>(ld_chunk(from), v);
@@ -332,10 +330,10 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
     }
     return;
   } else {
-    f16* out = (other ? a.out2 : a.out) + mat * a.o_mat;
-    f16* out_t = (MODE == NS_SYMMETRIC ? (other ? a.out2 : a.out) : a.out_t) + mat * a.o_mat;
+    f16* out = (other ? a.out2 : a.out) + mat * PARTS * part;
+    f16* out_t = (MODE == NS_SYMMETRIC ? (other ? a.out2 : a.out) : a.out_t) + mat * PARTS * part;
     const float alpha = other ? a.alpha2 : a.alpha;
-    const f16* d0 = MODE == NS_SYMMETRIC && a.d ? a.d + mat * a.o_mat : nullptr;
+    const f16* d0 = MODE == NS_SYMMETRIC && a.d ? a.d + mat * PARTS * part : nullptr;
     const bool turn = MODE == NS_BOTH || m0 != n0;
     constexpr int PITCH = NsLds<S, MODE>::PITCH;
     uint32_t* st = reinterpret_cast<uint32_t*>(smem + wave * NsLds<S, MODE>::WAVE);
@@ -362,7 +360,7 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
 #pragma unroll
           for (int j = 0; j < S::FN; ++j) {
             dv[j] = *reinterpret_cast<const half4*>(d0 + o + 16 * j);
-            if (PRECISE) d1[j] = *reinterpret_cast<const half4*>(d0 + a.o_plane + o + 16 * j);
+            if (PRECISE) d1[j] = *reinterpret_cast<const half4*>(d0 + part + o + 16 * j);
           }
 #pragma unroll
           for (int j = 0; j < S::FN; ++j)
@@ -380,7 +378,7 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
           Chunk c;
 #pragma unroll
           for (int e = 0; e < 4; ++e) c.w[e] = pack_f16(v[2 * e], v[2 * e + 1], p != 0);
-          st_chunk(out + p * a.o_plane + (size_t)(mr + 16 * i + row) * a.N + nc + 32 * j + 16 * (q & 1) + 8 * (q >> 1), c);
+          st_chunk(out + p * part + (size_t)(mr + 16 * i + row) * a.N + nc + 32 * j + 16 * (q & 1) + 8 * (q >> 1), c);
         }
         // by columns, through LDS: neighbouring lanes (rows m and m + 1) exchange halves, the even one keeps columns 0 and 1 of
         // its four, the odd one 2 and 3
@@ -401,19 +399,22 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
 #pragma unroll
       for (int k = 0; k < S::WTN * CH / 64; ++k) {
         const int task = lane + 64 * k, r = task / CH, c = task % CH;
-        st_chunk(out_t + p * a.o_plane + (size_t)(nc + r) * a.M + mr + 8 * c, ld_chunk(st + r * PITCH + 4 * c));
+        st_chunk(out_t + p * part + (size_t)(nc + r) * a.M + mr + 8 * c, ld_chunk(st + r * PITCH + 4 * c));
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
   }
 }
 
-// 256 x 256 tiles with one wavefront per SIMD, 128 x 128 tiles two workgroups a CU, and 64 x 64 tiles with a deep ring; and the
-// quarters of 256 x 256 tiles, which share a launch with them.
+// 256 x 256 tiles with one wavefront per SIMD, 128 x 128 tiles two workgroups a CU, and the quarters of 256 x 256 tiles, which
+// share a launch with them. While all tiles are multiplied at once a launch is bound by latencies, the more K-tiles on their way
+// the better: 64 x 64 tiles, and 32 x 32 tiles with up to 18 K-tiles (three matrices of 384 rows, K = 384 in two parts: 7.0 us a
+// launch, with 64 x 64 tiles of four or eight wavefronts 10.4 and 8.1; an empty launch is 1.5).
 typedef NtShape<256, 256, 2, 2, 2> NsLarge;
 typedef NtShape<128, 128, 2, 2, 4> NsQuarter;
 typedef NtShape<128, 128, 2, 2, 2> NsSmall;
-typedef NtShape<64, 64, 2, 2, 8> NsTiny;
+typedef NtShape<64, 64, 4, 2, 8, 2> NsTiny;
+typedef NtShape<32, 32, 2, 1, 18, 6> NsTiniest;
 
 // Tile l of a grid of `tm` x `tn` tiles of every matrix (for symmetric products, of those on and above the diagonal).
 template <int MODE>
@@ -494,13 +495,13 @@ hipError_t ns_product(const char* name, const NsArgs& a, bool precise, hipStream
   const int64_t cus = device_cus();
   const auto rounds = [&](int64_t tiles, int64_t slots) { return (double)((tiles + slots - 1) / slots); };
   const double large = rounds(ns_tiles<NsLarge, MODE>(a), cus) * 4 / 1.4, small = rounds(ns_tiles<NsSmall, MODE>(a), 2 * cus) * 2;
+  if (ns_tiles<NsTiniest, MODE>(a) <= cus) return go(NsTiniest{});
   if (ns_tiles<NsTiny, MODE>(a) <= cus) return go(NsTiny{});
   return large <= small ? go(NsLarge{}) : go(NsSmall{});
 }
 
 struct MuonLayout {
   int mats, m, n;
-  size_t x_plane, a_plane;  // elements of a part of X and of A
   size_t x, xt[2], a, r, b[3], bytes;  // the partial sums of squares come first
 };
 MuonLayout muon_layout(const moe_desc& d, bool precise) {
@@ -509,19 +510,18 @@ MuonLayout muon_layout(const moe_desc& d, bool precise) {
   l.m = std::min(d.d_model, d.d_ff);
   l.n = std::max(d.d_model, d.d_ff);
   const size_t parts = precise ? 2 : 1;
-  l.x_plane = (size_t)l.mats * l.m * l.n;
-  l.a_plane = (size_t)l.mats * l.m * l.m;
+  const size_t all_x = (size_t)l.mats * l.m * l.n, all_a = (size_t)l.mats * l.m * l.m;
   size_t at = align256(sizeof(double) * l.mats * SUM_BLOCKS);
-  const auto take = [&](size_t plane) {
+  const auto take = [&](size_t n) {
     const size_t here = at;
-    at += align256(parts * plane * 2);
+    at += align256(parts * n * 2);
     return here;
   };
-  l.x = take(l.x_plane);
-  for (size_t& o : l.xt) o = take(l.x_plane);
-  l.a = take(l.a_plane);
-  l.r = take(l.a_plane);
-  for (size_t& o : l.b) o = take(l.a_plane);
+  l.x = take(all_x);
+  for (size_t& o : l.xt) o = take(all_x);
+  l.a = take(all_a);
+  l.r = take(all_a);
+  for (size_t& o : l.b) o = take(all_a);
   l.bytes = at;
   return l;
 }
@@ -602,7 +602,6 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
   a.eps = (double)o.eps;
   a.x = (f16*)(base + l.x);
   a.xt = (f16*)(base + l.xt[0]);
-  a.plane = l.x_plane;
   double sx = two_to(1.0);
   a.s0 = (float)sx;
   const bool bf = d.dtype == MOE_BF16;
@@ -629,7 +628,6 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
   f16 *xt[2] = {a.xt, (f16*)(base + l.xt[1])}, *A = (f16*)(base + l.a), *R = (f16*)(base + l.r);
   f16* buf[3];
   for (int i = 0; i < 3; ++i) buf[i] = (f16*)(base + l.b[i]);
-  const size_t mn = (size_t)l.m * l.n, mm = (size_t)l.m * l.m;
   double top = 1.0;   // of X's singular values
   int turn = 0;
   for (int done = 0; done < o.steps;) {
@@ -641,17 +639,11 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
     n.M = n.N = l.m;
     n.K = l.n;
     n.p = n.q = a.x;
-    n.p_mat = n.q_mat = mn;
-    n.p_plane = n.q_plane = l.x_plane;
     n.out = A;
-    n.o_mat = mm;
-    n.o_plane = l.a_plane;
     double sa = two_to(top * top);
     n.alpha = (float)(sa / (sx * sx));
     if (hipError_t e = ns_product<NS_SYMMETRIC>("muon_gram", n, o.precise, s); e != hipSuccess) return e;
     n.K = l.m;
-    n.p_mat = n.q_mat = mm;
-    n.p_plane = n.q_plane = l.a_plane;
     f16 *P = nullptr, *Q = nullptr;
     double sp = 0, sq = 0, tq = 1.0;
     for (int i = 0; i < group; ++i) {
@@ -711,10 +703,6 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
     n.N = l.n;
     n.p = Q;
     n.q = xt[turn];
-    n.q_mat = mn;
-    n.q_plane = l.x_plane;
-    n.o_mat = mn;
-    n.o_plane = l.x_plane;
     const double sn = last ? 1.0 : two_to(top);
     n.alpha = (float)(sn / (sq * sx));
     if (last) {

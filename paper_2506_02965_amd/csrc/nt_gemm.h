@@ -39,9 +39,10 @@ struct I8 {
 
 constexpr int NT_ROWB = 128;  // bytes of a tile row
 
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int TOGETHER_ = 1>
 struct NtShape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
+  static constexpr int TOGETHER = TOGETHER_;              // K-tiles between two barriers of the ring
   static constexpr int NW = WM * WN, NT = 64 * NW;
   static constexpr int WTM = BM / WM, WTN = BN / WN;      // a wavefront's part of the tile
   static constexpr int FM = WTM / 16, FN = WTN / 16;
@@ -85,20 +86,25 @@ __device__ __forceinline__ void nt_ring(char* smem, int ktiles, bool live, LA&& 
   for (int i = 0; i < S::FM; ++i)
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) acc[i][j] = typename E::acc{0, 0, 0, 0};
+  constexpr int G = S::TOGETHER, AHEAD = S::STAGES - G, LOADS = S::IA + S::IB;
+  static_assert(S::STAGES % G == 0 && (AHEAD - G) * LOADS < 64, "whole groups of K-tiles, waited for by count");
 #pragma unroll
-  for (int s = 0; s < S::STAGES - 1; ++s)
+  for (int s = 0; s < AHEAD; ++s)
     if (s < ktiles) issue(s);
-  for (int kt = 0; kt < ktiles; ++kt) {
-    if (kt + S::STAGES - 2 < ktiles) wait_vmcnt<(S::STAGES - 2) * (S::IA + S::IB)>();
+  for (int k0 = 0; k0 < ktiles; k0 += G) {
+    if (k0 + AHEAD <= ktiles) wait_vmcnt<(AHEAD - G) * LOADS>();
     else wait_vmcnt<0>();
-    // every wavefront's loads of kt have landed, and its reads of the stage that is filled next are done
+    // every wavefront's loads of these K-tiles have landed, and its reads of the stages that are filled next are done
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (kt + S::STAGES - 1 < ktiles) issue(kt + S::STAGES - 1);
-    if (!live) continue;
-    const char* As = smem + (kt % S::STAGES) * S::STAGE;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int at = li * NT_ROWB + (((4 * s + q) ^ (li & 7)) << 4);
+    for (int g = 0; g < G; ++g)
+      if (k0 + AHEAD + g < ktiles) issue(k0 + AHEAD + g);
+    if (!live) continue;
+#pragma unroll
+    for (int s = 0; s < 2 * G; ++s) {
+      if (G > 1 && k0 + s / 2 >= ktiles) break;
+      const char* As = smem + ((k0 + s / 2) % S::STAGES) * S::STAGE;
+      const int at = li * NT_ROWB + (((4 * (s & 1) + q) ^ (li & 7)) << 4);
       Chunk a[S::FM], b[S::FN];
 #pragma unroll
       for (int i = 0; i < S::FM; ++i) a[i] = ld_chunk(As + (wm * S::WTM + 16 * i) * NT_ROWB + at);

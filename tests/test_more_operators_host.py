@@ -126,6 +126,8 @@ def test_muon_arguments():
                 refused(INV, P.moe_expert_update_muon, d, o, *a, need)
         refused(WS, P.moe_expert_update_muon, d, o, *good, need - 1)
         refused(INV, P.moe_expert_update_muon, d, o, *good[:8], OK + 128, need)
+    huge = desc(d_model=23296, d_ff=23296, n_experts=1, top_k=1)       # both parts of a matrix are one buffer
+    refused(UNS, P.moe_expert_update_muon, huge, muon(precise=1), *[OK] * 9, 1 << 40)
     # X in both orientations and a turn of one, A and B, for three matrices of every expert
     assert P.moe_workspace_size(d, P.MOE_WS_UPDATE_MUON) >= 2 * 48 * (3 * 256 * 384 + 2 * 256 * 256)
 
