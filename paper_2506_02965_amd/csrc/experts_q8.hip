@@ -390,7 +390,7 @@ __global__ __launch_bounds__(256) void q8_walk_kernel(Q8Args a) {
 }
 
 typedef NtShape<128, 128, 2, 4, 2> Q8Mid;   // two workgroups a CU
-typedef NtShape<64, 128, 2, 2, 3> Q8Few;
+typedef NtShape<64, 128, 2, 4, 3> Q8Few;
 
 struct Q8Layout {
   size_t sx, prefix, tail, mid, few, h, hq, sh, bytes;
@@ -424,15 +424,17 @@ double expected_tiles(const moe_desc& d, int bm) {
 }
 
 // Which tiles a contraction takes.
-//   Few rows a group: 64 x 128, two workgroups a CU with two K-tiles of weights on their way each. Fewer than 64 rows, or so few
-//   tiles that 128 x 128 ones would leave CUs idle.
+//   Few rows a group: 64 x 128, two workgroups of eight wavefronts a CU with two K-tiles of weights on their way each. Fewer than
+//   64 rows, or so few tiles that 128 x 128 ones would leave CUs idle.
 //   Else by the rounds of the chip and what a tile costs (us): 1.55 a K-tile and 10 for the 256 x 256 tiles, 1.15 and 3 for the
 //   128 x 128 tiles, two at once.
 // us of gate and up / down for 64-row, 128-row and 256-row tiles (d, f, experts: rows an expert):
-//   4096, 14336, 8:  6: 158/81  172/113  188/145;  75: 237/130  196/124  216/156;  250: 424/242  369/246  335/198;
-//                    500: 798/413  623/346  522/322
-//   1024, 2816, 16:  32: 22/18  23/19  32/25;  97: 32/18  27/22  35/28;  375: 85/38  62/31  69/44
-//   2048, 1408, 64:  12: 73/39  76/41  86/46;  96: 104/61  98/54  107/56;  384: 275/161  224/140  222/129
+//   4096, 14336, 8:  6: 161/83  172/113  188/145;  75: 237/128  196/124  216/156;  250: 427/240  369/246  335/198;
+//                    500: 783/413  623/346  522/322
+//   1024, 2816, 16:  32: 22/15  23/19  32/25;  97: 28/15  27/22  35/28;  375: 72/35  62/31  69/44
+//   2048, 1408, 64:  12: 71/39  76/41  86/46;  96: 103/60  98/54  107/56;  384: 259/156  224/140  222/129
+// (64 x 128 with four wavefronts: 97 rows of 1024, 2816, 16: 31/18. 64 x 256, 128 x 64, 64 x 64, 32 x 128 and four stages of 128 x
+// 128 tiles, one workgroup a CU, were slower in most cells.)
 enum Q8Tiles { Q8_FEW, Q8_MID, Q8_LARGE };
 Q8Tiles pick_tiles(const moe_desc& d, bool down) {
   const double kts = (down ? d.d_ff : d.d_model) / 128., cus = device_cus(), n = down ? d.d_model : 2. * d.d_ff;

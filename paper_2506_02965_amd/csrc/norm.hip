@@ -367,7 +367,7 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
         }
         if (in) st_chunk((Chunk*)a.dx + row + c, f_to_chunk<T>(o));
       }
-      if (!a.y) continue;
+      if (!a.dy) continue;
       if (POST) {
         s = ly ? block_sum<0, 2>(s, lds, turn) : block_sum<0, 1>(s, lds, turn);
         const float cy = (float)((double)s.f0 * a.inv_d), mb = (float)((double)s.f1 * a.inv_d);

@@ -287,6 +287,18 @@ def test_in_place_strides_and_streams():
     assert torch.equal(h3, h) and torch.equal(r3, r)
 
 
+@pytest.mark.parametrize("pre", ["none", "layer"])
+def test_backward_without_y(pre):
+    """Neither a post norm nor a gate reads y: dy is written without it, and r only where a pre norm reads it."""
+    c = Case(70, 384, pre, "none", alpha=0.5, dtype="bf16")
+    r, _ = c.forward()
+    o = c.backward(r)
+    c.y = None
+    other = c.backward(r if pre != "none" else None)
+    assert torch.equal(o["dx"], other["dx"]) and torch.equal(o["dy"], other["dy"])
+    assert not (o["dy"] == 7.0).all()
+
+
 def test_graph_replays():
     c = Case(130, 640, "layer", "rms", gate=2, dtype="bf16")
     n = P.moe_workspace_size(c.desc, P.MOE_WS_NORM_BWD)

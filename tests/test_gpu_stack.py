@@ -131,6 +131,17 @@ def test_train_update_and_serve(final):
         assert float((got.float() - small[t:t + 1].float()).norm() / small[t:t + 1].float().norm()) < 0.02
 
 
+def test_the_examples_prompt():
+    """The example's prompt through 8-bit experts. x, H and the weights are off by some 1% of a row's size each; tokens for which
+    two experts are nearly equal may take the other."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import gated_experts as G
+    student, _ = G.train(2, 64, log=lambda *a: None)
+    assert G.prompt(student, 130, log=lambda *a: None) < 0.2
+
+
 def test_a_captured_training_step():
     cfg = LayerConfig("s", T=64, d=128, f=256, E=4, k=2)
     ws, ns, normal = make(cfg, 2, 2, seed=5)
