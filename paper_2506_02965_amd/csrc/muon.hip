@@ -31,13 +31,14 @@ struct MuonArgs {
   void* w[3];
   const void* g[3];
   int G;             // experts: matrices of a tensor
+  int mat0;          // the first matrix of this pass, of [gate, up, down][G]
   int d, f;
   float *master, *m; // [3][G][f d]
-  double* part;      // [3 G][SUM_BLOCKS]
+  double* part;      // [matrices of a pass][SUM_BLOCKS]
   float mu;
   int nesterov;
   double eps;
-  f16 *x, *xt;       // [3 G][parts][m][n], [3 G][parts][n][m]
+  f16 *x, *xt;       // [matrices of a pass][parts][m][n], [..][parts][n][m]
   float s0;          // power of two of the first X
   int wide_first;    // gate and up are wide (f <= d)
 };
@@ -51,7 +52,7 @@ __device__ __forceinline__ float update_of(const MuonArgs& a, float g, float m) 
 template <typename T>
 __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonArgs a) {
   constexpr int EP = EPC<T>::value;
-  const int mat = blockIdx.y;
+  const int mat = a.mat0 + (int)blockIdx.y;
   const int64_t n = (int64_t)a.d * a.f / EP;  // chunks
   const Chunk* g = (const Chunk*)a.g[mat / a.G] + (size_t)(mat % a.G) * n;
   float* mm = a.m + (size_t)mat * a.d * a.f;
@@ -80,7 +81,7 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(MuonArgs a) {
     if (threadIdx.x < o) s[threadIdx.x] += s[threadIdx.x + o];
     __syncthreads();
   }
-  if (threadIdx.x == 0) a.part[(size_t)mat * SUM_BLOCKS + blockIdx.x] = s[0];
+  if (threadIdx.x == 0) a.part[(size_t)blockIdx.y * SUM_BLOCKS + blockIdx.x] = s[0];
 }
 
 // fp16 parts of a value: its rounding, and the rounding of the rest.
@@ -94,14 +95,14 @@ template <typename T, bool PRECISE>
 __global__ __launch_bounds__(256) void muon_normalise_kernel(MuonArgs a) {
   constexpr int EP = EPC<T>::value;
   // the last rows of the last matrices first: they are what the pass before this left in the last-level cache
-  const int mat = (int)gridDim.y - 1 - (int)blockIdx.y, tensor = mat / a.G;
+  const int here = (int)gridDim.y - 1 - (int)blockIdx.y, mat = a.mat0 + here, tensor = mat / a.G;
   const int rows = tensor == 2 ? a.d : a.f, cols = tensor == 2 ? a.f : a.d;
   const int l = (int)gridDim.x - 1 - (int)blockIdx.x, tr = l / (cols / 64), tc = l % (cols / 64);
   __shared__ double norm2;
   __shared__ f16 tile[PRECISE ? 2 : 1][64][72];
-  const size_t at = (size_t)mat * a.d * a.f, part = (size_t)a.d * a.f, at_x = at * (PRECISE ? 2 : 1);
+  const size_t at = (size_t)mat * a.d * a.f, part = (size_t)a.d * a.f, at_x = here * part * (PRECISE ? 2 : 1);
   if (threadIdx.x < 64) {
-    double s = a.part[(size_t)mat * SUM_BLOCKS + threadIdx.x];
+    double s = a.part[(size_t)here * SUM_BLOCKS + threadIdx.x];
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     if (threadIdx.x == 0) norm2 = s;
   }
@@ -156,7 +157,7 @@ struct NsArgs {
   // last step: parameters in place of out
   void* w[3];
   float* master;
-  int G, dtype;
+  int mat0, G, dtype;
   int flip_up, flip_down;  // gate and up, down are stored transposed to X
   float decay, step;       // p <- decay p - step X
 };
@@ -220,8 +221,8 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
   const size_t part = (size_t)a.M * a.N;                     // elements of a part of the result
 
   if constexpr (MODE == NS_LAST) {
-    const int tensor = mat / a.G;
-    const size_t at_w = (size_t)(mat % a.G) * part;
+    const int tensor = (a.mat0 + mat) / a.G;
+    const size_t at_w = (size_t)((a.mat0 + mat) % a.G) * part;
     float* mp = a.master ? a.master + (size_t)tensor * a.G * part + at_w : nullptr;
     void* const w = tensor == 0 ? a.w[0] : tensor == 1 ? a.w[1] : a.w[2];
     float* wf = (float*)w + at_w;
@@ -500,8 +501,27 @@ hipError_t ns_product(const char* name, const NsArgs& a, bool precise, hipStream
   return large <= small ? go(NsLarge{}) : go(NsSmall{});
 }
 
+// Matrices taken at a time, from X to the parameters: as few as fill the chip, since the workspace is theirs alone (192 matrices
+// of 1408 x 2048: twelve at a time 0.45 GB and 19.2 ms, all 7.1 GB and 19.0 ms; 48 of 1024 x 2816: 24 at a time 2.65 ms, all
+// 2.70). The least number whose symmetric products take a round of the chip and, 3% aside, no more rounds in all than all
+// matrices at once (a last round in quarters: 0.4, or 0.8 of a round), the last pass at least half full.
+int muon_pass(int m, int mats) {
+  const int64_t tm = (m + 255) / 256, tiles = tm * (tm + 1) / 2, cus = 256;
+  const auto cost = [&](int64_t n) {
+    const int64_t whole = n * tiles / cus, rest = n * tiles % cus;
+    return (double)whole + (rest == 0 ? 0. : 4 * rest <= cus ? 0.4 : 4 * rest <= 2 * cus ? 0.8 : 1.);
+  };
+  for (int n = 1; n < mats; ++n) {
+    const int last = mats % n;
+    if (n * tiles * 10 < cus * 9 || (last && 2 * last < n)) continue;
+    if ((mats / n) * cost(n) + cost(last) <= 1.03 * cost(mats)) return n;
+  }
+  return mats;
+}
+
 struct MuonLayout {
   int mats, m, n;
+  int pass;  // matrices taken at a time
   size_t x, xt[2], a, r, b[3], bytes;  // the partial sums of squares come first
 };
 MuonLayout muon_layout(const moe_desc& d, bool precise) {
@@ -509,9 +529,10 @@ MuonLayout muon_layout(const moe_desc& d, bool precise) {
   l.mats = 3 * (d.local_count + d.n_shared);
   l.m = std::min(d.d_model, d.d_ff);
   l.n = std::max(d.d_model, d.d_ff);
+  l.pass = muon_pass(l.m, l.mats);
   const size_t parts = precise ? 2 : 1;
-  const size_t all_x = (size_t)l.mats * l.m * l.n, all_a = (size_t)l.mats * l.m * l.m;
-  size_t at = align256(sizeof(double) * l.mats * SUM_BLOCKS);
+  const size_t all_x = (size_t)l.pass * l.m * l.n, all_a = (size_t)l.pass * l.m * l.m;
+  size_t at = align256(sizeof(double) * l.pass * SUM_BLOCKS);
   const auto take = [&](size_t n) {
     const size_t here = at;
     at += align256(parts * n * 2);
@@ -584,14 +605,16 @@ double muon_growth(const moe_muon& o) {
 
 size_t update_muon_ws_bytes(const moe_desc& d, bool precise) { return muon_layout(d, precise).bytes; }
 
-hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void* wg, void* wu, void* wd, const void* gg,
-                                     const void* gu, const void* gd, float* master, float* m, void* ws, hipStream_t s) {
-  const MuonLayout l = muon_layout(d, o.precise != 0);
+// Matrices mat0 .. mat0 + mats - 1.
+static hipError_t muon_run(const moe_desc& d, const moe_muon& o, const MuonLayout& l, int mat0, int mats, void* wg, void* wu,
+                           void* wd, const void* gg, const void* gu, const void* gd, float* master, float* m, void* ws,
+                           hipStream_t s) {
   char* base = (char*)ws;
   MuonArgs a{};
   a.w[0] = wg; a.w[1] = wu; a.w[2] = wd;
   a.g[0] = gg; a.g[1] = gu; a.g[2] = gd;
   a.G = d.local_count + d.n_shared;
+  a.mat0 = mat0;
   a.d = d.d_model;
   a.f = d.d_ff;
   a.master = master;
@@ -607,14 +630,14 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
   const bool bf = d.dtype == MOE_BF16;
   {
     KernelTimer kt("muon_momentum", s);
-    const dim3 grid(SUM_BLOCKS, l.mats);
+    const dim3 grid(SUM_BLOCKS, mats);
     if (bf) hipLaunchKernelGGL(muon_momentum_kernel<bf16>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(muon_momentum_kernel<float>, grid, dim3(256), 0, s, a);
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   {
     KernelTimer kt("muon_normalise", s);
-    const dim3 grid((unsigned)((size_t)(a.d / 64) * (a.f / 64)), l.mats);
+    const dim3 grid((unsigned)((size_t)(a.d / 64) * (a.f / 64)), mats);
     if (o.precise) {
       if (bf) hipLaunchKernelGGL((muon_normalise_kernel<bf16, true>), grid, dim3(256), 0, s, a);
       else hipLaunchKernelGGL((muon_normalise_kernel<float, true>), grid, dim3(256), 0, s, a);
@@ -635,7 +658,7 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
     const bool last = done + group == o.steps;
     // A = X X^T
     NsArgs n{};
-    n.mats = l.mats;
+    n.mats = mats;
     n.M = n.N = l.m;
     n.K = l.n;
     n.p = n.q = a.x;
@@ -711,6 +734,7 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
       n.flip_down = a.d > a.f;
       n.master = master;
       n.G = a.G;
+      n.mat0 = mat0;
       n.dtype = d.dtype;
       n.decay = (float)(1.0 - (double)o.lr * (double)o.weight_decay);
       n.step = (float)((double)o.lr * (double)o.scale);
@@ -723,6 +747,16 @@ hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void*
     }
     sx = sn;
     done += group;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_expert_update_muon(const moe_desc& d, const moe_muon& o, void* wg, void* wu, void* wd, const void* gg,
+                                     const void* gu, const void* gd, float* master, float* m, void* ws, hipStream_t s) {
+  const MuonLayout l = muon_layout(d, o.precise != 0);
+  for (int mat0 = 0; mat0 < l.mats; mat0 += l.pass) {
+    const int mats = std::min(l.pass, l.mats - mat0);
+    if (hipError_t e = muon_run(d, o, l, mat0, mats, wg, wu, wd, gg, gu, gd, master, m, ws, s); e != hipSuccess) return e;
   }
   return hipSuccess;
 }

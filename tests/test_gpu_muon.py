@@ -241,3 +241,25 @@ def test_nothing_behind_the_workspace_or_state_is_written():
         setattr(r, name, whole[:t.numel()])
     r.check()
     assert (r.ws_whole[r.ws.numel():] == 3).all() and (r.m_whole[r.m.numel():] == 3).all()
+
+
+def test_matrices_taken_in_several_passes():
+    """Small matrices of so many experts that the workspace holds some of them at a time: 1,032 of 256 x 128, and 96 of 640 x 256
+    (six tiles each), as the matrices alone would be."""
+    for d, f, E, dtype, picks in ((128, 256, 256, "bf16", (0, 100, 255)), (256, 640, 256, "f32", (0, 200))):
+        r = Run(d, f, E, shared=88 if d == 128 else 0, dtype=dtype, master=True)
+        n, G = d * f, r.G
+        alone = Run(d, f, len(picks), dtype=dtype, master=True)
+        for t in range(3):
+            for k, i in enumerate(picks):
+                alone.w[t][k], alone.g[t][k] = r.w[t][i], r.g[t][i]
+                for name in ("m", "master"):
+                    getattr(alone, name)[(t * len(picks) + k) * n:][:n] = getattr(r, name)[(t * G + i) * n:][:n]
+        r.step()
+        alone.check()       # against 64 bits
+        for t in range(3):
+            for k, i in enumerate(picks):
+                # other tiles may add up in another order
+                a = alone.master[(t * len(picks) + k) * n:][:n]
+                b = r.master[(t * G + i) * n:][:n]
+                assert float((a - b).norm()) <= 0.02 * float(r.opt.lr) * float(r.opt.scale) * min(d, f) ** 0.5
