@@ -101,6 +101,20 @@ __global__ __launch_bounds__(256) void muon_normalise_kernel(MuonArgs a) {
   __shared__ double norm2;
   __shared__ f16 tile[PRECISE ? 2 : 1][64][72];
   const size_t at = (size_t)mat * a.d * a.f, part = (size_t)a.d * a.f, at_x = here * part * (PRECISE ? 2 : 1);
+  const T* g = (const T*)a.g[tensor] + (size_t)(mat % a.G) * a.d * a.f;
+  const bool flip = rows > cols;  // stored tall: X is the transpose
+  f16* straight = flip ? a.xt : a.x;
+  f16* turned = flip ? a.x : a.xt;
+  constexpr int PER_ROW = 64 / EP, TASKS = 64 * PER_ROW / 256;
+  Chunk gc[TASKS], mc[TASKS][EP / 4];  // on their way while the norm is formed
+#pragma unroll
+  for (int k = 0; k < TASKS; ++k) {
+    const int task = threadIdx.x + 256 * k, r = task / PER_ROW, c = (task % PER_ROW) * EP;
+    const size_t src = (size_t)(tr * 64 + r) * cols + tc * 64 + c;
+    gc[k] = ld_chunk(g + src);
+#pragma unroll
+    for (int h = 0; h < EP / 4; ++h) mc[k][h] = ld_chunk(a.m + at + src + 4 * h);
+  }
   if (threadIdx.x < 64) {
     double s = a.part[(size_t)here * SUM_BLOCKS + threadIdx.x];
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
@@ -108,19 +122,13 @@ __global__ __launch_bounds__(256) void muon_normalise_kernel(MuonArgs a) {
   }
   __syncthreads();
   const double inv = (double)a.s0 / (sqrt(norm2) + a.eps);
-  const T* g = (const T*)a.g[tensor] + (size_t)(mat % a.G) * a.d * a.f;
-  const bool flip = rows > cols;  // stored tall: X is the transpose
-  f16* straight = flip ? a.xt : a.x;
-  f16* turned = flip ? a.x : a.xt;
-  constexpr int PER_ROW = 64 / EP;
 #pragma unroll
-  for (int k = 0; k < 64 * PER_ROW / 256; ++k) {
+  for (int k = 0; k < TASKS; ++k) {
     const int task = threadIdx.x + 256 * k, r = task / PER_ROW, c = (task % PER_ROW) * EP;
-    const size_t src = (size_t)(tr * 64 + r) * cols + tc * 64 + c;
     float gv[EP], mv[EP];
-    chunk_to_f<T>(ld_chunk(g + src), gv);
+    chunk_to_f<T>(gc[k], gv);
 #pragma unroll
-    for (int h = 0; h < EP; h += 4) chunk_to_f<float>(ld_chunk(a.m + at + src + h), mv + h);
+    for (int h = 0; h < EP / 4; ++h) chunk_to_f<float>(mc[k][h], mv + 4 * h);
 #pragma unroll
     for (int p = 0; p < (PRECISE ? 2 : 1); ++p)
 #pragma unroll
