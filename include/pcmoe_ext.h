@@ -210,14 +210,17 @@ typedef struct {
  * weight matrix of every hosted and shared expert, made orthogonal by Newton-Schulz steps (as the Muon optimiser does):
  *   m <- mu m + g;  u = g + mu m or m;  X = u / (|u|_F + eps)
  *   steps times: A = X X^T, X <- a X + (b A + c A^2) X      (of a matrix with more rows than columns, of its transpose)
+ * (steps may be taken together as one polynomial of A, which multiplies X once)
  *   p <- p (1 - lr weight_decay) - lr scale X
- * Norms are held in fp64, the momentum and all sums in fp32. X, A and b A + c A^2 are held in fp16 between products (11
- * bits, scaled by powers of two so that none overflows), X some 2^-10 of its size off in the end; with precise = 1 in two
- * fp16 parts each (22 bits). A matrix whose u holds a NaN or an infinity becomes NaN, no other does.
+ * Norms are held in fp64, the momentum and all sums in fp32. X, A and a + b A + c A^2 are held in fp16 between products (11
+ * bits, scaled by powers of two so that none overflows): X is off by some 2^-10 to 2^-8 of its size in the end, more where a few
+ * directions of u are 20 times the others' size. With precise = 1 they are held in two fp16 parts each (22 bits), which leaves
+ * X as exact as fp32 products do. A matrix whose u holds a NaN or an infinity becomes NaN, no other does.
  *   w_*, dw_*, master   as for moe_expert_update;  m  fp32 [P] momentum, updated in place
  *   ws   MOE_WS_UPDATE_MUON bytes of scratch, with precise = 1 MOE_WS_UPDATE_MUON_PRECISE bytes
  * MOE_ERR_INVALID_ARGUMENT for a setting outside the ranges stated in moe_muon; MOE_ERR_UNSUPPORTED for coefficients by which
- * a singular value of [0, 1] can pass 16, and for precise = 1 with d_model * d_ff >= 2^29. Calls that overlap on the same parameters or workspace race.
+ * a singular value of [0, 1] can pass 16, and for precise = 1 with d_model * d_ff >= 2^29. Calls that overlap on the same
+ * parameters or workspace race.
  */
 moe_status moe_expert_update_muon(const moe_desc* desc, const moe_muon* opt, void* w_gate, void* w_up, void* w_down,
                                   const void* dw_gate, const void* dw_up, const void* dw_down, float* master, float* m,

@@ -1,18 +1,22 @@
 // Update of the experts' matrices by their orthogonalised momentum.
 //
 // m <- mu m + g, u = g + mu m or m, X = u / (|u|_F + eps); then a fixed number of Newton-Schulz steps
-//   A = X X^T,  B = b A + c A^2,  X <- a X + B X,
+//   A = X X^T,  P = a + b A + c A^2,  X <- P X,
 // taken with X's rows no longer than its columns' number (of a tall matrix X is the transpose), and p <- p (1 - lr wd) -
 // lr scale X. A step of an m x n matrix takes m^2 n (A, half of a symmetric product) + m^3 (A^2, the other) + 2 m^2 n
 // operations, all on the fp16 matrix cores: bound by them, and at small sizes by the launches in a row.
 //
-// All three are products of two K-contiguous operands: A = X X^T reads X, A^2 reads A = A^T, and B X reads B and X^T. So X is
+// Six matrices of 4096 x 14336: 14.5 ms, of which A = X X^T takes 1.26 a time (1,140 TFLOP/s of what the definition needs), X <- P
+// X 2.43 (1,190), a product of 4096^3 0.40; momentum, norm and the first X 1.42 at the memory's rate.
+//
+// All three are products of two K-contiguous operands: A = X X^T reads X, A^2 reads A = A^T, and P X reads P and X^T. So X is
 // kept in both orientations, each written by the epilogue that makes it. Of a symmetric product only the tiles on and above
 // the diagonal are computed; each is stored twice. The last step's epilogue updates the parameters.
 //
-// X, A and B are held in fp16 after a power of two that keeps them below 2^15: |X| never passes the polynomial's largest value
-// on [0, 1], which the host knows. Eleven bits leave X some 2^-11 of its size off; in the precise form each is held in two
-// fp16 parts (22 bits) and three products are added up, smallest first. Sums are fp32, the momentum fp32, the norm fp64.
+// X, A and P are held in fp16 after powers of two that keep them below 2^15: |X| never passes the polynomial's largest value
+// on [0, 1], which the host knows. Eleven bits leave X some 2^-10 of its size off (muon_group has figures); in the precise form
+// each is held in two fp16 parts (22 bits) and three products are added up, smallest first. Sums are fp32, the momentum fp32,
+// the norm fp64.
 #include "nt_gemm.h"
 #include "expert_ops.h"
 
