@@ -261,6 +261,12 @@ __device__ __forceinline__ void q8_store(const Q8Args& a, const Q8Tile<S, DOWN>&
                                : (j < S::FN / 2 ? a.sg : a.su) + (size_t)t.g * f + n + 16 * (j % (S::FN / 2));
       sw[j] = *reinterpret_cast<const floatx4*>(from);
     }
+    // Waited for here. Left open, they would be waited for where the compiler cannot count what was issued since: with all of
+    // the next tile's loads, and all of this one's stores.
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i) asm volatile("" : "+v"(s[i]));
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j) asm volatile("" : "+v"(sw[j]));
   }
   meanwhile();
   if (!live) return;

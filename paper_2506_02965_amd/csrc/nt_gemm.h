@@ -133,7 +133,7 @@ __device__ __forceinline__ void nt_ring(char* smem, int ktiles, bool live, LA&& 
 template <typename S, typename LA, typename LB>
 __device__ __forceinline__ void nt_load(uint32_t base, int ktiles, int kt, int l, LA&& src_a, LB&& src_b) {
   constexpr int OOR = 0x7fffffff;  // no operand has 2^31 bytes
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & (S::NW - 1);  // what of a row's number is l's, is known
   const uint32_t st = base + (kt & 1) * S::STAGE;
   const NtSrc s = l < S::IA ? src_a(kt, wave + S::NW * l) : src_b(kt, wave + S::NW * (l - S::IA));
   const uint32_t dst = l < S::IA ? st + (wave + S::NW * l) * 1024 : st + S::A_BYTES + (wave + S::NW * (l - S::IA)) * 1024;
