@@ -21,16 +21,20 @@ namespace {
 constexpr int Q8_THREADS = 256;
 
 __device__ __forceinline__ uint32_t max_u32(uint32_t a, uint32_t b) { return a > b ? a : b; }
-// Largest magnitude bits over the workgroup (of fp32 numbers: infinities and NaN are above all finite ones).
-__device__ __forceinline__ uint32_t block_max_bits(uint32_t v) {
+// Largest magnitude bits over a row's threads, a wavefront or the workgroup (of fp32 numbers: infinities and NaN are above all
+// finite ones).
+template <int THREADS>
+__device__ __forceinline__ uint32_t row_max_bits(uint32_t v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = max_u32(v, (uint32_t)__shfl_xor((int)v, o, 64));
-  __shared__ uint32_t s[Q8_THREADS / 64];
-  __syncthreads();  // the values of the last call have been read
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
+  if constexpr (THREADS > 64) {
+    __shared__ uint32_t s[THREADS / 64];
+    __syncthreads();  // the values of the last call have been read
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < Q8_THREADS / 64; ++w) v = max_u32(v, s[w]);
+    for (int w = 0; w < THREADS / 64; ++w) v = max_u32(v, s[w]);
+  }
   return v;
 }
 
@@ -72,12 +76,13 @@ __device__ __forceinline__ int code_of(const RowCodes& r, float v) {
   return r.ok ? (int)q : 0;
 }
 
-// A row of K values to codes and scale, by the whole workgroup. SRC: bf16 or float; F64: exact quotients of fp32 values. The
-// first KEEP chunks of a thread stay in registers; what a longer row has beyond them is read again.
-template <typename SRC, bool F64, int KEEP>
+// A row of K values to codes and scale, by THREADS threads: the workgroup, or a wavefront where a row is at most four chunks a
+// lane. SRC: bf16 or float; F64: exact quotients of fp32 values. The first KEEP chunks of a thread stay in registers; what a
+// longer row has beyond them is read again.
+template <typename SRC, bool F64, int KEEP, int THREADS>
 __device__ __forceinline__ void code_row(const SRC* v, int K, int8_t* codes, float* scale) {
   constexpr int EP = EPC<SRC>::value;
-  const int n = K / EP;
+  const int n = K / EP, t = threadIdx.x % THREADS;
   uint32_t top = 0;
   const auto look = [&](const Chunk& c) {
     float x[EP];
@@ -88,13 +93,13 @@ __device__ __forceinline__ void code_row(const SRC* v, int K, int8_t* codes, flo
   Chunk kept[KEEP];
 #pragma unroll
   for (int i = 0; i < KEEP; ++i) {
-    const int c = threadIdx.x + i * Q8_THREADS;
+    const int c = t + i * THREADS;
     kept[i] = c < n ? ld_chunk(v + c * EP) : zero_chunk();
   }
 #pragma unroll
   for (int i = 0; i < KEEP; ++i) look(kept[i]);
-  for (int c = threadIdx.x + KEEP * Q8_THREADS; c < n; c += Q8_THREADS) look(ld_chunk(v + c * EP));
-  top = block_max_bits(top);
+  for (int c = t + KEEP * THREADS; c < n; c += THREADS) look(ld_chunk(v + c * EP));
+  top = row_max_bits<THREADS>(top);
   const RowCodes r = row_codes(top);
   const auto put = [&](int c, const Chunk& from) {
     float x[EP];
@@ -110,32 +115,39 @@ __device__ __forceinline__ void code_row(const SRC* v, int K, int8_t* codes, flo
   };
 #pragma unroll
   for (int i = 0; i < KEEP; ++i) {
-    const int c = threadIdx.x + i * Q8_THREADS;
+    const int c = t + i * THREADS;
     if (c < n) put(c, kept[i]);
   }
-  for (int c = threadIdx.x + KEEP * Q8_THREADS; c < n; c += Q8_THREADS) put(c, ld_chunk(v + c * EP));
-  if (threadIdx.x == 0) *scale = row_scale(top);
+  for (int c = t + KEEP * THREADS; c < n; c += THREADS) put(c, ld_chunk(v + c * EP));
+  if (t == 0) *scale = row_scale(top);
 }
 
+// Rows a workgroup works on at once where they are short: a row's wavefronts share nothing with the others'.
+constexpr int ROWS = Q8_THREADS / 64;
 template <typename T>
+constexpr int short_row = 4 * 64 * EPC<T>::value;  // columns of the longest row that a wavefront takes
+
+template <typename T, bool SHORT>
 __global__ __launch_bounds__(Q8_THREADS) void q8_pack_kernel(const T* w, int64_t rows, int cols, int8_t* codes, float* scales) {
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    code_row<T, std::is_same<T, float>::value, 4>(w + r * cols, cols, codes + r * cols, scales + r);
+  constexpr int AT_ONCE = SHORT ? ROWS : 1;
+  for (int64_t r = (int64_t)blockIdx.x * AT_ONCE + (SHORT ? threadIdx.x / 64 : 0); r < rows; r += (int64_t)gridDim.x * AT_ONCE)
+    code_row<T, std::is_same<T, float>::value, 4, SHORT ? 64 : Q8_THREADS>(w + r * cols, cols, codes + r * cols, scales + r);
 }
 
+// 16 codes a thread.
 template <typename T>
 __global__ __launch_bounds__(Q8_THREADS) void q8_unpack_kernel(const int8_t* codes, const float* scales, int64_t rows, int cols,
                                                                T* w) {
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const float s = scales[r];
-    for (int c = threadIdx.x; c < cols / 16; c += Q8_THREADS) {
-      const Chunk q = ld_chunk(codes + r * cols + 16 * c);
-      float v[16];
+  const int per_row = cols / 16;
+  const int64_t all = rows * per_row, step = (int64_t)gridDim.x * Q8_THREADS;
+  for (int64_t i = (int64_t)blockIdx.x * Q8_THREADS + threadIdx.x; i < all; i += step) {
+    const float s = scales[i / per_row];
+    const Chunk q = ld_chunk(codes + 16 * i);
+    float v[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = (float)(int8_t)(q.w[e / 4] >> (8 * (e % 4))) * s;
+    for (int e = 0; e < 16; ++e) v[e] = (float)(int8_t)(q.w[e / 4] >> (8 * (e % 4))) * s;
 #pragma unroll
-      for (int e = 0; e < 16; e += EPC<T>::value) st_chunk(w + r * cols + 16 * c + e, f_to_chunk<T>(v + e));
-    }
+    for (int e = 0; e < 16; e += EPC<T>::value) st_chunk(w + 16 * i + e, f_to_chunk<T>(v + e));
   }
 }
 
@@ -154,9 +166,9 @@ struct Q8Args {
 };
 
 // Codes of the rows of x_perm and x; the last workgroup makes the m-tile prefixes of the groups, a wavefront each.
-__global__ __launch_bounds__(Q8_THREADS) void q8_rows_x_kernel(Q8Args a) {
-  const int r = blockIdx.x;
-  if (r == (int)gridDim.x - 1) {
+template <bool SHORT>
+__global__ __launch_bounds__(Q8_THREADS) void q8_rows_x_kernel(Q8Args a, int rows_x) {
+  if (blockIdx.x == gridDim.x - 1) {
     const int lane = threadIdx.x & 63, which = threadIdx.x >> 6, bm = which < 2 ? 256 : which == 2 ? 128 : 64;
     int32_t* out = which == 0 ? a.prefix : which == 1 ? a.tail : which == 2 ? a.mid : a.few;
     const int G = a.ga.Eloc + a.ga.S;
@@ -178,16 +190,18 @@ __global__ __launch_bounds__(Q8_THREADS) void q8_rows_x_kernel(Q8Args a) {
     }
     return;
   }
+  const int r = SHORT ? blockIdx.x * ROWS + threadIdx.x / 64 : blockIdx.x;
   const bool routed = r < a.ga.rows_cap;
-  if (routed && r >= a.ga.offsets[a.ga.Eloc]) return;
+  if (r >= rows_x || (routed && r >= a.ga.offsets[a.ga.Eloc])) return;
   const bf16* v = routed ? (const bf16*)a.xp + (size_t)r * a.ga.d : (const bf16*)a.x + (size_t)(r - a.ga.rows_cap) * a.ga.d;
-  code_row<bf16, false, 2>(v, a.ga.d, a.xq + (size_t)r * a.ga.d, a.sx + r);
+  code_row<bf16, false, SHORT ? 4 : 2, SHORT ? 64 : Q8_THREADS>(v, a.ga.d, a.xq + (size_t)r * a.ga.d, a.sx + r);
 }
-template <int KEEP>
-__global__ __launch_bounds__(Q8_THREADS) void q8_rows_h_kernel(Q8Args a) {
-  const int r = blockIdx.x;
-  if (r < a.ga.rows_cap && r >= a.ga.offsets[a.ga.Eloc]) return;
-  code_row<float, false, KEEP>(a.h + (size_t)r * a.ga.f, a.ga.f, a.hq + (size_t)r * a.ga.f, a.sh + r);
+// Codes of the rows of H.
+template <int KEEP, bool SHORT>
+__global__ __launch_bounds__(Q8_THREADS) void q8_rows_h_kernel(Q8Args a, int64_t rows) {
+  const int64_t r = SHORT ? (int64_t)blockIdx.x * ROWS + threadIdx.x / 64 : blockIdx.x;
+  if (r >= rows || (r < a.ga.rows_cap && r >= a.ga.offsets[a.ga.Eloc])) return;
+  code_row<float, false, KEEP, SHORT ? 64 : Q8_THREADS>(a.h + (size_t)r * a.ga.f, a.ga.f, a.hq + (size_t)r * a.ga.f, a.sh + r);
 }
 
 // 1 / (1 + exp(-g)) with the hardware's exponential and reciprocal. The exponential of a product rounded to fp32 alone would be
@@ -482,24 +496,30 @@ size_t ffn_q8_ws_bytes(const moe_desc& d) { return q8_layout(d).bytes; }
 hipError_t launch_q8_pack(int n, int rows, int cols, int dtype, const void* w, void* codes, void* scales, hipStream_t s) {
   const int64_t all = (int64_t)n * rows;
   KernelTimer kt("q8_pack", s);
-  if (dtype == MOE_BF16)
-    hipLaunchKernelGGL(q8_pack_kernel<bf16>, dim3(row_grid(all)), dim3(Q8_THREADS), 0, s, (const bf16*)w, all, cols, (int8_t*)codes,
-                       (float*)scales);
-  else
-    hipLaunchKernelGGL(q8_pack_kernel<float>, dim3(row_grid(all)), dim3(Q8_THREADS), 0, s, (const float*)w, all, cols,
-                       (int8_t*)codes, (float*)scales);
+  const auto go = [&](auto t) {
+    using T = decltype(t);
+    if (cols <= short_row<T>)
+      hipLaunchKernelGGL((q8_pack_kernel<T, true>), dim3(row_grid((all + ROWS - 1) / ROWS)), dim3(Q8_THREADS), 0, s,
+                         (const T*)w, all, cols, (int8_t*)codes, (float*)scales);
+    else
+      hipLaunchKernelGGL((q8_pack_kernel<T, false>), dim3(row_grid(all)), dim3(Q8_THREADS), 0, s, (const T*)w, all, cols,
+                         (int8_t*)codes, (float*)scales);
+  };
+  if (dtype == MOE_BF16) go(bf16{});
+  else go(float{});
   return hipGetLastError();
 }
 
 hipError_t launch_q8_unpack(int n, int rows, int cols, int dtype, const void* codes, const void* scales, void* w,
                             hipStream_t s) {
   const int64_t all = (int64_t)n * rows;
+  const unsigned grid = row_grid((all * (cols / 16) + Q8_THREADS - 1) / Q8_THREADS);
   KernelTimer kt("q8_unpack", s);
   if (dtype == MOE_BF16)
-    hipLaunchKernelGGL(q8_unpack_kernel<bf16>, dim3(row_grid(all)), dim3(Q8_THREADS), 0, s, (const int8_t*)codes,
+    hipLaunchKernelGGL(q8_unpack_kernel<bf16>, dim3(grid), dim3(Q8_THREADS), 0, s, (const int8_t*)codes,
                        (const float*)scales, all, cols, (bf16*)w);
   else
-    hipLaunchKernelGGL(q8_unpack_kernel<float>, dim3(row_grid(all)), dim3(Q8_THREADS), 0, s, (const int8_t*)codes,
+    hipLaunchKernelGGL(q8_unpack_kernel<float>, dim3(grid), dim3(Q8_THREADS), 0, s, (const int8_t*)codes,
                        (const float*)scales, all, cols, (float*)w);
   return hipGetLastError();
 }
@@ -538,7 +558,10 @@ hipError_t launch_ffn_q8(const moe_desc& d, const void* x, const void* xp, const
   const int rx = d.T * d.top_k + (d.n_shared ? d.T : 0);
   {
     KernelTimer kt("q8_rows_x", s);
-    hipLaunchKernelGGL(q8_rows_x_kernel, dim3(rx + 1), dim3(Q8_THREADS), 0, s, a);
+    if (d.d_model <= short_row<bf16>)
+      hipLaunchKernelGGL(q8_rows_x_kernel<true>, dim3((rx + ROWS - 1) / ROWS + 1), dim3(Q8_THREADS), 0, s, a, rx);
+    else
+      hipLaunchKernelGGL(q8_rows_x_kernel<false>, dim3(rx + 1), dim3(Q8_THREADS), 0, s, a, rx);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   const auto gemm = [&](const char* name, auto down) {
@@ -551,11 +574,15 @@ hipError_t launch_ffn_q8(const moe_desc& d, const void* x, const void* xp, const
   if (hipError_t e = gemm("q8_gate_up", std::false_type{}); e != hipSuccess) return e;
   {
     KernelTimer kt("q8_rows_h", s);
-    const auto rows_h = [&](auto keep) {
-      hipLaunchKernelGGL(q8_rows_h_kernel<decltype(keep)::value>, dim3((unsigned)rows_total(d)), dim3(Q8_THREADS), 0, s, a);
+    const int64_t rows = rows_total(d);
+    const auto rows_h = [&](auto keep, auto is_short) {
+      constexpr bool SHORT = decltype(is_short)::value;
+      hipLaunchKernelGGL((q8_rows_h_kernel<decltype(keep)::value, SHORT>), dim3((unsigned)(SHORT ? (rows + ROWS - 1) / ROWS : rows)),
+                         dim3(Q8_THREADS), 0, s, a, rows);
     };
-    if (d.d_ff <= 4 * 4 * Q8_THREADS) rows_h(std::integral_constant<int, 4>{});
-    else rows_h(std::integral_constant<int, 16>{});
+    if (d.d_ff <= short_row<float>) rows_h(std::integral_constant<int, 4>{}, std::true_type{});
+    else if (d.d_ff <= 4 * 4 * Q8_THREADS) rows_h(std::integral_constant<int, 4>{}, std::false_type{});
+    else rows_h(std::integral_constant<int, 16>{}, std::false_type{});
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   return gemm("q8_down", std::true_type{});

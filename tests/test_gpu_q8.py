@@ -159,6 +159,20 @@ def test_shards_and_large_groups():
     Experts(700, 1024, 2816, 4, 2, shared=1).check()
 
 
+def test_long_rows():
+    """Rows of x and of H that a workgroup codes, with and without chunks beyond those it keeps."""
+    Experts(33, 2304, 1152, 2, 1).check()
+    Experts(9, 4224, 4352, 2, 1, shared=1).check()
+    Experts(3, 256, 20480, 1, 1).check()
+
+
+@pytest.mark.parametrize("T,d,f,counts", [(1100, 4096, 4096, [1030, 70]), (1100, 4096, 4096, [512, 0]), (4160, 2176, 2048, [4100, 60]),
+                                          (4160, 2176, 2048, [0, 4160])])
+def test_large_tiles(T, d, f, counts):
+    """Groups that the walking 256-row tiles are chosen for, in gate and up or in the down projection, whole tiles and tails."""
+    Experts(T, d, f, 2, 1, counts=counts).check()
+
+
 def test_many_groups():
     Experts(64, 128, 128, 256, 8, shared=3).check()
 
