@@ -497,17 +497,23 @@ hipError_t ns_launch(const char* name, NsArgs a, hipStream_t s) {
   hipLaunchKernelGGL(kern, dim3((unsigned)tiles), dim3(S::NT), lds, s, a);
   return hipGetLastError();
 }
+// Rounds of n 256 x 256 tiles, a last one of few tiles in quarters.
+double rounds_of(int64_t n, int64_t cus) {
+  const int64_t rest = n % cus;
+  return (double)(n / cus) + (rest == 0 ? 0. : 4 * rest <= cus ? 0.4 : 4 * rest <= 2 * cus ? 0.8 : 1.);
+}
+
 template <int MODE>
 hipError_t ns_product(const char* name, const NsArgs& a, bool precise, hipStream_t s) {
   const auto go = [&](auto shape) {
     using S = decltype(shape);
     return precise ? ns_launch<S, MODE, true>(name, a, s) : ns_launch<S, MODE, false>(name, a, s);
   };
-  // Rounds of the chip, each priced by a tile's time: 4 units of the 128 x 128 tile's work at 1.4 times its rate, two such
-  // tiles at once.
+  // Rounds of the chip, each priced by a tile's time: 4 units of the 128 x 128 tile's work at 1.4 times its rate (a last round in
+  // quarters 0.4 or 0.8 of that), two such tiles at once. 48 matrices of 1024 x 2816: A 170 and 204 us, P 82 and 94, X 346 and 407.
   const int64_t cus = device_cus();
-  const auto rounds = [&](int64_t tiles, int64_t slots) { return (double)((tiles + slots - 1) / slots); };
-  const double large = rounds(ns_tiles<NsLarge, MODE>(a), cus) * 4 / 1.4, small = rounds(ns_tiles<NsSmall, MODE>(a), 2 * cus) * 2;
+  const double large = rounds_of(ns_tiles<NsLarge, MODE>(a), cus) * 4 / 1.4;
+  const double small = (double)((ns_tiles<NsSmall, MODE>(a) + 2 * cus - 1) / (2 * cus)) * 2;
   if (ns_tiles<NsTiniest, MODE>(a) <= cus) return go(NsTiniest{});
   if (ns_tiles<NsTiny, MODE>(a) <= cus) return go(NsTiny{});
   return large <= small ? go(NsLarge{}) : go(NsSmall{});
@@ -519,10 +525,7 @@ hipError_t ns_product(const char* name, const NsArgs& a, bool precise, hipStream
 // matrices at once (a last round in quarters: 0.4, or 0.8 of a round), the last pass at least half full.
 int muon_pass(int m, int mats) {
   const int64_t tm = (m + 255) / 256, tiles = tm * (tm + 1) / 2, cus = 256;
-  const auto cost = [&](int64_t n) {
-    const int64_t whole = n * tiles / cus, rest = n * tiles % cus;
-    return (double)whole + (rest == 0 ? 0. : 4 * rest <= cus ? 0.4 : 4 * rest <= 2 * cus ? 0.8 : 1.);
-  };
+  const auto cost = [&](int64_t n) { return rounds_of(n * tiles, cus); };
   for (int n = 1; n < mats; ++n) {
     const int last = mats % n;
     if (n * tiles * 10 < cus * 9 || (last && 2 * last < n)) continue;

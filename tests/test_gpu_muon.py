@@ -163,6 +163,14 @@ def test_larger_matrices():
     Run(256, 256, 24, dtype="bf16").check()
 
 
+@pytest.mark.parametrize("d,f,E,dtype,precise", [(1024, 1536, 9, "bf16", False), (1536, 1024, 9, "f32", True),
+                                                 (640, 896, 16, "bf16", True), (896, 640, 16, "f32", False)])
+def test_large_tiles_and_their_quarters(d, f, E, dtype, precise):
+    """So many matrices that the 256 x 256 tiles are taken: 270 of them on and above the diagonals, the last 14 in quarters, and
+    288 of matrices that end within a tile."""
+    Run(d, f, E, dtype=dtype, precise=precise).check()
+
+
 def test_zero_tiny_huge_and_broken_gradients():
     for precise in (False, True):
         r = Run(256, 384, 6, precise=precise, dtype="f32")
