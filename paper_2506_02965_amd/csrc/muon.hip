@@ -162,6 +162,8 @@ struct NsArgs {
   int M, N, K, mats;
   int whole;               // tiles that are not split into quarters
   float alpha, beta, diag;
+  float* partial;          // NS_PARTIAL: [ksplit][mats][M][N]
+  int ksplit;
   // a second product of the same shape by the same P, in the same launch
   const f16* q2;
   f16* out2;
@@ -174,7 +176,8 @@ struct NsArgs {
   float decay, step;       // p <- decay p - step X
 };
 
-enum NsMode { NS_SYMMETRIC, NS_BOTH, NS_LAST };  // stores: one tile and its mirror, both orientations, the parameters
+// Stores: one tile and its mirror, both orientations, the parameters, or a part of a symmetric product's sums over K.
+enum NsMode { NS_SYMMETRIC, NS_BOTH, NS_LAST, NS_PARTIAL };
 
 // LDS of an epilogue: a wavefront's part transposed, [WTN][WTM] fp16 with rows of PITCH words, or for parameters stored
 // transposed to X half of it in fp32. Rows an odd multiple of 4 words apart spread the writes over all banks.
@@ -202,7 +205,7 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b, bool second) {
 
 // The tile of matrix `mat` whose first row and column are m0 and n0.
 template <typename S, int MODE, bool PRECISE>
-__device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int mat, bool other, int m0, int n0) {
+__device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int mat, bool other, int m0, int n0, int split = 0) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / S::WN, wn = wave % S::WN, q = lane >> 4, li = lane & 15;
   const int ld = a.K * 2;
@@ -217,13 +220,17 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
   const bool live = m0 + wm * S::WTM < a.M && n0 + wn * S::WTN < a.N;
   typename F16::acc acc[S::FM][S::FN];
   // K-tiles kt: of a precise product first P1 Q2, then P2 Q1, then P1 Q1
+  const int all = PRECISE ? 3 * kts : kts;
+  const int k0 = MODE == NS_PARTIAL ? all * split / a.ksplit : 0, k1 = MODE == NS_PARTIAL ? all * (split + 1) / a.ksplit : all;
   nt_loop<S, F16>(
-      smem, PRECISE ? 3 * kts : kts, live,
+      smem, k1 - k0, live,
       [&](int kt, int j) {
+        if (MODE == NS_PARTIAL) kt += k0;
         const int seg = PRECISE ? (kt >= 2 * kts ? 2 : kt >= kts ? 1 : 0) : 0;
         return NtSrc{rp, (m0 + 8 * j) * ld + at + (kt - seg * kts) * NT_ROWB + (PRECISE && seg == 1 ? (int)p_part : 0)};
       },
       [&](int kt, int j) {
+        if (MODE == NS_PARTIAL) kt += k0;
         const int seg = PRECISE ? (kt >= 2 * kts ? 2 : kt >= kts ? 1 : 0) : 0;
         return NtSrc{rq, (n0 + 8 * j) * ld + at + (kt - seg * kts) * NT_ROWB + (PRECISE && seg == 0 ? (int)q_part : 0)};
       },
@@ -232,7 +239,14 @@ __device__ __forceinline__ void product_tile(const NsArgs& a, char* smem, int ma
   const int mr = m0 + wm * S::WTM, nc = n0 + wn * S::WTN;  // the wavefront's part
   const size_t part = (size_t)a.M * a.N;                     // elements of a part of the result
 
-  if constexpr (MODE == NS_LAST) {
+  if constexpr (MODE == NS_PARTIAL) {
+    float* to = a.partial + ((size_t)split * a.mats + mat) * part;
+#pragma unroll
+    for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::FN; ++j)
+        *reinterpret_cast<floatx4*>(to + (size_t)(mr + 16 * i + li) * a.N + nc + 16 * j + 4 * q) = acc[i][j];
+  } else if constexpr (MODE == NS_LAST) {
     const int tensor = (a.mat0 + mat) / a.G;
     const size_t at_w = (size_t)((a.mat0 + mat) % a.G) * part;
     float* mp = a.master ? a.master + (size_t)tensor * a.G * part + at_w : nullptr;
@@ -432,12 +446,13 @@ typedef NtShape<32, 32, 2, 1, 18, 6> NsTiniest;
 // Tile l of a grid of `tm` x `tn` tiles of every matrix (for symmetric products, of those on and above the diagonal).
 template <int MODE>
 __device__ __forceinline__ void ns_tile(const NsArgs& a, int l, int tm, int tn, int& mat, bool& other, int& mt, int& nt) {
-  const int per = MODE == NS_SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn;
+  constexpr bool SYM = MODE == NS_SYMMETRIC || MODE == NS_PARTIAL;
+  const int per = SYM ? tm * (tm + 1) / 2 : tm * tn;
   other = MODE == NS_SYMMETRIC && l >= per * a.mats;
   if (other) l -= per * a.mats;
   mat = l / per;
   l -= mat * per;
-  if (MODE == NS_SYMMETRIC) {  // nt >= mt, by columns: nt (nt + 1) / 2 tiles stand before column nt
+  if (SYM) {  // nt >= mt, by columns: nt (nt + 1) / 2 tiles stand before column nt
     nt = (int)((sqrtf(8.f * (float)l + 1.f) - 1.f) * 0.5f);
     while (nt * (nt + 1) / 2 > l) --nt;
     while ((nt + 1) * (nt + 2) / 2 <= l) ++nt;
@@ -458,7 +473,11 @@ __global__ __launch_bounds__(S::NT) void muon_product_kernel(NsArgs a) {
   const int tm = (a.M + S::BM - 1) / S::BM, tn = (a.N + S::BN - 1) / S::BN;
   int mat, mt, nt;
   bool other;
-  if (!S::PIPE || (int)blockIdx.x < a.whole) {
+  if constexpr (MODE == NS_PARTIAL) {
+    const int l = xcd_order(blockIdx.x, (int)gridDim.x), tile = l / a.ksplit;
+    ns_tile<MODE>(a, tile, tm, tn, mat, other, mt, nt);
+    product_tile<S, MODE, PRECISE>(a, smem, mat, other, mt * S::BM, nt * S::BN, l - tile * a.ksplit);
+  } else if (!S::PIPE || (int)blockIdx.x < a.whole) {
     ns_tile<MODE>(a, xcd_order(blockIdx.x, S::PIPE ? a.whole : (int)gridDim.x), tm, tn, mat, other, mt, nt);
     product_tile<S, MODE, PRECISE>(a, smem, mat, other, mt * S::BM, nt * S::BN);
   } else {  // a quarter of one of the last tiles
@@ -470,10 +489,42 @@ __global__ __launch_bounds__(S::NT) void muon_product_kernel(NsArgs a) {
   }
 }
 
+// The parts of a symmetric product's sums added up in order, times alpha: a 32 x 32 block on or above the diagonal, and its
+// mirror. blockIdx.y: the matrix.
+template <bool PRECISE>
+__global__ __launch_bounds__(256) void muon_join_kernel(NsArgs a) {
+  constexpr int PARTS = PRECISE ? 2 : 1;
+  __shared__ float block[32][33];
+  int bc = (int)((sqrtf(8.f * (float)blockIdx.x + 1.f) - 1.f) * 0.5f);
+  while (bc * (bc + 1) / 2 > (int)blockIdx.x) --bc;
+  while ((bc + 1) * (bc + 2) / 2 <= (int)blockIdx.x) ++bc;
+  const int br = blockIdx.x - bc * (bc + 1) / 2, mat = blockIdx.y, r = threadIdx.x >> 3, c = 4 * (threadIdx.x & 7);
+  const size_t part = (size_t)a.M * a.N;
+  const float* from = a.partial + mat * part + (size_t)(32 * br + r) * a.N + 32 * bc + c;
+  floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.ksplit; ++s) {
+    const floatx4 v = *reinterpret_cast<const floatx4*>(from + (size_t)s * a.mats * part);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += v[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) block[r][c + e] = a.alpha * sum[e];
+  __syncthreads();
+  f16* out = a.out + mat * PARTS * part;
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) {
+    const uint2 straight = {pack_f16(block[r][c], block[r][c + 1], p != 0), pack_f16(block[r][c + 2], block[r][c + 3], p != 0)};
+    const uint2 turned = {pack_f16(block[c][r], block[c + 1][r], p != 0), pack_f16(block[c + 2][r], block[c + 3][r], p != 0)};
+    *reinterpret_cast<uint2*>(out + p * part + (size_t)(32 * br + r) * a.N + 32 * bc + c) = straight;
+    if (br != bc) *reinterpret_cast<uint2*>(out + p * part + (size_t)(32 * bc + r) * a.N + 32 * br + c) = turned;
+  }
+}
+
 template <typename S, int MODE>
 int64_t ns_tiles(const NsArgs& a) {
   const int64_t tm = (a.M + S::BM - 1) / S::BM, tn = (a.N + S::BN - 1) / S::BN;
-  return (MODE == NS_SYMMETRIC ? tm * (tm + 1) / 2 * (a.q2 ? 2 : 1) : tm * tn) * a.mats;
+  return (MODE == NS_SYMMETRIC ? tm * (tm + 1) / 2 * (a.q2 ? 2 : 1) : MODE == NS_PARTIAL ? tm * (tm + 1) / 2 * a.ksplit : tm * tn) *
+         a.mats;
 }
 
 template <typename S, int MODE, bool PRECISE>
@@ -513,10 +564,25 @@ hipError_t ns_product(const char* name, const NsArgs& a, bool precise, hipStream
   // quarters 0.4 or 0.8 of that), two such tiles at once. 48 matrices of 1024 x 2816: A 170 and 204 us, P 82 and 94, X 346 and 407.
   const int64_t cus = device_cus();
   const double large = rounds_of(ns_tiles<NsLarge, MODE>(a), cus) * 4 / 1.4;
-  const double small = (double)((ns_tiles<NsSmall, MODE>(a) + 2 * cus - 1) / (2 * cus)) * 2;
+  const int64_t n = ns_tiles<NsSmall, MODE>(a);
+  const double small = n <= cus ? 1.1 : (double)((n + 2 * cus - 1) / (2 * cus)) * 2;  // alone on a CU a tile is faster
   if (ns_tiles<NsTiniest, MODE>(a) <= cus) return go(NsTiniest{});
   if (ns_tiles<NsTiny, MODE>(a) <= cus) return go(NsTiny{});
   return large <= small ? go(NsLarge{}) : go(NsSmall{});
+}
+
+hipError_t ns_gram_split(const NsArgs& a, bool tiniest, bool precise, hipStream_t s) {
+  const auto go = [&](auto shape) {
+    using S = decltype(shape);
+    return precise ? ns_launch<S, NS_PARTIAL, true>("muon_gram", a, s) : ns_launch<S, NS_PARTIAL, false>("muon_gram", a, s);
+  };
+  if (hipError_t e = tiniest ? go(NsTiniest{}) : go(NsTiny{}); e != hipSuccess) return e;
+  const int tm = a.M / 32;
+  const dim3 grid((unsigned)(tm * (tm + 1) / 2), a.mats);
+  KernelTimer kt("muon_join", s);
+  if (precise) hipLaunchKernelGGL(muon_join_kernel<true>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(muon_join_kernel<false>, grid, dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 // Matrices taken at a time, from X to the parameters: as few as fill the chip, since the workspace is theirs alone (192 matrices
@@ -534,10 +600,36 @@ int muon_pass(int m, int mats) {
   return mats;
 }
 
+// A = X X^T of few rows and long K would leave most CUs idle while some walk over all of K: its sums are split over K, and joined
+// by a second launch. Both ways priced by a workgroup's time: 0.2 us a K-tile of 32 x 32 tiles, 0.33 of 64 x 64 tiles, all at
+// once, and 4 for the second launch (two parts of two fp32 experts, 2048 x 256: 238 -> 209 us an update of six steps; four of
+// 4096 x 128: 298 -> 214).
+struct GramSplit {
+  int parts;    // 1: not split
+  bool tiniest; // 32 x 32 tiles
+};
+GramSplit gram_split(int m, int n, int mats, bool precise) {
+  const int64_t cus = 256, kts = n / 64 * (precise ? 3 : 1);
+  const auto tiles = [&](int b) { return (int64_t)((m + b - 1) / b) * ((m + b - 1) / b + 1) / 2 * mats; };
+  GramSplit best{1, true};
+  if (tiles(64) > cus) return best;
+  double time = kts * (tiles(32) <= cus ? 0.2 : 0.33);
+  for (int b : {32, 64}) {
+    const int64_t s = std::min(cus / tiles(b), kts / 8);
+    const double t = kts * (b == 32 ? 0.2 : 0.33) / s + 4;
+    if (s >= 2 && t < time) {
+      best = {(int)s, b == 32};
+      time = t;
+    }
+  }
+  return best;
+}
+
 struct MuonLayout {
   int mats, m, n;
   int pass;  // matrices taken at a time
-  size_t x, xt[2], a, r, b[3], bytes;  // the partial sums of squares come first
+  GramSplit split;
+  size_t x, xt[2], a, r, b[3], partial, bytes;  // the partial sums of squares come first
 };
 MuonLayout muon_layout(const moe_desc& d, bool precise) {
   MuonLayout l{};
@@ -558,6 +650,9 @@ MuonLayout muon_layout(const moe_desc& d, bool precise) {
   l.a = take(all_a);
   l.r = take(all_a);
   for (size_t& o : l.b) o = take(all_a);
+  l.split = gram_split(l.m, l.n, l.pass, precise);
+  l.partial = at;
+  if (l.split.parts > 1) at += align256((size_t)l.split.parts * all_a * sizeof(float));
   l.bytes = at;
   return l;
 }
@@ -680,7 +775,13 @@ static hipError_t muon_run(const moe_desc& d, const moe_muon& o, const MuonLayou
     n.out = A;
     double sa = two_to(top * top);
     n.alpha = (float)(sa / (sx * sx));
-    if (hipError_t e = ns_product<NS_SYMMETRIC>("muon_gram", n, o.precise, s); e != hipSuccess) return e;
+    if (l.split.parts > 1) {
+      n.ksplit = l.split.parts;
+      n.partial = (float*)(base + l.partial);
+      if (hipError_t e = ns_gram_split(n, l.split.tiniest, o.precise, s); e != hipSuccess) return e;
+    } else if (hipError_t e = ns_product<NS_SYMMETRIC>("muon_gram", n, o.precise, s); e != hipSuccess) {
+      return e;
+    }
     n.K = l.m;
     f16 *P = nullptr, *Q = nullptr;
     double sp = 0, sq = 0, tq = 1.0;

@@ -171,6 +171,13 @@ def test_large_tiles_and_their_quarters(d, f, E, dtype, precise):
     Run(d, f, E, dtype=dtype, precise=precise).check()
 
 
+@pytest.mark.parametrize("d,f,E,dtype,precise", [(128, 2048, 1, "f32", True), (4096, 128, 2, "bf16", False), (256, 3200, 2, "bf16", True),
+                                                 (2176, 384, 1, "bf16", False), (128, 1152, 8, "f32", False)])
+def test_long_rows_split_their_sums(d, f, E, dtype, precise):
+    """Matrices of few rows and long columns, whose Gram matrices are summed in parts."""
+    Run(d, f, E, dtype=dtype, precise=precise).check()
+
+
 def test_zero_tiny_huge_and_broken_gradients():
     for precise in (False, True):
         r = Run(256, 384, 6, precise=precise, dtype="f32")
