@@ -5,8 +5,8 @@
 // row again once the whole row is there, and y = sh sd (h . d). So a call is four launches: rows of x to codes, gate and up,
 // rows of H to codes, down.
 //
-// Bound by the int8 matrix cores for long prompts (8192 tokens, 4096, 14336, 8 experts, 2 a token: gate and up 1,868 us, 2,070
-// TOP/s; down 900, 2,130), where H passes memory once in fp32 and once in codes (210 us), and by the weights for few rows (24
+// Bound by the int8 matrix cores for long prompts (8192 tokens, 4096, 14336, 8 experts, 2 a token: gate and up 1,775 us, 2,170
+// TOP/s; down 905, 2,130), where H passes memory once in fp32 and once in codes (210 us), and by the weights for few rows (24
 // tokens, 2048, 1408, 64 experts: 64 + 34 us, 5.4 and 5.1 TB/s).
 #include "nt_gemm.h"
 #include "expert_ops.h"

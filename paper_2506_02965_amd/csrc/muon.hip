@@ -6,8 +6,8 @@
 // lr scale X. A step of an m x n matrix takes m^2 n (A, half of a symmetric product) + m^3 (A^2, the other) + 2 m^2 n
 // operations, all on the fp16 matrix cores: bound by them, and at small sizes by the launches in a row.
 //
-// Six matrices of 4096 x 14336: 14.5 ms, of which A = X X^T takes 1.26 a time (1,140 TFLOP/s of what the definition needs), X <- P
-// X 2.43 (1,190), a product of 4096^3 0.40; momentum, norm and the first X 1.42 at the memory's rate.
+// Six matrices of 4096 x 14336: 14.4 ms, of which A = X X^T takes 1.26 a time (1,150 TFLOP/s of what the definition needs), X
+// <- P X 2.41 (1,200), a product of 4096^3 0.40; momentum, norm and the first X 1.42 at the memory's rate.
 //
 // All three are products of two K-contiguous operands: A = X X^T reads X, A^2 reads A = A^T, and P X reads P and X^T. So X is
 // kept in both orientations, each written by the epilogue that makes it. Of a symmetric product only the tiles on and above
@@ -561,14 +561,15 @@ hipError_t ns_product(const char* name, const NsArgs& a, bool precise, hipStream
     return precise ? ns_launch<S, MODE, true>(name, a, s) : ns_launch<S, MODE, false>(name, a, s);
   };
   // Rounds of the chip, each priced by a tile's time: 4 units of the 128 x 128 tile's work at 1.4 times its rate (a last round in
-  // quarters 0.4 or 0.8 of that), two such tiles at once. 48 matrices of 1024 x 2816: A 170 and 204 us, P 82 and 94, X 346 and 407.
+  // quarters 0.4 or 0.8 of that), two such tiles at once, the smaller ones where both cost the same. 48 matrices of 1024 x 2816: A 170
+  // and 204 us, P 82 and 94, X 346 and 407; 27 of 1024 x 1536 (A and P cost the same) 74 and 73, 58 and 52, X 122 and 142.
   const int64_t cus = device_cus();
   const double large = rounds_of(ns_tiles<NsLarge, MODE>(a), cus) * 4 / 1.4;
   const int64_t n = ns_tiles<NsSmall, MODE>(a);
   const double small = n <= cus ? 1.1 : (double)((n + 2 * cus - 1) / (2 * cus)) * 2;  // alone on a CU a tile is faster
   if (ns_tiles<NsTiniest, MODE>(a) <= cus) return go(NsTiniest{});
   if (ns_tiles<NsTiny, MODE>(a) <= cus) return go(NsTiny{});
-  return large <= small ? go(NsLarge{}) : go(NsSmall{});
+  return large < small ? go(NsLarge{}) : go(NsSmall{});
 }
 
 hipError_t ns_gram_split(const NsArgs& a, bool tiniest, bool precise, hipStream_t s) {
