@@ -199,9 +199,11 @@ __global__ __launch_bounds__(Q8_THREADS) void q8_rows_x_kernel(Q8Args a, int row
 // Codes of the rows of H.
 template <int KEEP, bool SHORT>
 __global__ __launch_bounds__(Q8_THREADS) void q8_rows_h_kernel(Q8Args a, int64_t rows) {
-  const int64_t r = SHORT ? (int64_t)blockIdx.x * ROWS + threadIdx.x / 64 : blockIdx.x;
-  if (r >= rows || (r < a.ga.rows_cap && r >= a.ga.offsets[a.ga.Eloc])) return;
-  code_row<float, false, KEEP, SHORT ? 64 : Q8_THREADS>(a.h + (size_t)r * a.ga.f, a.ga.f, a.hq + (size_t)r * a.ga.f, a.sh + r);
+  constexpr int AT_ONCE = SHORT ? ROWS : 1;
+  const int64_t routed = a.ga.offsets[a.ga.Eloc];
+  for (int64_t r = (int64_t)blockIdx.x * AT_ONCE + (SHORT ? threadIdx.x / 64 : 0); r < rows; r += (int64_t)gridDim.x * AT_ONCE)
+    if (r >= a.ga.rows_cap || r < routed)
+      code_row<float, false, KEEP, SHORT ? 64 : Q8_THREADS>(a.h + r * a.ga.f, a.ga.f, a.hq + r * a.ga.f, a.sh + r);
 }
 
 // 1 / (1 + exp(-g)) with the hardware's exponential and reciprocal. The exponential of a product rounded to fp32 alone would be
@@ -577,8 +579,8 @@ hipError_t launch_ffn_q8(const moe_desc& d, const void* x, const void* xp, const
     const int64_t rows = rows_total(d);
     const auto rows_h = [&](auto keep, auto is_short) {
       constexpr bool SHORT = decltype(is_short)::value;
-      hipLaunchKernelGGL((q8_rows_h_kernel<decltype(keep)::value, SHORT>), dim3((unsigned)(SHORT ? (rows + ROWS - 1) / ROWS : rows)),
-                         dim3(Q8_THREADS), 0, s, a, rows);
+      const unsigned grid = row_grid(SHORT ? (rows + ROWS - 1) / ROWS : rows);
+      hipLaunchKernelGGL((q8_rows_h_kernel<decltype(keep)::value, SHORT>), dim3(grid), dim3(Q8_THREADS), 0, s, a, rows);
     };
     if (d.d_ff <= short_row<float>) rows_h(std::integral_constant<int, 4>{}, std::true_type{});
     else if (d.d_ff <= 4 * 4 * Q8_THREADS) rows_h(std::integral_constant<int, 4>{}, std::false_type{});

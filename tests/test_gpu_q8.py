@@ -188,6 +188,18 @@ def test_rows_do_not_depend_on_each_other():
         assert torch.equal(s.run()[:T], y[:T]), T
 
 
+def test_more_rows_than_a_launch_has_workgroups():
+    """4.3 million rows of H: more than a launch of 2^20 workgroups takes at once."""
+    T, k = 720000, 6
+    e = Experts(T, 128, 128, k, k, counts=[T] * k)
+    y = e.run()
+    last = k * T - 50
+    s = Experts(50, 128, 128, k, 1, counts=[0] * (k - 1) + [50])
+    s.gate, s.up, s.down = e.gate, e.up, e.down
+    s.x_perm = e.x_perm[last:].clone()
+    assert torch.equal(s.run(), y[last:])
+
+
 def test_broken_rows_and_weights():
     e = Experts(150, 256, 384, 2, 1, counts=[100, 50])
     clean = e.run().clone()
