@@ -13,7 +13,7 @@ All calls are enqueued on one stream; no per-expert count ever returns to the ho
 """
 from __future__ import annotations
 
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 from typing import Optional
 
 import numpy as np
@@ -368,7 +368,9 @@ class MoEStack:
     """Layers one after the other with norms, gates and the residual stream around them:
         r_0 = x, h_0 = pre(r_0);  y_i = layer_i(h_i);  r_i+1 = alpha r_i + gate_i+1 * post(y_i), h_i+1 = pre(r_i+1)
     with `final` in place of pre at the end. The result is the last h, or the last r where final is "none". layers: MoELayers of
-    one T, d and dtype. forward takes the layers' weights (whose x it sets) and len(layers) + 1 NormWeights."""
+    one T, d and dtype. forward takes the layers' weights (whose x it sets) and len(layers) + 1 NormWeights. The stack's calls
+    read the layers' inputs from its own buffers, never from the weights' x: other stacks may run with the same weights between
+    a forward and its backward, and layers of one stack may share theirs."""
 
     def __init__(self, layers, pre="rms", post="none", final="rms", eps=1e-6, residual_scale=1.0, gate_groups=1):
         if not layers:
@@ -396,6 +398,7 @@ class MoEStack:
         r, h = self.norms[0].forward(ns[0], x)
         for i, (layer, w) in enumerate(zip(self.layers, ws)):
             w.x = h
+            w = replace(w, x=h)
             if experts is None:
                 y = layer.forward(w)
             else:
@@ -409,7 +412,7 @@ class MoEStack:
         dr, dh = (d, None) if self.norms[-1].h is None else (None, d)
         for i in reversed(range(len(self.layers))):
             dr, dy = self.norms[i + 1].backward(ns[i + 1], dr, dh)
-            dh = self.layers[i].backward(ws[i], dy)
+            dh = self.layers[i].backward(replace(ws[i], x=self.norms[i].h), dy)
         return self.norms[0].backward(ns[0], dr, dh)[0]
 
 

@@ -177,3 +177,22 @@ def test_a_captured_training_step():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((out, dx, *state), want))
+
+
+def test_a_backward_after_another_stacks_forward():
+    """Two stacks with the same weights: the first one's gradients are those that it gives alone."""
+    cfg = LayerConfig("s", T=96, d=256, f=128, E=4, k=2, n_shared=1)
+    ws, ns, normal = make(cfg, 2, 1, seed=7)
+    first, second = (MoEStack([MoELayer(c) for _ in range(2)]) for c in (cfg, cfg.scaled(T=33)))
+    for n in ns:
+        n.w_post = None
+    x, other, d = normal(cfg.T, cfg.d), normal(33, cfg.d), normal(cfg.T, cfg.d)
+
+    def gradients(between):
+        first.forward(x, ws, ns)
+        if between:
+            second.forward(other, ws, ns)
+        dx = first.backward(d, ws, ns)
+        return [t.clone() for l in first.layers for t in (l.dw_gate, l.dw_up, l.dw_down, l.dw_router)] + [dx.clone()]
+    alone = gradients(False)
+    assert all(torch.equal(a, b) for a, b in zip(alone, gradients(True)))

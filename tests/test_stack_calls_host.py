@@ -1,0 +1,68 @@
+"""What MoEStack hands to the library's calls, recorded in their place (host buffers, no GPU is touched)."""
+import os
+
+import pytest
+import torch
+
+from paper_2506_02965_amd import pcmoe as P
+from paper_2506_02965_amd.layer import LayerWeights, MoELayer, MoEStack, NormWeights
+from paper_2506_02965_amd.synth import LayerConfig
+
+pytestmark = pytest.mark.skipif(not os.path.exists(P.LIB_PATH), reason="libpcmoe.so not built")
+CFG = LayerConfig("h", T=64, d=128, f=256, E=4, k=2, n_shared=1)
+X_AT = {"moe_route": 1, "moe_permute": 2, "moe_expert_ffn_fwd": 1, "moe_expert_ffn_bwd": 1, "moe_route_bwd": 1}  # x among the arguments
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    made = []
+    for name in P.EXPORTS + P.EXPORTS_EXT:
+        if name not in ("moe_workspace_size", "moe_status_string", "moe_last_error"):
+            monkeypatch.setattr(P, name, lambda *a, _n=name, **k: made.append((_n, a)), raising=False)
+    return made
+
+
+def weights():
+    return LayerWeights(None, None, None, 1, None, None, None)
+
+
+def stack_of(n, cfg=CFG, **kw):
+    return MoEStack([MoELayer(cfg, device="cpu") for _ in range(n)], **kw)
+
+
+def rows(cfg=CFG):
+    return torch.zeros(cfg.T, cfg.d, dtype=torch.bfloat16)
+
+
+def inputs_of(made):
+    """(call, address of its x, rows of x) of every call that reads a layer's input."""
+    return [(n, a[X_AT[n]].data_ptr(), a[X_AT[n]].shape[0], a[0].T) for n, a in made if n in X_AT]
+
+
+def test_backward_reads_this_stacks_inputs_after_another_stacks_forward(calls):
+    """Weights shared by two stacks, of 64 tokens and of one, as when a token is decoded between a forward and its backward."""
+    one = CFG.scaled(T=1)
+    train, decode = stack_of(2), stack_of(2, one)
+    ws, ns = [weights(), weights()], [NormWeights()] * 3
+    train.forward(rows(), ws, ns)
+    decode.forward(rows(one), ws, ns)
+    del calls[:]
+    train.backward(rows(), ws, ns)
+    want = [train.norms[i].h.data_ptr() for i in (1, 1, 0, 0)]
+    got = inputs_of(calls)
+    assert [g[0] for g in got] == ["moe_expert_ffn_bwd", "moe_route_bwd"] * 2
+    assert [g[1] for g in got] == want
+    assert all(rows_of_x == T == CFG.T for _, _, rows_of_x, T in got)
+
+
+def test_layers_with_the_same_weights(calls):
+    """Tied layers: each layer's calls read its own input, forward and backward."""
+    stack = stack_of(2)
+    w = weights()
+    ws, ns = [w, w], [NormWeights()] * 3
+    stack.forward(rows(), ws, ns)
+    first, second = (stack.norms[i].h.data_ptr() for i in range(2))
+    assert [g[1] for g in inputs_of(calls)] == [first] * 3 + [second] * 3
+    del calls[:]
+    stack.backward(rows(), ws, ns)
+    assert [g[1] for g in inputs_of(calls)] == [second] * 2 + [first] * 2
