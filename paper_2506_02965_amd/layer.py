@@ -393,8 +393,15 @@ class MoEStack:
                                            backward=self.backward_enabled, ws=ws))
             ws = getattr(self.norms[-1], "ws", None)
 
+    def _check_counts(self, ws, ns, experts=None):
+        n = len(self.layers)
+        if len(ws) != n or len(ns) != n + 1 or (experts is not None and len(experts) != n):
+            raise ValueError(f"{n} layers take {n} weights, {n + 1} norms and, if any, {n} experts: got {len(ws)}, {len(ns)}"
+                             + (f" and {len(experts)}" if experts is not None else ""))
+
     def forward(self, x, ws, ns, experts=None):
         """experts: a Q4Experts or Q8Experts for each layer, to run the experts from (no backward can follow)."""
+        self._check_counts(ws, ns, experts)
         r, h = self.norms[0].forward(ns[0], x)
         for i, (layer, w) in enumerate(zip(self.layers, ws)):
             w.x = h
@@ -409,6 +416,7 @@ class MoEStack:
     def backward(self, d, ws, ns):
         """The gradient of x from that of forward's result. Layers leave the gradients of their weights in their buffers, the
         norms in theirs."""
+        self._check_counts(ws, ns)
         dr, dh = (d, None) if self.norms[-1].h is None else (None, d)
         for i in reversed(range(len(self.layers))):
             dr, dy = self.norms[i + 1].backward(ns[i + 1], dr, dh)

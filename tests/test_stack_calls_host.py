@@ -66,3 +66,19 @@ def test_layers_with_the_same_weights(calls):
     del calls[:]
     stack.backward(rows(), ws, ns)
     assert [g[1] for g in inputs_of(calls)] == [second] * 2 + [first] * 2
+
+
+def test_weights_norms_and_experts_for_every_layer(calls):
+    """As many weights and experts as layers and one norm more, or nothing runs."""
+    stack = stack_of(2)
+    ws, ns, q = [weights(), weights()], [NormWeights()] * 3, [None] * 2
+    for wrong in ((ws[:1], ns, None), (ws + ws, ns, None), (ws, ns[:2], None), (ws, ns + ns, None), (ws, ns, q[:1]), (ws, ns, q + q)):
+        with pytest.raises(ValueError, match="layers"):
+            stack.forward(rows(), *wrong)
+    assert not calls
+    stack.forward(rows(), ws, ns)
+    del calls[:]
+    for wrong in ((ws[:1], ns), (ws + ws, ns), (ws, ns[:2]), (ws, ns + ns)):
+        with pytest.raises(ValueError, match="layers"):
+            stack.backward(rows(), *wrong)
+    assert not calls
