@@ -368,7 +368,7 @@ class MoEStack:
     """Layers one after the other with norms, gates and the residual stream around them:
         r_0 = x, h_0 = pre(r_0);  y_i = layer_i(h_i);  r_i+1 = alpha r_i + gate_i+1 * post(y_i), h_i+1 = pre(r_i+1)
     with `final` in place of pre at the end. The result is the last h, or the last r where final is "none". layers: MoELayers of
-    one T, d and dtype. forward takes the layers' weights (whose x it sets) and len(layers) + 1 NormWeights. The stack's calls
+    one T, d and dtype that host all experts. forward takes the layers' weights (whose x it sets) and len(layers) + 1 NormWeights. The stack's calls
     read the layers' inputs from its own buffers, never from the weights' x: other stacks may run with the same weights between
     a forward and its backward, and layers of one stack may share theirs."""
 
@@ -381,6 +381,9 @@ class MoEStack:
         for l in layers:
             if (l.cfg.T, l.cfg.d, l.cfg.dtype) != (cfg.T, cfg.d, cfg.dtype):
                 raise ValueError("the layers of a stack share T, d and dtype")
+            if l.cfg.n_local != l.cfg.E:
+                raise ValueError(f"a stack's layers host all experts, got {l.cfg.n_local} of {l.cfg.E}: one party's output is a "
+                                 "part of a sum; add the parties' up and join the layers with ResidualNorm")
         if pre == "none":
             raise ValueError("a stack norms the input of its layers: pre is 'rms' or 'layer'")
         self.layers = list(layers)

@@ -82,3 +82,12 @@ def test_weights_norms_and_experts_for_every_layer(calls):
         with pytest.raises(ValueError, match="layers"):
             stack.backward(rows(), *wrong)
     assert not calls
+
+
+def test_layers_that_host_a_part_of_the_experts():
+    """Their output is one party's part of a sum, which no norm or residual may take alone."""
+    for part in (dict(local_count=2), dict(local_begin=1, local_count=3)):
+        layers = [MoELayer(CFG, device="cpu"), MoELayer(CFG.scaled(**part), device="cpu")]
+        with pytest.raises(ValueError, match="all experts"):
+            MoEStack(layers)
+    MoEStack([MoELayer(CFG.scaled(local_count=CFG.E), device="cpu")])
