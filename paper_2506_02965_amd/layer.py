@@ -329,6 +329,7 @@ class ResidualNorm:
             need = P.moe_workspace_size(self.desc, P.MOE_WS_NORM_BWD)
             self.ws = torch.empty(need, dtype=torch.uint8, device=device) if ws is None else ws
         self.dw_post = self.dgate = self.dw_pre = None   # fp32, allocated by the first backward
+        self.y = self.r_of_backward = None   # of the last forward
 
     def _check(self, what, t, shape, dtype=None):
         if t is not None and (tuple(t.shape) != shape or t.dtype != (dtype or self.dt)):
@@ -354,6 +355,10 @@ class ResidualNorm:
         self._check_weights(w)
         self._check("dr", dr, self.shape)
         self._check("dh", dh, self.shape)
+        if not self.backward_enabled:
+            raise RuntimeError("a norm built with backward=False has no backward")
+        if self.r_of_backward is None:
+            raise RuntimeError("a backward needs a forward before it")
         for name, t in (("dw_post", w.w_post), ("dgate", w.gate), ("dw_pre", w.w_pre)):
             if t is None:
                 setattr(self, name, None)
@@ -420,6 +425,10 @@ class MoEStack:
         """The gradient of x from that of forward's result. Layers leave the gradients of their weights in their buffers, the
         norms in theirs."""
         self._check_counts(ws, ns)
+        if not self.backward_enabled:
+            raise RuntimeError("a stack with a layer built with backward=False has no backward")
+        if self.norms[-1].r_of_backward is None:
+            raise RuntimeError("a backward needs a forward before it")
         dr, dh = (d, None) if self.norms[-1].h is None else (None, d)
         for i in reversed(range(len(self.layers))):
             dr, dy = self.norms[i + 1].backward(ns[i + 1], dr, dh)

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2506_02965_amd import pcmoe as P
-from paper_2506_02965_amd.layer import LayerWeights, MoELayer, MoEStack, NormWeights
+from paper_2506_02965_amd.layer import LayerWeights, MoELayer, MoEStack, NormWeights, ResidualNorm
 from paper_2506_02965_amd.synth import LayerConfig
 
 pytestmark = pytest.mark.skipif(not os.path.exists(P.LIB_PATH), reason="libpcmoe.so not built")
@@ -91,3 +91,25 @@ def test_layers_that_host_a_part_of_the_experts():
         with pytest.raises(ValueError, match="all experts"):
             MoEStack(layers)
     MoEStack([MoELayer(CFG.scaled(local_count=CFG.E), device="cpu")])
+
+
+def test_backward_of_what_was_built_without_it(calls):
+    stack = MoEStack([MoELayer(CFG, device="cpu"), MoELayer(CFG, device="cpu", backward=False)])
+    ws, ns = [weights(), weights()], [NormWeights()] * 3
+    stack.forward(rows(), ws, ns)
+    norm = ResidualNorm(CFG.T, CFG.d, P.make_norm(), device="cpu", backward=False)
+    norm.forward(NormWeights(), rows(), rows())
+    del calls[:]
+    with pytest.raises(RuntimeError, match="backward=False"):
+        stack.backward(rows(), ws, ns)
+    with pytest.raises(RuntimeError, match="backward=False"):
+        norm.backward(NormWeights(), rows(), rows())
+    assert not calls
+
+
+def test_backward_before_any_forward(calls):
+    with pytest.raises(RuntimeError, match="forward"):
+        stack_of(1).backward(rows(), [weights()], [NormWeights()] * 2)
+    with pytest.raises(RuntimeError, match="forward"):
+        ResidualNorm(CFG.T, CFG.d, P.make_norm(), device="cpu").backward(NormWeights(), rows(), rows())
+    assert not calls
