@@ -134,6 +134,7 @@ class MoELayer:
         self.ws_q4 = None   # of forward_q4 and forward_q8, allocated by their first calls
         self.ws_q8 = None
         self.saved_nothing = False  # the last forward was forward_q4 or forward_q8
+        self.runs = 0       # forwards so far: what the activations are of
         self.ws_ffn_fwd = ws(P.MOE_WS_FFN_FWD)
         if self.backward_enabled:
             G = Eloc + S
@@ -171,6 +172,7 @@ class MoELayer:
         P.moe_route(self.desc, w.x, w.w_router, w.logit_bias, w.bias_groups, self.logits, self.topk_idx, self.topk_w)
 
     def permute(self, w: LayerWeights):
+        self.runs += 1
         P.moe_permute(self.desc, self.topk_idx, w.x, self.counts, self.offsets, self.row_to_slot, self.slot_to_row,
                       self.x_perm, self.ws_permute, self.ws_permute.numel())
 
@@ -375,7 +377,8 @@ class MoEStack:
     with `final` in place of pre at the end. The result is the last h, or the last r where final is "none". layers: MoELayers of
     one T, d and dtype that host all experts. forward takes the layers' weights (whose x it sets) and len(layers) + 1 NormWeights. The stack's calls
     read the layers' inputs from its own buffers, never from the weights' x: other stacks may run with the same weights between
-    a forward and its backward, and layers of one stack may share theirs."""
+    a forward and its backward, and layers of one stack may share theirs. A backward belongs to the last forward of each of its
+    layers."""
 
     def __init__(self, layers, pre="rms", post="none", final="rms", eps=1e-6, residual_scale=1.0, gate_groups=1):
         if not layers:
@@ -393,6 +396,7 @@ class MoEStack:
             raise ValueError("a stack norms the input of its layers: pre is 'rms' or 'layer'")
         self.layers = list(layers)
         self.backward_enabled = all(l.backward_enabled for l in layers)
+        self.ran = None   # the layers' runs after the last forward
         self.norms, ws = [], None
         for i in range(len(layers) + 1):
             norm = P.make_norm(final if i == len(layers) else pre, post if i else "none", eps, residual_scale if i else 1.0,
@@ -419,6 +423,7 @@ class MoEStack:
             else:
                 y = (layer.forward_q8 if isinstance(experts[i], Q8Experts) else layer.forward_q4)(w, experts[i])
             r, h = self.norms[i + 1].forward(ns[i + 1], r, y)
+        self.ran = [l.runs for l in self.layers]
         return r if h is None else h
 
     def backward(self, d, ws, ns):
@@ -427,8 +432,12 @@ class MoEStack:
         self._check_counts(ws, ns)
         if not self.backward_enabled:
             raise RuntimeError("a stack with a layer built with backward=False has no backward")
-        if self.norms[-1].r_of_backward is None:
+        if self.ran is None:
             raise RuntimeError("a backward needs a forward before it")
+        for layer in self.layers:
+            layer._need_saved()
+        if [l.runs for l in self.layers] != self.ran:
+            raise RuntimeError("a layer ran another forward since this stack's: its activations are of that one")
         dr, dh = (d, None) if self.norms[-1].h is None else (None, d)
         for i in reversed(range(len(self.layers))):
             dr, dy = self.norms[i + 1].backward(ns[i + 1], dr, dh)

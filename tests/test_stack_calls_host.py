@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2506_02965_amd import pcmoe as P
-from paper_2506_02965_amd.layer import LayerWeights, MoELayer, MoEStack, NormWeights, ResidualNorm
+from paper_2506_02965_amd.layer import LayerWeights, MoELayer, MoEStack, NormWeights, Q8Experts, ResidualNorm
 from paper_2506_02965_amd.synth import LayerConfig
 
 pytestmark = pytest.mark.skipif(not os.path.exists(P.LIB_PATH), reason="libpcmoe.so not built")
@@ -112,4 +112,26 @@ def test_backward_before_any_forward(calls):
         stack_of(1).backward(rows(), [weights()], [NormWeights()] * 2)
     with pytest.raises(RuntimeError, match="forward"):
         ResidualNorm(CFG.T, CFG.d, P.make_norm(), device="cpu").backward(NormWeights(), rows(), rows())
+    assert not calls
+
+
+def test_backward_after_the_layers_ran_elsewhere(calls):
+    """A layer holds the activations of its last forward: a backward of an earlier one is refused before anything runs."""
+    layers = [MoELayer(CFG, device="cpu") for _ in range(2)]
+    first, second = MoEStack(layers), MoEStack(layers, post="rms")
+    ws, ns, q = [weights(), weights()], [NormWeights()] * 3, [Q8Experts(*[(None, None)] * 3)] * 2
+    others = (lambda: second.forward(rows(), ws, ns), lambda: layers[1].forward(weights()), lambda: layers[0].forward_q8(weights(), q[0]))
+    for other in others:
+        first.forward(rows(), ws, ns)
+        other()
+        del calls[:]
+        with pytest.raises(RuntimeError, match="forward"):
+            first.backward(rows(), ws, ns)
+        assert not calls
+    second.forward(rows(), ws, ns)
+    second.backward(rows(), ws, ns)
+    first.forward(rows(), ws, ns, q)
+    del calls[:]
+    with pytest.raises(RuntimeError, match="forward_q8"):
+        first.backward(rows(), ws, ns)
     assert not calls
