@@ -207,11 +207,19 @@ class MoELayer:
         self.combine()
         return self.y
 
+    def _check_q8(self, q: Q8Experts):
+        G, d, f = self.cfg.n_local + self.cfg.n_shared, self.cfg.d, self.cfg.f
+        for name, rows, cols in (("gate", f, d), ("up", f, d), ("down", d, f)):
+            for t, shape, dtype in zip(getattr(q, name), ((G, rows, cols), (G, rows)), (torch.int8, torch.float32)):
+                if t is not None and (tuple(t.shape) != shape or t.dtype != dtype):
+                    raise ValueError(f"8-bit {name}: {tuple(t.shape)} {t.dtype}, this layer takes {shape} {dtype}")
+
     def forward_q8(self, w: LayerWeights, q: Q8Experts):
         """The forward of a bf16 layer with the experts in 8-bit integers (inference, prompts above all: nothing is saved, no
         backward can follow; w's expert weights are not read and may be None)."""
         if self.cfg.dtype != "bf16":
             raise ValueError("experts in 8-bit integers are for bf16 layers")
+        self._check_q8(q)
         if self.ws_q8 is None:
             self.ws_q8 = torch.empty(P.moe_workspace_size(self.desc, P.MOE_WS_FFN_Q8), dtype=torch.uint8,
                                      device=self.device)

@@ -135,3 +135,22 @@ def test_backward_after_the_layers_ran_elsewhere(calls):
     with pytest.raises(RuntimeError, match="forward_q8"):
         first.backward(rows(), ws, ns)
     assert not calls
+
+
+def test_8_bit_experts_of_another_layer(calls):
+    """Codes and scales of other sizes or types than the layer's would be read past their end."""
+    G, d, f = CFG.n_groups, CFG.d, CFG.f
+    layer = MoELayer(CFG, device="cpu")
+
+    def part(n, rows_, cols, codes=torch.int8, scales=torch.float32):
+        return torch.zeros(n, rows_, cols, dtype=codes), torch.zeros(n, rows_, dtype=scales)
+    up, down = part(G, f, d), part(G, d, f)
+    bad = {"gate": [part(G - 1, f, d), part(G, f // 2, d), part(G, d, f), part(G, f, d, codes=torch.uint8), (up[0], up[1][:, :-1])],
+           "up": [part(G, f, 2 * d), part(G, f, d, scales=torch.bfloat16)], "down": [up, (down[0], up[1])]}
+    for name, parts in bad.items():
+        for p in parts:
+            with pytest.raises(ValueError, match=name):
+                layer.forward_q8(weights(), Q8Experts(**{**dict(gate=up, up=up, down=down), name: p}))
+    assert not calls
+    layer.forward_q8(weights(), Q8Experts(up, up, down))
+    assert calls
