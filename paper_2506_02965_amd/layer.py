@@ -454,16 +454,20 @@ class MoEStack:
 
 
 def training_footprint(cfg, local_count: int, master: bool = True, checkpoint: bool = False,
-                       shared_saved: bool = False) -> dict:
+                       shared_saved: bool = False, update: str = "adamw") -> dict:
     """Device bytes one party allocates for the expert layer's training step (route, permute, expert FFN forward
-    and backward, combine and its adjoint, router adjoint, expert AdamW update) when it hosts `local_count` of the
+    and backward, combine and its adjoint, router adjoint, expert update) when it hosts `local_count` of the
     cfg.E routed experts, by category:
       expert_state  hosted experts' weights and weight gradients (dtype) plus fp32 moments and master copy;
       activations   row-space buffers (capacity T*k + S*T rows), saved activations and the FFN workspaces;
       owner         the owner-side buffers of its own T tokens (input, router, combine, input gradient).
     checkpoint: with the 8-bit checkpoint of a MoELayer(checkpoint=True). shared_saved: without the saved activations, for
     a layer that is given a buffer which all the layers of a stack share, and whose size is returned as `shared_saved`.
-    The sizes are those MoELayer and init_update_state allocate, with workspace sizes from the library."""
+    update: "adamw", or "muon" or "muon_precise" for update_muon, with one moment and a workspace, returned as `update_ws`.
+    The sizes are those MoELayer, init_update_state and init_muon_state allocate, with workspace sizes from the library."""
+    muon_ws = {"muon": P.MOE_WS_UPDATE_MUON, "muon_precise": P.MOE_WS_UPDATE_MUON_PRECISE}
+    if update != "adamw" and update not in muon_ws:
+        raise ValueError(f"update {update!r} is not 'adamw', 'muon' or 'muon_precise'")
     if shared_saved and not checkpoint:
         raise ValueError("a shared saved buffer needs checkpoint=True")
     T, d, f, E, k, S = cfg.T, cfg.d, cfg.f, cfg.E, cfg.k, cfg.n_shared
@@ -472,7 +476,9 @@ def training_footprint(cfg, local_count: int, master: bool = True, checkpoint: b
     ws = lambda which: max(P.moe_workspace_size(desc, which), 1)
     G, R = local_count + S, T * k + S * T
     params = G * 3 * f * d
-    expert_state = params * es * 2 + params * 4 * (3 if master else 2)
+    moments = 2 if update == "adamw" else 1
+    expert_state = params * es * 2 + params * 4 * (moments + (1 if master else 0))
+    update_ws = P.moe_workspace_size(desc, muon_ws[update]) if update in muon_ws else 0
     activations = (T * k * d * es            # x_perm
                    + R * d * es              # y_perm
                    + T * k * d * es          # dy_perm
@@ -487,7 +493,9 @@ def training_footprint(cfg, local_count: int, master: bool = True, checkpoint: b
              + T * k * (4 + 4 + 4)           # topk_idx, topk_w, dgate
              + ws(P.MOE_WS_ROUTE_BWD))
     out = {"local_experts": local_count, "expert_state": expert_state, "activations": activations, "owner": owner,
-           "total": expert_state + activations + owner}
+           "total": expert_state + activations + owner + update_ws}
+    if update in muon_ws:
+        out["update_ws"] = update_ws
     if shared_saved:
         out["shared_saved"] = ws(P.MOE_WS_FFN_SAVED)
     return out
