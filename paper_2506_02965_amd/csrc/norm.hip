@@ -2,8 +2,8 @@
 //
 // RMS: N(v) = v / sqrt(mean(v^2) + eps) * w; LAYER: the same of v - mean(v). With vhat = N(v) / w and a = dN w,
 // dv = (a - vhat mean(a vhat) [- mean(a)]) / sqrt(...). Both passes are bound by memory: every row is read once, kept in
-// registers and written once. Squares and row sums are added up in fp64, so that no row of finite numbers overflows and a
-// mean far from zero costs no digits; everything else is fp32, rounded once on the way out.
+// registers and written once. Squares and row sums are added up in fp64, so that no row of finite numbers overflows, and means
+// are kept in two fp32 parts, so that one far from zero costs no digits; everything else is fp32, rounded once on the way out.
 // 16384 x 2048 bf16 with a post norm and a gate: 268 MB in 44 us alone and 51 among other passes. Adjoint of 8192 x 4096: 403 MB
 // in 67 + 5; of 777 x 1024 fp32 with layer norms 10 + 4, two launches and a row's three sums one after the other.
 #include "expert_ops.h"
@@ -103,6 +103,29 @@ __device__ __forceinline__ Sums block_sum(Sums v, SumLds& lds, int& turn) {
   return t;
 }
 
+// A value that all lanes hold, in a scalar register where S.
+template <bool S = true>
+__device__ __forceinline__ float uniform(float v) {
+  return S ? __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))) : v;
+}
+
+// A mean as two fp32 parts. v - hi is exact where v is within a factor of two of it, so that v - mean is off by its own rounding
+// only, however far the mean is above the deviation (rounded to fp32 alone, a mean of 1e4 deviations would move every v of the
+// row by up to 2^-11 of one).
+struct Mean {
+  float hi = 0.f, lo = 0.f;
+  __device__ __forceinline__ Mean() {}
+  __device__ __forceinline__ explicit Mean(double m) : hi((float)m), lo((float)(m - (double)(float)m)) {}
+  template <bool S>
+  __device__ __forceinline__ Mean in() const {
+    Mean m;
+    m.hi = uniform<S>(hi);
+    m.lo = uniform<S>(lo);
+    return m;
+  }
+  __device__ __forceinline__ float from(float v) const { return (v - hi) - lo; }  // v - mean
+};
+
 // 1 / sqrt(v) to fp32: the hardware's estimate (23 bits) and a Newton step, in fp64 for its range.
 __device__ __forceinline__ float rsqrt_of(double v) {
   const double y = __builtin_amdgcn_rsq(v);
@@ -130,7 +153,8 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
         xc[i] = in ? ld_chunk((const Chunk*)a.x + row + c) : zero_chunk();
         gc[i] = gate && in ? ld_chunk(gate + c) : zero_chunk();
       }
-      float mean = 0.f, rstd = 1.f;
+      Mean mean;
+      float rstd = 1.f;
       if (a.post == MOE_NORM_LAYER) {
         Sums s{0., 0., 0.f, 0.f};
 #pragma unroll
@@ -140,7 +164,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
 #pragma unroll
           for (int e = 0; e < EP; ++e) s.d0 += (double)y[e];
         }
-        mean = (float)(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d);
+        mean = Mean(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d);
       }
       if (a.post != MOE_NORM_NONE) {
         Sums s{0., 0., 0.f, 0.f};
@@ -151,7 +175,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
           chunk_to_f<T>(yc[i], y);
           if (in)
 #pragma unroll
-            for (int e = 0; e < EP; ++e) s.d0 += (double)(y[e] - mean) * (double)(y[e] - mean);
+            for (int e = 0; e < EP; ++e) s.d0 += (double)mean.from(y[e]) * (double)mean.from(y[e]);
         }
         rstd = rsqrt_of(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d + a.eps);
       }
@@ -165,7 +189,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
         chunk_to_f<T>(a.w_post && in ? ld_chunk((const Chunk*)a.w_post + c) : zero_chunk(), w);
 #pragma unroll
         for (int e = 0; e < EP; ++e) {
-          float n = (y[e] - mean) * rstd;
+          float n = mean.from(y[e]) * rstd;
           if (a.w_post) n *= w[e];
           if (gate) n *= g[e];
           v[i][e] = a.alpha * x[e] + n;
@@ -180,7 +204,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
       }
     }
     if (a.pre == MOE_NORM_NONE) continue;
-    float mean = 0.f;
+    Mean mean;
     if (a.pre == MOE_NORM_LAYER) {
       Sums s{0., 0., 0.f, 0.f};
 #pragma unroll
@@ -190,7 +214,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
 #pragma unroll
           for (int e = 0; e < EP; ++e) s.d0 += (double)v[i][e];
       }
-      mean = (float)(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d);
+      mean = Mean(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d);
     }
     Sums s{0., 0., 0.f, 0.f};
 #pragma unroll
@@ -198,7 +222,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
       PIECE(i);
       if (in)
 #pragma unroll
-        for (int e = 0; e < EP; ++e) s.d0 += (double)(v[i][e] - mean) * (double)(v[i][e] - mean);
+        for (int e = 0; e < EP; ++e) s.d0 += (double)mean.from(v[i][e]) * (double)mean.from(v[i][e]);
     }
     const float rstd = rsqrt_of(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d + a.eps);
 #pragma unroll
@@ -209,7 +233,7 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
       if (a.w_pre) chunk_to_f<T>(ld_chunk((const Chunk*)a.w_pre + c), w);
 #pragma unroll
       for (int e = 0; e < EP; ++e) {
-        o[e] = (v[i][e] - mean) * rstd;
+        o[e] = mean.from(v[i][e]) * rstd;
         if (a.w_pre) o[e] *= w[e];
       }
       st_chunk((Chunk*)a.h + row + c, f_to_chunk<T>(o));
@@ -225,6 +249,8 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
   __shared__ SumLds lds;
   int turn = 0;
   const bool need_y = a.y && (POST || a.gate);
+  // Row sums in scalar registers where vector registers are short (8192 x 7168 bf16 176 -> 168 us; 8192 x 4096 96 -> 98).
+  constexpr bool SCALAR = CPT * EP > 8;
   const bool lr = PRE && a.pre == MOE_NORM_LAYER, ly = POST && a.post == MOE_NORM_LAYER;
   float s_pre[CPT][EP], s_post[CPT][EP], s_gate[CPT][EP];
   Chunk wpre[CPT], wpost[CPT], gc[CPT];
@@ -286,7 +312,8 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
       }
       fetch(t + 1, t + 1 < t1);
       // row sums: of r and y (LAYER), then of their squares with those of a = dh w_pre
-      float mr = 0.f, my = 0.f, ma = 0.f, rr = 1.f, ry = 1.f, car = 0.f;
+      Mean mr, my;
+      float ma = 0.f, rr = 1.f, ry = 1.f, car = 0.f;
       if (lr || ly) {
         Sums s{0., 0., 0.f, 0.f};
 #pragma unroll
@@ -304,8 +331,8 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
           }
         }
         s = block_sum<2, 1>(s, lds, turn);
-        if (lr) mr = (float)(s.d0 * a.inv_d);
-        if (ly) my = (float)(s.d1 * a.inv_d);
+        if (lr) mr = Mean(s.d0 * a.inv_d).template in<SCALAR>();
+        if (ly) my = Mean(s.d1 * a.inv_d).template in<SCALAR>();
         if (lr) ma = (float)((double)s.f0 * a.inv_d);
       }
       if (PRE || POST) {
@@ -321,17 +348,17 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
           if (in)
 #pragma unroll
             for (int e = 0; e < EP; ++e) {
-              if (PRE) s.d0 += (double)(r[e] - mr) * (double)(r[e] - mr);
-              if (POST) s.d1 += (double)(y[e] - my) * (double)(y[e] - my);
-              if (PRE) s.f0 += (a.w_pre ? dh[e] * w[e] : dh[e]) * (r[e] - mr);
+              if (PRE) s.d0 += (double)mr.from(r[e]) * (double)mr.from(r[e]);
+              if (POST) s.d1 += (double)my.from(y[e]) * (double)my.from(y[e]);
+              if (PRE) s.f0 += (a.w_pre ? dh[e] * w[e] : dh[e]) * mr.from(r[e]);
             }
         }
         if (PRE && POST) s = block_sum<2, 1>(s, lds, turn);
         else if (PRE) s = block_sum<1, 1>(s, lds, turn);
         else s = block_sum<2, 0>(s, lds, turn);
-        if (PRE) rr = rsqrt_of(s.d0 * a.inv_d + a.eps);
-        if (POST) ry = rsqrt_of(s.d1 * a.inv_d + a.eps);
-        if (PRE) car = (float)((double)s.f0 * a.inv_d) * rr;  // mean(a rhat)
+        if (PRE) rr = uniform<SCALAR>(rsqrt_of(s.d0 * a.inv_d + a.eps));
+        if (POST) ry = uniform<SCALAR>(rsqrt_of(s.d1 * a.inv_d + a.eps));
+        if (PRE) car = uniform<SCALAR>((float)((double)s.f0 * a.inv_d) * rr);  // mean(a rhat)
       }
       float b[CPT][EP];  // gradient of r, then of post(y)
       Sums s{0., 0., 0.f, 0.f};
@@ -350,12 +377,12 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
         for (int e = 0; e < EP; ++e) {
           float gr = dr[e];
           if (PRE) {
-            const float rhat = (r[e] - mr) * rr;
+            const float rhat = mr.from(r[e]) * rr;
             gr += (((a.w_pre ? dh[e] * w[e] : dh[e]) - ma) - rhat * car) * rr;
             s_pre[i][e] += dh[e] * rhat;
           }
           o[e] = a.alpha * gr;
-          const float yhat = (y[e] - my) * ry;
+          const float yhat = my.from(y[e]) * ry;
           if (a.gate) s_gate[i][e] += gr * (POST && a.w_post ? yhat * wp[e] : yhat);
           b[i][e] = a.gate ? gr * gt[e] : gr;
           if (POST) {
@@ -378,7 +405,7 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
           float y[EP];
           chunk_to_f<T>(yc[i], y);
 #pragma unroll
-          for (int e = 0; e < EP; ++e) b[i][e] = ((b[i][e] - mb) - (y[e] - my) * ry * cy) * ry;
+          for (int e = 0; e < EP; ++e) b[i][e] = ((b[i][e] - mb) - my.from(y[e]) * ry * cy) * ry;
         }
       }
 #pragma unroll
