@@ -2,8 +2,9 @@
 //
 // RMS: N(v) = v / sqrt(mean(v^2) + eps) * w; LAYER: the same of v - mean(v). With vhat = N(v) / w and a = dN w,
 // dv = (a - vhat mean(a vhat) [- mean(a)]) / sqrt(...). Both passes are bound by memory: every row is read once, kept in
-// registers and written once. Squares and row sums are added up in fp64, so that no row of finite numbers overflows, and means
-// are kept in two fp32 parts, so that one far from zero costs no digits; everything else is fp32, rounded once on the way out.
+// registers and written once. Row sums are fp64, those of products with gradients fp64 sums of a chunk's in fp32, so that none
+// overflows whose row and gradients do not, and means are kept in two fp32 parts, so that one far from zero costs no digits;
+// everything else is fp32, rounded once on the way out.
 // 16384 x 2048 bf16 with a post norm and a gate: 268 MB in 44 us alone and 51 among other passes. Adjoint of 8192 x 4096: 403 MB
 // in 67 + 5; of 777 x 1024 fp32 with layer norms 10 + 4, two launches and a row's three sums one after the other.
 #include "expert_ops.h"
@@ -37,18 +38,11 @@ struct NormArgs {
 
 // Sum over a wavefront, in every lane: DPP within 16 lanes, then the four row sums from scalar registers.
 template <int CTRL>
-__device__ __forceinline__ float dpp(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-template <int CTRL>
 __device__ __forceinline__ double dpp(double v) {
   const uint64_t b = (uint64_t)__double_as_longlong(v);
   const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xf, 0xf, true);
   const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xf, 0xf, true);
   return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
-}
-__device__ __forceinline__ float lane_of(float v, int l) {
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l));
 }
 __device__ __forceinline__ double lane_of(double v, int l) {
   const uint64_t b = (uint64_t)__double_as_longlong(v);
@@ -56,8 +50,7 @@ __device__ __forceinline__ double lane_of(double v, int l) {
   const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), l);
   return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
 }
-template <typename F>
-__device__ __forceinline__ F sum64(F v) {
+__device__ __forceinline__ double sum64(double v) {
   v += dpp<0xb1>(v);   // lanes 1 apart
   v += dpp<0x4e>(v);   // 2 apart
   v += dpp<0x141>(v);  // mirrored within 8
@@ -65,40 +58,30 @@ __device__ __forceinline__ F sum64(F v) {
   return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
 
-// Sums of up to two fp64 and two fp32 values over the workgroup's wavefronts (D, F: how many; the others are left alone).
-// Consecutive calls alternate between two halves of `lds`: a wavefront that writes a half again has passed the barrier that the
-// others reach after reading it.
+// Sums of N fp64 values over the workgroup's wavefronts. Consecutive calls alternate between two halves of `lds`: a wavefront that
+// writes a half again has passed the barrier that the others reach after reading it.
+constexpr int kMaxSums = 3;
 struct Sums {
-  double d0, d1;
-  float f0, f1;
+  double v[kMaxSums];
 };
 struct SumLds {
   Sums s[2][kMaxWaves];
 };
-template <int D, int F>
+template <int N>
 __device__ __forceinline__ Sums block_sum(Sums v, SumLds& lds, int& turn) {
-  if (D > 0) v.d0 = sum64(v.d0);
-  if (D > 1) v.d1 = sum64(v.d1);
-  if (F > 0) v.f0 = sum64(v.f0);
-  if (F > 1) v.f1 = sum64(v.f1);
+#pragma unroll
+  for (int k = 0; k < N; ++k) v.v[k] = sum64(v.v[k]);
   const int waves = blockDim.x >> 6;
   if (waves == 1) return v;
   Sums* at = lds.s[turn];
-  if ((threadIdx.x & 63) == 0) {
-    Sums& to = at[threadIdx.x >> 6];
-    if (D > 0) to.d0 = v.d0;
-    if (D > 1) to.d1 = v.d1;
-    if (F > 0) to.f0 = v.f0;
-    if (F > 1) to.f1 = v.f1;
-  }
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int k = 0; k < N; ++k) at[threadIdx.x >> 6].v[k] = v.v[k];
   __syncthreads();
-  Sums t{0., 0., 0.f, 0.f};
-  for (int w = 0; w < waves; ++w) {
-    if (D > 0) t.d0 += at[w].d0;
-    if (D > 1) t.d1 += at[w].d1;
-    if (F > 0) t.f0 += at[w].f0;
-    if (F > 1) t.f1 += at[w].f1;
-  }
+  Sums t{};
+  for (int w = 0; w < waves; ++w)
+#pragma unroll
+    for (int k = 0; k < N; ++k) t.v[k] += at[w].v[k];
   turn ^= 1;
   return t;
 }
@@ -124,6 +107,15 @@ struct Mean {
     return m;
   }
   __device__ __forceinline__ float from(float v) const { return (v - hi) - lo; }  // v - mean
+};
+
+// A power of two that takes a chunk's differences from the mean, of which q is the sum of squares, to about one, and back: their
+// products with gradients are added up in fp32 within a chunk, where those of rows above 1e19 could overflow.
+struct Scale {
+  int e;
+  __device__ __forceinline__ explicit Scale(double q) : e(max(-100, min(120, (((__double2hiint(q) >> 20) & 0x7ff) - 1023) >> 1))) {}
+  __device__ __forceinline__ float down() const { return __int_as_float((127 - e) << 23); }
+  __device__ __forceinline__ double up() const { return __hiloint2double((1023 + e) << 20, 0); }
 };
 
 // 1 / sqrt(v) to fp32: the hardware's estimate (23 bits) and a Newton step, in fp64 for its range.
@@ -156,18 +148,18 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
       Mean mean;
       float rstd = 1.f;
       if (a.post == MOE_NORM_LAYER) {
-        Sums s{0., 0., 0.f, 0.f};
+        Sums s{};
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
           float y[EP];
           chunk_to_f<T>(yc[i], y);
 #pragma unroll
-          for (int e = 0; e < EP; ++e) s.d0 += (double)y[e];
+          for (int e = 0; e < EP; ++e) s.v[0] += (double)y[e];
         }
-        mean = Mean(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d);
+        mean = Mean(block_sum<1>(s, lds, turn).v[0] * a.inv_d);
       }
       if (a.post != MOE_NORM_NONE) {
-        Sums s{0., 0., 0.f, 0.f};
+        Sums s{};
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
           PIECE(i);
@@ -175,9 +167,9 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
           chunk_to_f<T>(yc[i], y);
           if (in)
 #pragma unroll
-            for (int e = 0; e < EP; ++e) s.d0 += (double)mean.from(y[e]) * (double)mean.from(y[e]);
+            for (int e = 0; e < EP; ++e) s.v[0] += (double)mean.from(y[e]) * (double)mean.from(y[e]);
         }
-        rstd = rsqrt_of(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d + a.eps);
+        rstd = rsqrt_of(block_sum<1>(s, lds, turn).v[0] * a.inv_d + a.eps);
       }
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
@@ -206,25 +198,25 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
     if (a.pre == MOE_NORM_NONE) continue;
     Mean mean;
     if (a.pre == MOE_NORM_LAYER) {
-      Sums s{0., 0., 0.f, 0.f};
+      Sums s{};
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
         PIECE(i);
         if (in)
 #pragma unroll
-          for (int e = 0; e < EP; ++e) s.d0 += (double)v[i][e];
+          for (int e = 0; e < EP; ++e) s.v[0] += (double)v[i][e];
       }
-      mean = Mean(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d);
+      mean = Mean(block_sum<1>(s, lds, turn).v[0] * a.inv_d);
     }
-    Sums s{0., 0., 0.f, 0.f};
+    Sums s{};
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
       PIECE(i);
       if (in)
 #pragma unroll
-        for (int e = 0; e < EP; ++e) s.d0 += (double)mean.from(v[i][e]) * (double)mean.from(v[i][e]);
+        for (int e = 0; e < EP; ++e) s.v[0] += (double)mean.from(v[i][e]) * (double)mean.from(v[i][e]);
     }
-    const float rstd = rsqrt_of(block_sum<1, 0>(s, lds, turn).d0 * a.inv_d + a.eps);
+    const float rstd = rsqrt_of(block_sum<1>(s, lds, turn).v[0] * a.inv_d + a.eps);
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
       PIECE(i);
@@ -315,7 +307,7 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
       Mean mr, my;
       float ma = 0.f, rr = 1.f, ry = 1.f, car = 0.f;
       if (lr || ly) {
-        Sums s{0., 0., 0.f, 0.f};
+        Sums s{};
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
           float r[EP], y[EP], dh[EP], w[EP];
@@ -323,20 +315,22 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
           chunk_to_f<T>(yc[i], y);
           chunk_to_f<T>(dhc[i], dh);
           chunk_to_f<T>(wpre[i], w);
+          float fa = 0.f;
 #pragma unroll
           for (int e = 0; e < EP; ++e) {
-            if (lr) s.d0 += (double)r[e];
-            if (ly) s.d1 += (double)y[e];
-            if (lr) s.f0 += a.w_pre ? dh[e] * w[e] : dh[e];
+            if (lr) s.v[0] += (double)r[e];
+            if (ly) s.v[1] += (double)y[e];
+            if (lr) fa += a.w_pre ? dh[e] * w[e] : dh[e];
           }
+          s.v[2] += (double)fa;
         }
-        s = block_sum<2, 1>(s, lds, turn);
-        if (lr) mr = Mean(s.d0 * a.inv_d).template in<SCALAR>();
-        if (ly) my = Mean(s.d1 * a.inv_d).template in<SCALAR>();
-        if (lr) ma = (float)((double)s.f0 * a.inv_d);
+        s = block_sum<3>(s, lds, turn);
+        if (lr) mr = Mean(s.v[0] * a.inv_d).template in<SCALAR>();
+        if (ly) my = Mean(s.v[1] * a.inv_d).template in<SCALAR>();
+        if (lr) ma = (float)(s.v[2] * a.inv_d);
       }
       if (PRE || POST) {
-        Sums s{0., 0., 0.f, 0.f};
+        Sums s{};
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
           PIECE(i);
@@ -345,23 +339,32 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
           chunk_to_f<T>(yc[i], y);
           chunk_to_f<T>(dhc[i], dh);
           chunk_to_f<T>(wpre[i], w);
-          if (in)
+          if (!in) continue;
+          if (PRE) {
+            double q = 0.;
 #pragma unroll
             for (int e = 0; e < EP; ++e) {
-              if (PRE) s.d0 += (double)mr.from(r[e]) * (double)mr.from(r[e]);
-              if (POST) s.d1 += (double)my.from(y[e]) * (double)my.from(y[e]);
-              if (PRE) s.f0 += (a.w_pre ? dh[e] * w[e] : dh[e]) * mr.from(r[e]);
+              r[e] = mr.from(r[e]);
+              q += (double)r[e] * (double)r[e];
             }
+            s.v[0] += q;
+            const Scale by(q);
+            float f = 0.f;
+#pragma unroll
+            for (int e = 0; e < EP; ++e) f += (a.w_pre ? dh[e] * w[e] : dh[e]) * (r[e] * by.down());
+            s.v[2] += (double)f * by.up();
+          }
+          if (POST)
+#pragma unroll
+            for (int e = 0; e < EP; ++e) s.v[1] += (double)my.from(y[e]) * (double)my.from(y[e]);
         }
-        if (PRE && POST) s = block_sum<2, 1>(s, lds, turn);
-        else if (PRE) s = block_sum<1, 1>(s, lds, turn);
-        else s = block_sum<2, 0>(s, lds, turn);
-        if (PRE) rr = uniform<SCALAR>(rsqrt_of(s.d0 * a.inv_d + a.eps));
-        if (POST) ry = uniform<SCALAR>(rsqrt_of(s.d1 * a.inv_d + a.eps));
-        if (PRE) car = uniform<SCALAR>((float)((double)s.f0 * a.inv_d) * rr);  // mean(a rhat)
+        s = block_sum<PRE ? 3 : 2>(s, lds, turn);
+        if (PRE) rr = uniform<SCALAR>(rsqrt_of(s.v[0] * a.inv_d + a.eps));
+        if (POST) ry = uniform<SCALAR>(rsqrt_of(s.v[1] * a.inv_d + a.eps));
+        if (PRE) car = uniform<SCALAR>((float)(s.v[2] * a.inv_d * (double)rr));  // mean(a rhat)
       }
       float b[CPT][EP];  // gradient of r, then of post(y)
-      Sums s{0., 0., 0.f, 0.f};
+      Sums s{};
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
         PIECE(i);
@@ -373,6 +376,7 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
         chunk_to_f<T>(wpre[i], w);
         chunk_to_f<T>(wpost[i], wp);
         chunk_to_f<T>(gc[i], gt);
+        float fb = 0.f, fm = 0.f;
 #pragma unroll
         for (int e = 0; e < EP; ++e) {
           float gr = dr[e];
@@ -389,17 +393,21 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
             s_post[i][e] += b[i][e] * yhat;
             if (a.w_post) b[i][e] *= wp[e];
             if (in) {
-              s.f0 += b[i][e] * yhat;
-              if (ly) s.f1 += b[i][e];
+              fb += b[i][e] * yhat;
+              if (ly) fm += b[i][e];
             }
           }
+        }
+        if (POST) {
+          s.v[0] += (double)fb;
+          if (ly) s.v[1] += (double)fm;
         }
         if (in) st_chunk((Chunk*)a.dx + row + c, f_to_chunk<T>(o));
       }
       if (!a.dy) continue;
       if (POST) {
-        s = ly ? block_sum<0, 2>(s, lds, turn) : block_sum<0, 1>(s, lds, turn);
-        const float cy = (float)((double)s.f0 * a.inv_d), mb = (float)((double)s.f1 * a.inv_d);
+        s = ly ? block_sum<2>(s, lds, turn) : block_sum<1>(s, lds, turn);
+        const float cy = (float)(s.v[0] * a.inv_d), mb = (float)(s.v[1] * a.inv_d);
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
           float y[EP];

@@ -1,5 +1,5 @@
 """moe_residual_norm and its adjoint against 64 bits where the other tests' tolerances grow: rows whose mean is far above their
-deviation, and the normed output by the deviation itself.
+deviation, rows next to the end of fp32's range, and the normed output by the deviation itself.
 
 Tolerances, elementwise, from what the kernels round (u = 2^-24, a step's half of fp32; the output's own half step is added):
 - The inputs are exact. A mean is an fp64 sum of d terms here and there, at most 2 d 2^-53 of the terms' size apart, and is held in
@@ -184,3 +184,33 @@ def test_a_mean_far_above_the_deviation(T, d, mean):
     c = Case(x, normal(T, d, mean=2 * mean), normal(T, d), normal(T, d), "layer", "layer", gate=1, alpha=0.0)
     c.forward()
     c.check_backward(x)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("pre,post", [("rms", "rms"), ("layer", "layer"), ("rms", "layer")])
+@pytest.mark.parametrize("T,d", [(64, 4096), (7, 256), (2, 8192)])
+def test_rows_next_to_the_end_of_fp32(T, d, pre, post, dt):
+    """Rows of some 2e37 and up to 3e38, of which sums over a row, and of their products with gradients, pass fp32. Column sums of
+    all tokens hold what such rows add."""
+    normal = normals(9, dt)
+    x, y = normal(T, d), normal(T, d)
+    size = torch.tensor([2e37, 6e37, 1.0, 3e36], device="cuda").repeat(T // 4 + 1)[:T, None]
+    big = lambda v: (v.float() * size).clamp(-3e38, 3e38).to(dt)
+    c = Case(x, big(y), normal(T, d), normal(T, d), pre, post, gate=1)
+    c.check_backward(c.forward()[0])                       # y of any size, r of ordinary ones
+    c = Case(big(x), y, normal(T, d), normal(T, d), pre, post, gate=1, alpha=1.0)
+    r, _ = c.forward()
+    c.check_backward(r)                                    # the residual stream
+    c = Case(big(x), None, normal(T, d), normal(T, d), pre, "none")
+    c.forward()
+    c.check_backward(c.x)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("post", ["rms", "layer"])
+def test_large_gradients(post, dt):
+    """Products of gradients and differences up to 1e38 a term, whose sums over a row pass fp32: r and y of 1e8, dh of 1e30."""
+    normal = normals(13, dt)
+    T, d = 33, 2048
+    c = Case(normal(T, d), normal(T, d, std=1e8), normal(T, d, std=1e29), normal(T, d, std=1e30), "rms", post, gate=1)
+    c.check_backward(normal(T, d, std=1e8))
