@@ -508,7 +508,8 @@ NormArgs norm_args(const moe_desc& d, const moe_norm& n, const void* y, const vo
 }
 
 // 16-byte chunks per thread (a power of two) and threads of a workgroup of at most `most`, for rows of cpr chunks. `most` is
-// raised to 1024 for rows that would need more than four; the longest rows (of 5,776 chunks) then take eight.
+// raised to 1024 for rows that would need more than four; the longest fp32 rows (of up to 5,760 chunks; bf16 rows end at 4,080)
+// then take eight.
 struct Shape {
   int p, nt, most;
 };
@@ -528,7 +529,7 @@ void row_kernels(int dtype, const Shape& sh, F&& f) {
     if (sh.p == 1) with(std::integral_constant<int, 1>{});
     else if (sh.p == 2) with(std::integral_constant<int, 2>{});
     else if (sh.p == 4) with(std::integral_constant<int, 4>{});
-    else f(t, std::integral_constant<int, 8>{}, std::integral_constant<int, 1024>{});
+    else if constexpr (std::is_same<decltype(t), float>::value) f(t, std::integral_constant<int, 8>{}, std::integral_constant<int, 1024>{});
   };
   if (dtype == MOE_BF16) one(bf16{});
   else one(float{});
