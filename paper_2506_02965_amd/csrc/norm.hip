@@ -1,10 +1,10 @@
 // What stands between two layers of a stack: r = alpha x + gamma * post(y), h = pre(r), and the adjoint of both.
 //
 // RMS: N(v) = v / sqrt(mean(v^2) + eps) * w; LAYER: the same of v - mean(v). With vhat = N(v) / w and a = dN w,
-// dv = (a - vhat mean(a vhat) [- mean(a)]) / sqrt(...). Both passes are bound by memory: every row is read once, kept in
-// registers and written once. Row sums are fp64, those of products with gradients fp64 sums of a chunk's in fp32, so that none
-// overflows whose row and gradients do not, and means are kept in two fp32 parts, so that one far from zero costs no digits;
-// everything else is fp32, rounded once on the way out.
+// dv = (a - vhat mean(a vhat) [- mean(a)]) / sqrt(...). Both passes are bound by memory: every row is read once and written once
+// (what the adjoint uses again of its longest rows comes from the L2). Row sums are fp64, those of products with gradients fp64
+// sums of a chunk's in fp32, so that none overflows whose row and gradients do not, and means are kept in two fp32 parts, so that
+// one far from zero costs no digits; everything else is fp32, rounded once on the way out.
 // 16384 x 2048 bf16 with a post norm and a gate: 268 MB in 44 us alone and 51 among other passes. Adjoint of 8192 x 4096: 403 MB
 // in 67 + 5; of 777 x 1024 fp32 with layer norms 10 + 4, two launches and a row's three sums one after the other.
 #include "expert_ops.h"
@@ -233,26 +233,90 @@ __global__ __launch_bounds__(NT) void residual_norm_kernel(NormArgs a) {
   }
 }
 
-// Adjoint. A workgroup walks over the rows of a part of a gate row's tokens (or over whole gate rows) and keeps the sums over
-// tokens of its columns in registers; norm_sums_kernel adds the workgroups' up in a fixed order.
-template <typename T, int CPT, int NT, bool PRE, bool POST>
-__global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
-  constexpr int EP = EPC<T>::value;
+template <typename T>
+__device__ __forceinline__ Chunk ones() {
+  Chunk c;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c.w[i] = std::is_same<T, float>::value ? 0x3f800000u : 0x3f803f80u;
+  return c;
+}
+// What goes into v is computed here. Sums that are used much later would be formed there, and their operands kept until then.
+template <typename V>
+__device__ __forceinline__ void settle(V& v) {
+  asm volatile("" : "+v"(v));
+}
+// What was unpacked from a chunk is unpacked again after this, not kept.
+__device__ __forceinline__ void forget(Chunk& c) {
+  asm volatile("" : "+v"(c.w[0]), "+v"(c.w[1]), "+v"(c.w[2]), "+v"(c.w[3]));
+}
+// Loads of the next chunk stay behind this.
+__device__ __forceinline__ void next_chunk() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Adjoint. A workgroup walks over the rows of a part of a gate row's tokens (or over whole gate rows) and keeps two sums over
+// tokens of its columns in registers; norm_sums_kernel adds the workgroups' up in a fixed order. With g the gradient of r they are
+// dh rhat and, of a gate row's tokens, c = g yhat: the gate's gradient is w_post c, that of w_post the sum of gate c over gate rows.
+//
+// What else a row needs is kept in registers as far as they go; nothing is spilled to memory but a few words where stated:
+//   up to 1024 chunks (8,192 bf16, 4,096 fp32)   the row, the next row's loads, weights and gate; a third sum (w_post's) if MANY
+//   up to 2048, 512 threads of up to four chunks  the row; weights and gate come from the L2 for every row
+//   above, 1024 threads of up to six              the sums alone; each of a row's rounds loads its chunks again, from the L2
+// us, before (all of it in registers for every length, up to 3.7 KB a lane spilled) and now, of 6 T d elements through memory at
+// the copy's rate: bf16 with post norm and gate 4096 x 12288 1,265 -> 195 (117), 4096 x 16384 1,461 -> 283 (156), 2048 x 28672
+// 1,923 -> 330 (136), without 490 -> 123, 573 -> 167, 1,066 -> 173; fp32 with 4096 x 8192 329 -> 213 (156), 2048 x 20480 1,775 ->
+// 385 (194). The rounds' dependent loads and sums bound them; the two norms' rounds are one after the other.
+// One-chunk bf16 rows with two workgroups a CU (128 registers, 12 bytes spilled): 8192 x 2560 with layer norms 109 -> 82.
+template <typename T, int CPT, int NT, bool PRE, bool POST, bool MANY>
+__global__ __launch_bounds__(NT, (CPT == 1 && sizeof(T) == 2 && !MANY ? 4 : 1))
+void residual_norm_bwd_kernel(NormArgs a) {
+  constexpr int EP = EPC<T>::value, N = CPT * EP, BYTES = CPT * 16;
+  constexpr bool BF16 = std::is_same<T, bf16>::value;
+  constexpr bool KEEP = NT <= 512;                  // a row's chunks stay in registers; else they are loaded again (from the L2)
+  constexpr bool AHEAD = KEEP && BYTES <= 32;       // the next row's are on their way while a row is worked on
+  constexpr bool KEEP_W = BYTES <= 32;              // weights and gate stay too
+  constexpr bool KEEP_B = POST && KEEP && BYTES <= 48;  // the gradient of post(y) stays until its row sums are there
+  constexpr bool LONG = !KEEP || N > 16;            // chunk after chunk, nothing moved from one to another
+  constexpr bool FORGET = BF16 && N > 16, FORGET_W = FORGET || (BF16 && MANY && N > 8);  // values are unpacked where they are used
+  // Row sums in scalar registers where vector registers are short (8192 x 7168 bf16 176 -> 168 us; 8192 x 4096 96 -> 98).
+  constexpr bool SCALAR = N > 8;
   __shared__ SumLds lds;
   int turn = 0;
   const bool need_y = a.y && (POST || a.gate);
-  // Row sums in scalar registers where vector registers are short (8192 x 7168 bf16 176 -> 168 us; 8192 x 4096 96 -> 98).
-  constexpr bool SCALAR = CPT * EP > 8;
   const bool lr = PRE && a.pre == MOE_NORM_LAYER, ly = POST && a.post == MOE_NORM_LAYER;
-  float s_pre[CPT][EP], s_post[CPT][EP], s_gate[CPT][EP];
-  Chunk wpre[CPT], wpost[CPT], gc[CPT];
+  // Sums over tokens: dh rhat, and g yhat of the present gate row, from which the gate's gradient (by w_post) and w_post's (by the
+  // gate, summed over gate rows) are made
+  float s_pre[CPT][EP], s_y[CPT][EP], s_post[MANY ? CPT : 1][EP];
+  Chunk wk[3][KEEP_W ? CPT : 1];
+  // chunk c of row t of p
+  const auto ld = [&](const void* p, int t, int c, bool there) {
+    return buf_ld16(buf_rsrc(p ? (const char*)p + (size_t)t * (uint32_t)(a.cpr * 16) : nullptr, p && there ? a.cpr * 16 : 0), c * 16);
+  };
+  const auto st = [&](void* p, int t, int c, const Chunk& v) {
+    typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{v.w[0], v.w[1], v.w[2], v.w[3]},
+                                           buf_rsrc((char*)p + (size_t)t * (uint32_t)(a.cpr * 16), a.cpr * 16), c * 16, 0, 0);
+  };
+  // chunk c of w_pre (0), w_post (1) or row g of the gate (2); ones where there is none
+  const auto ld_w = [&](int k, int g, int c) {
+    const void* p = k == 0 ? (PRE ? a.w_pre : nullptr) : k == 1 ? (POST ? a.w_post : nullptr) : a.gate;
+    return p ? ld(p, k == 2 ? g : 0, c, true) : ones<T>();
+  };
+  const auto put_sums = [&](float* out, int c, const float* v) {  // a chunk's columns
+#pragma unroll
+    for (int e = 0; e < EP; e += 4) st_chunk((float*)((char*)out + (uint32_t)(c * EP * 4)) + e, f_to_chunk<float>(v + e));
+  };
 #pragma unroll
   for (int i = 0; i < CPT; ++i) {
-    PIECE(i);
-    wpre[i] = PRE && a.w_pre && in ? ld_chunk((const Chunk*)a.w_pre + c) : zero_chunk();
-    wpost[i] = POST && a.w_post && in ? ld_chunk((const Chunk*)a.w_post + c) : zero_chunk();
+    if constexpr (KEEP_W)
 #pragma unroll
-    for (int e = 0; e < EP; ++e) s_pre[i][e] = s_post[i][e] = 0.f;
+      for (int k = 0; k < 2; ++k) wk[k][i] = ld_w(k, 0, threadIdx.x + i * blockDim.x);
+#pragma unroll
+    for (int e = 0; e < EP; ++e) s_pre[i][e] = 0.f;
+    if (MANY)
+#pragma unroll
+      for (int e = 0; e < EP; ++e) s_post[i][e] = 0.f;
   }
   // gate rows of this workgroup, and its tokens of each
   int g0, g1, first, last;
@@ -268,41 +332,52 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
     first = 0;
     last = a.gate_rows;
   }
+  float* const o_pre = a.direct ? a.dw_pre : a.part + (size_t)blockIdx.x * a.d;
+  float* const o_post = a.direct ? a.dw_post : a.part + ((size_t)a.n_part + blockIdx.x) * a.d;
   for (int g = g0; g < g1; ++g) {
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
-      PIECE(i);
-      gc[i] = a.gate && in ? ld_chunk((const Chunk*)a.gate + (size_t)g * a.cpr + c) : zero_chunk();
+      if constexpr (KEEP_W) wk[2][i] = ld_w(2, g, threadIdx.x + i * blockDim.x);
 #pragma unroll
-      for (int e = 0; e < EP; ++e) s_gate[i][e] = 0.f;
+      for (int e = 0; e < EP; ++e) s_y[i][e] = 0.f;
     }
-    // the next row's chunks are loaded while a row is worked on
-    Chunk next[4][CPT];
-    const auto fetch = [&](int t, bool there) {
-      const size_t row = (size_t)t * a.cpr;
-#pragma unroll
-      for (int i = 0; i < CPT; ++i) {
-        PIECE(i);
-        const bool ld = in && there;
-        next[0][i] = a.dr && ld ? ld_chunk((const Chunk*)a.dr + row + c) : zero_chunk();
-        next[1][i] = PRE && ld ? ld_chunk((const Chunk*)a.dh + row + c) : zero_chunk();
-        next[2][i] = PRE && ld ? ld_chunk((const Chunk*)a.r + row + c) : zero_chunk();
-        next[3][i] = need_y && ld ? ld_chunk((const Chunk*)a.y + row + c) : zero_chunk();
-      }
-    };
     const int t1 = g * a.gate_rows + last;
-    fetch(g * a.gate_rows + first, first < last);
-    for (int t = g * a.gate_rows + first; t < t1; ++t) {
-      const size_t row = (size_t)t * a.cpr;
-      Chunk drc[CPT], dhc[CPT], rc[CPT], yc[CPT];
+    Chunk kept[4][KEEP ? CPT : 1], next[4][AHEAD ? CPT : 1];
+    // chunk i of row t of dr (0), dh (1), r (2) or y (3)
+    const auto load = [&](int k, int t, int i, bool there) {
+      const void* p = k == 0 ? a.dr : k == 1 ? (PRE ? a.dh : nullptr) : k == 2 ? (PRE ? a.r : nullptr) : need_y ? a.y : nullptr;
+      return ld(p, t, threadIdx.x + i * blockDim.x, there);
+    };
+    const auto fetch = [&](auto& to, int t, bool there) {
 #pragma unroll
-      for (int i = 0; i < CPT; ++i) {
-        drc[i] = next[0][i];
-        dhc[i] = next[1][i];
-        rc[i] = next[2][i];
-        yc[i] = next[3][i];
+      for (int i = 0; i < (KEEP ? CPT : 0); ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) to[k][i] = load(k, t, i, there);
+    };
+    if constexpr (AHEAD) fetch(next, g * a.gate_rows + first, first < last);
+    for (int t = g * a.gate_rows + first; t < t1; ++t) {
+      if constexpr (AHEAD) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int i = 0; i < CPT; ++i) kept[k][i] = next[k][i];
+        fetch(next, t + 1, t + 1 < t1);
+      } else if constexpr (KEEP) {
+        fetch(kept, t, true);
       }
-      fetch(t + 1, t + 1 < t1);
+      const auto part = [&](int k, int i, float (&v)[EP]) {
+        if constexpr (KEEP && FORGET) forget(kept[k][i]);
+        if constexpr (KEEP) chunk_to_f<T>(kept[k][i], v);
+        else chunk_to_f<T>(load(k, t, i, true), v);
+      };
+      const auto weight = [&](int k, int i, float (&v)[EP]) {
+        if constexpr (KEEP_W) {
+          if constexpr (FORGET_W) forget(wk[k][i]);
+          chunk_to_f<T>(wk[k][i], v);
+        } else {
+          chunk_to_f<T>(ld_w(k, g, threadIdx.x + i * blockDim.x), v);
+        }
+      };
       // row sums: of r and y (LAYER), then of their squares with those of a = dh w_pre
       Mean mr, my;
       float ma = 0.f, rr = 1.f, ry = 1.f, car = 0.f;
@@ -310,19 +385,21 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
         Sums s{};
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
+          if constexpr (LONG) next_chunk();
           float r[EP], y[EP], dh[EP], w[EP];
-          chunk_to_f<T>(rc[i], r);
-          chunk_to_f<T>(yc[i], y);
-          chunk_to_f<T>(dhc[i], dh);
-          chunk_to_f<T>(wpre[i], w);
+          part(2, i, r);
+          part(3, i, y);
+          part(1, i, dh);
+          weight(0, i, w);
           float fa = 0.f;
 #pragma unroll
           for (int e = 0; e < EP; ++e) {
             if (lr) s.v[0] += (double)r[e];
             if (ly) s.v[1] += (double)y[e];
-            if (lr) fa += a.w_pre ? dh[e] * w[e] : dh[e];
+            if (lr) fa += dh[e] * w[e];
           }
           s.v[2] += (double)fa;
+          if constexpr (LONG) { settle(s.v[0]); settle(s.v[1]); settle(s.v[2]); }
         }
         s = block_sum<3>(s, lds, turn);
         if (lr) mr = Mean(s.v[0] * a.inv_d).template in<SCALAR>();
@@ -334,11 +411,12 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
           PIECE(i);
+          if constexpr (LONG) next_chunk();
           float r[EP], y[EP], dh[EP], w[EP];
-          chunk_to_f<T>(rc[i], r);
-          chunk_to_f<T>(yc[i], y);
-          chunk_to_f<T>(dhc[i], dh);
-          chunk_to_f<T>(wpre[i], w);
+          part(2, i, r);
+          part(3, i, y);
+          part(1, i, dh);
+          weight(0, i, w);
           if (!in) continue;
           if (PRE) {
             double q = 0.;
@@ -351,99 +429,152 @@ __global__ __launch_bounds__(NT) void residual_norm_bwd_kernel(NormArgs a) {
             const Scale by(q);
             float f = 0.f;
 #pragma unroll
-            for (int e = 0; e < EP; ++e) f += (a.w_pre ? dh[e] * w[e] : dh[e]) * (r[e] * by.down());
+            for (int e = 0; e < EP; ++e) f += dh[e] * w[e] * (r[e] * by.down());
             s.v[2] += (double)f * by.up();
           }
           if (POST)
 #pragma unroll
             for (int e = 0; e < EP; ++e) s.v[1] += (double)my.from(y[e]) * (double)my.from(y[e]);
+          if constexpr (LONG) { settle(s.v[0]); settle(s.v[1]); settle(s.v[2]); }
         }
         s = block_sum<PRE ? 3 : 2>(s, lds, turn);
         if (PRE) rr = uniform<SCALAR>(rsqrt_of(s.v[0] * a.inv_d + a.eps));
         if (POST) ry = uniform<SCALAR>(rsqrt_of(s.v[1] * a.inv_d + a.eps));
         if (PRE) car = uniform<SCALAR>((float)(s.v[2] * a.inv_d * (double)rr));  // mean(a rhat)
       }
-      float b[CPT][EP];  // gradient of r, then of post(y)
+      // The gradient g of r; that of post(y) is g by the gate, and by w_post, b.
+      const auto grad = [&](int i, float (&gr)[EP], float (&rhat)[EP]) {
+        float dh[EP], r[EP], w[EP];
+        part(0, i, gr);
+        if (!PRE) return;
+        part(1, i, dh);
+        part(2, i, r);
+        weight(0, i, w);
+#pragma unroll
+        for (int e = 0; e < EP; ++e) {
+          rhat[e] = mr.from(r[e]) * rr;
+          gr[e] += ((dh[e] * w[e] - ma) - rhat[e] * car) * rr;
+          rhat[e] *= dh[e];
+        }
+      };
+      const auto factor = [&](int i, float (&f)[EP]) {  // gate w_post
+        float gt[EP], wp[EP];
+        weight(2, i, gt);
+        weight(1, i, wp);
+#pragma unroll
+        for (int e = 0; e < EP; ++e) f[e] = gt[e] * wp[e];
+      };
+      const auto put_dx = [&](int i, const float (&gr)[EP]) {
+        float o[EP];
+#pragma unroll
+        for (int e = 0; e < EP; ++e) o[e] = a.alpha * gr[e];
+        st(a.dx, t, threadIdx.x + i * blockDim.x, f_to_chunk<T>(o));
+      };
+      const auto put_dy = [&](int i, const float (&b)[EP]) { st(a.dy, t, threadIdx.x + i * blockDim.x, f_to_chunk<T>(b)); };
+      float b[KEEP_B ? CPT : 1][EP];
       Sums s{};
 #pragma unroll
       for (int i = 0; i < CPT; ++i) {
         PIECE(i);
-        float dr[EP], dh[EP], r[EP], y[EP], w[EP], wp[EP], gt[EP], o[EP];
-        chunk_to_f<T>(drc[i], dr);
-        chunk_to_f<T>(dhc[i], dh);
-        chunk_to_f<T>(rc[i], r);
-        chunk_to_f<T>(yc[i], y);
-        chunk_to_f<T>(wpre[i], w);
-        chunk_to_f<T>(wpost[i], wp);
-        chunk_to_f<T>(gc[i], gt);
+        if constexpr (LONG) next_chunk();
+        float gr[EP], rhat[EP], y[EP], f[EP];
+        grad(i, gr, rhat);
+        if (PRE)
+#pragma unroll
+          for (int e = 0; e < EP; ++e) s_pre[i][e] += rhat[e];
+        part(3, i, y);
+        factor(i, f);
+        float (&bi)[EP] = b[KEEP_B ? i : 0];
         float fb = 0.f, fm = 0.f;
 #pragma unroll
         for (int e = 0; e < EP; ++e) {
-          float gr = dr[e];
-          if (PRE) {
-            const float rhat = mr.from(r[e]) * rr;
-            gr += (((a.w_pre ? dh[e] * w[e] : dh[e]) - ma) - rhat * car) * rr;
-            s_pre[i][e] += dh[e] * rhat;
-          }
-          o[e] = a.alpha * gr;
-          const float yhat = my.from(y[e]) * ry;
-          if (a.gate) s_gate[i][e] += gr * (POST && a.w_post ? yhat * wp[e] : yhat);
-          b[i][e] = a.gate ? gr * gt[e] : gr;
+          const float gy = gr[e] * (my.from(y[e]) * ry);
+          s_y[i][e] += gy;
+          bi[e] = gr[e] * f[e];
           if (POST) {
-            s_post[i][e] += b[i][e] * yhat;
-            if (a.w_post) b[i][e] *= wp[e];
-            if (in) {
-              fb += b[i][e] * yhat;
-              if (ly) fm += b[i][e];
-            }
+            fb += gy * f[e];
+            if (ly) fm += bi[e];
           }
         }
-        if (POST) {
+        if (POST && in) {
           s.v[0] += (double)fb;
           if (ly) s.v[1] += (double)fm;
         }
-        if (in) st_chunk((Chunk*)a.dx + row + c, f_to_chunk<T>(o));
+        if constexpr (LONG) {
+          settle(s.v[0]);
+          settle(s.v[1]);
+#pragma unroll
+          for (int e = 0; e < EP; ++e) {
+            if (PRE) settle(s_pre[i][e]);
+            settle(s_y[i][e]);
+          }
+        }
+        // dx may take the place of dr or dh: with POST and without KEEP they are read once more before it is written
+        if (KEEP || !POST) put_dx(i, gr);
+        if (!POST && a.dy) put_dy(i, bi);
       }
-      if (!a.dy) continue;
-      if (POST) {
-        s = ly ? block_sum<2>(s, lds, turn) : block_sum<1>(s, lds, turn);
-        const float cy = (float)(s.v[0] * a.inv_d), mb = (float)(s.v[1] * a.inv_d);
+      if (!POST) continue;
+      s = ly ? block_sum<2>(s, lds, turn) : block_sum<1>(s, lds, turn);
+      const float cy = (float)(s.v[0] * a.inv_d), mb = (float)(s.v[1] * a.inv_d);
 #pragma unroll
-        for (int i = 0; i < CPT; ++i) {
-          float y[EP];
-          chunk_to_f<T>(yc[i], y);
+      for (int i = 0; i < CPT; ++i) {
+        if constexpr (LONG) next_chunk();
+        float gr[EP], rhat[EP], y[EP], f[EP];
+        float (&bi)[EP] = b[KEEP_B ? i : 0];
+        part(3, i, y);
+        if constexpr (!KEEP_B) {
+          grad(i, gr, rhat);
+          factor(i, f);
 #pragma unroll
-          for (int e = 0; e < EP; ++e) b[i][e] = ((b[i][e] - mb) - my.from(y[e]) * ry * cy) * ry;
+          for (int e = 0; e < EP; ++e) bi[e] = gr[e] * f[e];
+        }
+#pragma unroll
+        for (int e = 0; e < EP; ++e) bi[e] = ((bi[e] - mb) - my.from(y[e]) * ry * cy) * ry;
+        if (!KEEP) put_dx(i, gr);
+        put_dy(i, bi);
+      }
+    }
+    if (!POST && !a.gate) continue;
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+      PIECE(i);
+      if (!in) continue;
+      float gt[EP], wp[EP], v[EP];
+      chunk_to_f<T>(KEEP_W ? wk[2][KEEP_W ? i : 0] : ld_w(2, g, c), gt);
+      chunk_to_f<T>(KEEP_W ? wk[1][KEEP_W ? i : 0] : ld_w(1, g, c), wp);
+      if (a.gate) {
+        float* out = a.parts > 1 ? a.part + ((size_t)2 * a.n_part + blockIdx.x) * a.d : a.dgate + (size_t)g * a.d;
+#pragma unroll
+        for (int e = 0; e < EP; ++e) v[e] = s_y[i][e] * wp[e];
+        put_sums(out, c, v);
+      }
+      if (!POST || !a.dw_post) continue;
+#pragma unroll
+      for (int e = 0; e < EP; ++e) v[e] = s_y[i][e] * gt[e];
+      if constexpr (MANY) {
+#pragma unroll
+        for (int e = 0; e < EP; ++e) s_post[i][e] += v[e];
+        if (g + 1 < g1) continue;
+#pragma unroll
+        for (int e = 0; e < EP; ++e) v[e] = s_post[i][e];
+      }
+      if (!MANY && g > g0) {  // to the sum so far, which this thread wrote
+#pragma unroll
+        for (int e = 0; e < EP; e += 4) {
+          float was[4];
+          chunk_to_f<float>(ld_chunk(o_post + c * EP + e), was);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[e + k] += was[k];
         }
       }
-#pragma unroll
-      for (int i = 0; i < CPT; ++i) {
-        PIECE(i);
-        if (in) st_chunk((Chunk*)a.dy + row + c, f_to_chunk<T>(b[i]));
-      }
-    }
-    if (a.gate) {
-      float* out = a.parts > 1 ? a.part + ((size_t)2 * a.n_part + blockIdx.x) * a.d : a.dgate + (size_t)g * a.d;
-#pragma unroll
-      for (int i = 0; i < CPT; ++i) {
-        PIECE(i);
-        if (!in) continue;
-#pragma unroll
-        for (int e = 0; e < EP; e += 4) st_chunk(out + c * EP + e, f_to_chunk<float>(&s_gate[i][e]));
-      }
+      put_sums(o_post, c, v);
     }
   }
-  float* o_pre = a.direct ? a.dw_pre : a.part + (size_t)blockIdx.x * a.d;
-  float* o_post = a.direct ? a.dw_post : a.part + ((size_t)a.n_part + blockIdx.x) * a.d;
+  if (!PRE || !a.dw_pre) return;
 #pragma unroll
   for (int i = 0; i < CPT; ++i) {
     PIECE(i);
-    if (!in) continue;
-#pragma unroll
-    for (int e = 0; e < EP; e += 4) {
-      if (PRE && a.dw_pre) st_chunk(o_pre + c * EP + e, f_to_chunk<float>(&s_pre[i][e]));
-      if (POST && a.dw_post) st_chunk(o_post + c * EP + e, f_to_chunk<float>(&s_post[i][e]));
-    }
+    if (in) put_sums(o_pre, c, s_pre[i]);
   }
 }
 #undef PIECE
@@ -578,19 +709,40 @@ hipError_t launch_residual_norm_bwd(const moe_desc& d, const moe_norm& n, const 
   a.parts = a.groups <= want ? std::min(want / a.groups, a.gate_rows) : 0;
   a.n_part = a.parts ? a.groups * a.parts : want;
   a.direct = a.n_part == 1;
-  const Shape sh = row_shape(a.cpr, 512);
   {
     KernelTimer kt("residual_norm_bwd", s);
-    row_kernels<512>(d.dtype, sh, [&](auto t, auto p, auto most) {
+    const bool pre = n.pre != MOE_NORM_NONE, post = y && n.post != MOE_NORM_NONE;
+    const auto with = [&](auto t, auto p, auto most, auto many) {
       using T = decltype(t);
       constexpr int C = decltype(p)::value, NT = decltype(most)::value;
-      const auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(a.n_part), dim3(sh.nt), 0, s, a); };
-      const bool pre = n.pre != MOE_NORM_NONE, post = y && n.post != MOE_NORM_NONE;
-      if (pre && post) go(residual_norm_bwd_kernel<T, C, NT, true, true>);
-      else if (pre) go(residual_norm_bwd_kernel<T, C, NT, true, false>);
-      else if (post) go(residual_norm_bwd_kernel<T, C, NT, false, true>);
-      else go(residual_norm_bwd_kernel<T, C, NT, false, false>);
-    });
+      constexpr bool M = decltype(many)::value;
+      const int nt = ((a.cpr + C - 1) / C + 63) / 64 * 64;
+      const auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(a.n_part), dim3(nt), 0, s, a); };
+      if (pre && post) go(residual_norm_bwd_kernel<T, C, NT, true, true, M>);
+      else if (pre) go(residual_norm_bwd_kernel<T, C, NT, true, false, false>);
+      else if (post) go(residual_norm_bwd_kernel<T, C, NT, false, true, M>);
+      else go(residual_norm_bwd_kernel<T, C, NT, false, false, false>);
+    };
+    constexpr std::integral_constant<int, 512> half;
+    constexpr std::integral_constant<int, 1024> whole;
+    const auto shapes = [&](auto t) {
+      using T = decltype(t);
+      const auto few = [&](auto p) {
+        if (a.parts) with(t, p, half, std::false_type{});
+        else with(t, p, half, std::true_type{});
+      };
+      // whole gate rows of a workgroup: what w_post's gradient has so far is added to in memory, a gate row at a time
+      const auto more = [&](auto p, auto most) { with(t, p, most, std::false_type{}); };
+      if (a.cpr <= 512) few(std::integral_constant<int, 1>{});
+      else if (a.cpr <= 1024) few(std::integral_constant<int, 2>{});
+      else if (a.cpr <= 1536) more(std::integral_constant<int, 3>{}, half);
+      else if (a.cpr <= 2048) more(std::integral_constant<int, 4>{}, half);
+      else if (a.cpr <= 3072) more(std::integral_constant<int, 3>{}, whole);
+      else if (a.cpr <= 4096) more(std::integral_constant<int, 4>{}, whole);
+      else if constexpr (std::is_same<T, float>::value) more(std::integral_constant<int, 6>{}, whole);  // at most 5,760
+    };
+    if (d.dtype == MOE_BF16) shapes(bf16{});
+    else shapes(float{});
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const bool weights = !a.direct && (a.dw_pre || a.dw_post), gates = gate && a.parts > 1;

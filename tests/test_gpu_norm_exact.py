@@ -214,3 +214,40 @@ def test_large_gradients(post, dt):
     T, d = 33, 2048
     c = Case(normal(T, d), normal(T, d, std=1e8), normal(T, d, std=1e29), normal(T, d, std=1e30), "rms", post, gate=1)
     c.check_backward(normal(T, d, std=1e8))
+
+
+LONG = [(torch.bfloat16, 8704), (torch.bfloat16, 13312), (torch.bfloat16, 18432), (torch.bfloat16, 32640), (torch.float32, 4352),
+        (torch.float32, 7680), (torch.float32, 9088), (torch.float32, 14336), (torch.float32, 23040)]
+
+
+@pytest.mark.parametrize("dt,d", LONG, ids=lambda v: str(v).replace("torch.", ""))
+@pytest.mark.parametrize("T,gate", [(520, 520), (1030, 515), (514, 2), (1, 1)])
+def test_long_rows_and_many_gates(dt, d, T, gate):
+    """More gate rows than workgroups, each with its share of w_post's gradient, and long rows of every kernel."""
+    normal = normals(d + T, dt)
+    c = Case(normal(T, d, std=2.0), normal(T, d, mean=-0.2), normal(T, d), normal(T, d), "layer" if T & 2 else "rms", "rms", gate=gate)
+    r, _ = c.forward()
+    c.check_backward(r)
+
+
+@pytest.mark.parametrize("dt,d", LONG + [(torch.bfloat16, 4096), (torch.bfloat16, 7168), (torch.float32, 3200)],
+                         ids=lambda v: str(v).replace("torch.", ""))
+@pytest.mark.parametrize("pre,post", [("rms", "layer"), ("layer", "none"), ("none", "rms")])
+def test_in_place(dt, d, pre, post):
+    """dx in the place of dr or dh, dy in that of y or dh: the same bits."""
+    normal = normals(d, dt)
+    T = 600
+    c = Case(normal(T, d), normal(T, d), normal(T, d), normal(T, d) if pre != "none" else None, pre, post, gate=3)
+    r, _ = c.forward()
+    want = c.backward(r)
+    n = P.moe_workspace_size(c.desc, P.MOE_WS_NORM_BWD)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    for dx_at, dy_at in (("dr", "y"), ("dh", "y"), ("dr", "dh")):
+        if pre == "none" and "dh" in (dx_at, dy_at):
+            continue
+        t = {k: getattr(c, k).clone() if getattr(c, k) is not None else None for k in ("dr", "dh", "y")}
+        o = {k: torch.full_like(v, 7.0) for k, v in want.items() if k.startswith("d") and v is not None and k not in ("dx", "dy")}
+        P.moe_residual_norm_bwd(c.desc, c.norm, t["dr"], t["dh"], t["y"], r, c.w_post, c.g, c.w_pre, t[dx_at], t[dy_at],
+                                o.get("dw_post"), o.get("dgate"), o.get("dw_pre"), ws, n)
+        assert torch.equal(t[dx_at], want["dx"]) and torch.equal(t[dy_at], want["dy"])
+        assert all(torch.equal(o[k], want[k]) for k in o)
