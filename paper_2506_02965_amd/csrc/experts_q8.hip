@@ -207,10 +207,12 @@ __global__ __launch_bounds__(Q8_THREADS) void q8_rows_h_kernel(Q8Args a, int64_t
 }
 
 // 1 / (1 + exp(-g)) with the hardware's exponential and reciprocal. The exponential of a product rounded to fp32 alone would be
-// |g| roundings off; what the product rounds away is put back.
+// |g| roundings off; what the product rounds away is put back. g stops where the result is one, and where it is 2^-126: the products
+// of numbers next to the end of fp32's range would be infinite, and what they round away not a number.
 __device__ __forceinline__ float sigmoid_of(float g) {
+  g = __builtin_amdgcn_fmed3f(g, -87.3f, 128.f);
   const float t = -1.44269504f * g, r = __builtin_fmaf(-1.44269504f, g, -t) + -1.925963e-8f * g;
-  const float e = __builtin_amdgcn_exp2f(fminf(t, 126.f));
+  const float e = __builtin_amdgcn_exp2f(t);
   return __builtin_amdgcn_rcpf(1.f + __builtin_fmaf(e, 0.693147181f * r, e));
 }
 
