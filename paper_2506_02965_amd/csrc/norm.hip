@@ -6,7 +6,7 @@
 // sums of a chunk's in fp32, so that none overflows whose row and gradients do not, and means are kept in two fp32 parts, so that
 // one far from zero costs no digits; everything else is fp32, rounded once on the way out.
 // 16384 x 2048 bf16 with a post norm and a gate: 268 MB in 44 us alone and 51 among other passes. Adjoint of 8192 x 4096: 403 MB
-// in 67 + 5; of 777 x 1024 fp32 with layer norms 10 + 4, two launches and a row's three sums one after the other.
+// in 68 + 5; of 777 x 1024 fp32 with layer norms 11 + 4, two launches and a row's three sums one after the other.
 #include "expert_ops.h"
 
 #include <algorithm>
@@ -86,12 +86,6 @@ __device__ __forceinline__ Sums block_sum(Sums v, SumLds& lds, int& turn) {
   return t;
 }
 
-// A value that all lanes hold, in a scalar register where S.
-template <bool S = true>
-__device__ __forceinline__ float uniform(float v) {
-  return S ? __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))) : v;
-}
-
 // A mean as two fp32 parts. v - hi is exact where v is within a factor of two of it, so that v - mean is off by its own rounding
 // only, however far the mean is above the deviation (rounded to fp32 alone, a mean of 1e4 deviations would move every v of the
 // row by up to 2^-11 of one).
@@ -99,13 +93,6 @@ struct Mean {
   float hi = 0.f, lo = 0.f;
   __device__ __forceinline__ Mean() {}
   __device__ __forceinline__ explicit Mean(double m) : hi((float)m), lo((float)(m - (double)(float)m)) {}
-  template <bool S>
-  __device__ __forceinline__ Mean in() const {
-    Mean m;
-    m.hi = uniform<S>(hi);
-    m.lo = uniform<S>(lo);
-    return m;
-  }
   __device__ __forceinline__ float from(float v) const { return (v - hi) - lo; }  // v - mean
 };
 
@@ -264,10 +251,11 @@ __device__ __forceinline__ void next_chunk() {
 //   up to 2048, 512 threads of up to four chunks  the row; weights and gate come from the L2 for every row
 //   above, 1024 threads of up to six              the sums alone; each of a row's rounds loads its chunks again, from the L2
 // us, before (all of it in registers for every length, up to 3.7 KB a lane spilled) and now, of 6 T d elements through memory at
-// the copy's rate: bf16 with post norm and gate 4096 x 12288 1,265 -> 195 (117), 4096 x 16384 1,461 -> 283 (156), 2048 x 28672
-// 1,923 -> 330 (136), without 490 -> 123, 573 -> 167, 1,066 -> 173; fp32 with 4096 x 8192 329 -> 213 (156), 2048 x 20480 1,775 ->
+// the copy's rate: bf16 with post norm and gate 4096 x 12288 1,265 -> 193 (117), 4096 x 16384 1,461 -> 272 (156), 2048 x 28672
+// 1,923 -> 334 (136), without 490 -> 124, 573 -> 170, 1,066 -> 172; fp32 with 4096 x 8192 329 -> 216 (156), 2048 x 20480 1,775 ->
 // 385 (194). The rounds' dependent loads and sums bound them; the two norms' rounds are one after the other.
-// One-chunk bf16 rows with two workgroups a CU (128 registers, 12 bytes spilled): 8192 x 2560 with layer norms 109 -> 82.
+// One-chunk bf16 rows with two workgroups a CU (128 registers, 12 bytes spilled): 8192 x 2560 with layer norms 109 -> 82. The
+// longest bf16 rows spill 44 bytes.
 template <typename T, int CPT, int NT, bool PRE, bool POST, bool MANY>
 __global__ __launch_bounds__(NT, (CPT == 1 && sizeof(T) == 2 && !MANY ? 4 : 1))
 void residual_norm_bwd_kernel(NormArgs a) {
@@ -279,8 +267,6 @@ void residual_norm_bwd_kernel(NormArgs a) {
   constexpr bool KEEP_B = POST && KEEP && BYTES <= 48;  // the gradient of post(y) stays until its row sums are there
   constexpr bool LONG = !KEEP || N > 16;            // chunk after chunk, nothing moved from one to another
   constexpr bool FORGET = BF16 && N > 16, FORGET_W = FORGET || (BF16 && MANY && N > 8);  // values are unpacked where they are used
-  // Row sums in scalar registers where vector registers are short (8192 x 7168 bf16 176 -> 168 us; 8192 x 4096 96 -> 98).
-  constexpr bool SCALAR = N > 8;
   __shared__ SumLds lds;
   int turn = 0;
   const bool need_y = a.y && (POST || a.gate);
@@ -402,8 +388,8 @@ void residual_norm_bwd_kernel(NormArgs a) {
           if constexpr (LONG) { settle(s.v[0]); settle(s.v[1]); settle(s.v[2]); }
         }
         s = block_sum<3>(s, lds, turn);
-        if (lr) mr = Mean(s.v[0] * a.inv_d).template in<SCALAR>();
-        if (ly) my = Mean(s.v[1] * a.inv_d).template in<SCALAR>();
+        if (lr) mr = Mean(s.v[0] * a.inv_d);
+        if (ly) my = Mean(s.v[1] * a.inv_d);
         if (lr) ma = (float)(s.v[2] * a.inv_d);
       }
       if (PRE || POST) {
@@ -438,9 +424,9 @@ void residual_norm_bwd_kernel(NormArgs a) {
           if constexpr (LONG) { settle(s.v[0]); settle(s.v[1]); settle(s.v[2]); }
         }
         s = block_sum<PRE ? 3 : 2>(s, lds, turn);
-        if (PRE) rr = uniform<SCALAR>(rsqrt_of(s.v[0] * a.inv_d + a.eps));
-        if (POST) ry = uniform<SCALAR>(rsqrt_of(s.v[1] * a.inv_d + a.eps));
-        if (PRE) car = uniform<SCALAR>((float)(s.v[2] * a.inv_d * (double)rr));  // mean(a rhat)
+        if (PRE) rr = rsqrt_of(s.v[0] * a.inv_d + a.eps);
+        if (POST) ry = rsqrt_of(s.v[1] * a.inv_d + a.eps);
+        if (PRE) car = (float)(s.v[2] * a.inv_d * (double)rr);  // mean(a rhat)
       }
       // The gradient g of r; that of post(y) is g by the gate, and by w_post, b.
       const auto grad = [&](int i, float (&gr)[EP], float (&rhat)[EP]) {
@@ -678,7 +664,6 @@ hipError_t launch_residual_norm(const moe_desc& d, const moe_norm& n, const void
   a.x = x;
   a.r = r;
   a.h = h;
-  if (!y && n.pre == MOE_NORM_NONE) return hipSuccess;  // r is x
   const Shape sh = row_shape(a.cpr, d.T >= 1024 ? 256 : 1024);
   KernelTimer kt("residual_norm", s);
   const auto go = [&](auto t, auto p, auto most) {

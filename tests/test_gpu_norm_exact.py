@@ -221,7 +221,7 @@ LONG = [(torch.bfloat16, 8704), (torch.bfloat16, 13312), (torch.bfloat16, 18432)
 
 
 @pytest.mark.parametrize("dt,d", LONG, ids=lambda v: str(v).replace("torch.", ""))
-@pytest.mark.parametrize("T,gate", [(520, 520), (1030, 515), (514, 2), (1, 1)])
+@pytest.mark.parametrize("T,gate", [(520, 520), (1030, 515), (514, 2), (2, 2), (1, 1)])
 def test_long_rows_and_many_gates(dt, d, T, gate):
     """More gate rows than workgroups, each with its share of w_post's gradient, and long rows of every kernel."""
     normal = normals(d + T, dt)
