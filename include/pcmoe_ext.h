@@ -166,7 +166,8 @@ typedef struct {
  *   w_post, w_pre [d] dtype or NULL (all ones); NULL where the norm is NONE
  *   gate    [gate_groups, d] dtype or NULL
  *   r, h    [T, d] dtype out; r may be x or y itself, h may be none of the inputs
- * The descriptor is checked as for the other calls; T, d_model and dtype of it are used. Sums over a row are held in fp64.
+ * The descriptor is checked as for the other calls; T, d_model and dtype of it are used. Sums over a row are held in fp64, means
+ * in two fp32 parts: rows far from zero, and next to the end of the type's range, lose no digits.
  * MOE_ERR_INVALID_ARGUMENT for a setting outside the ranges stated in moe_norm, and for weights, a gate or outputs that the
  * setting has no place for.
  */
@@ -177,8 +178,9 @@ moe_status moe_residual_norm(const moe_desc* desc, const moe_norm* norm, const v
  * Adjoint of moe_residual_norm at (r, y), from the gradients dr of r (from the rest of the stack) and dh of h:
  *   g = dr + the gradient of r through h;  dx = alpha g;  dy = gamma * g back through Npost
  *   dw_pre = sum_t dh_t * r^_t, dw_post = sum_t gamma_t g_t * y^_t, dgate = sum over a gate row's tokens of g_t * Npost(y_t)
- * (^: normalised, before the weight). The norms' statistics are formed again from r and y, r as it was rounded. Sums over
- * tokens have a fixed order: equal calls give equal bits.
+ * (^: normalised, before the weight). The norms' statistics are formed again from r and y, r as it was rounded. Sums over a row
+ * are fp64 sums of those of 16 bytes of it, which are fp32 where gradients are multiplied; sums over tokens are fp32 and have a
+ * fixed order: equal calls give equal bits.
  *   dr      [T, d] dtype, or NULL for zeros (the last block's r is used by nothing but h)
  *   dh      [T, d] dtype, NULL where pre is NONE
  *   y, r    [T, d] dtype: y NULL before the first block, where r is x; r may be NULL where pre is NONE, y where neither a
@@ -197,7 +199,7 @@ typedef struct {
   float lr;            /* learning rate, > 0 */
   float momentum;      /* mu, in [0, 1) */
   float weight_decay;  /* decoupled decay factor, >= 0 (the parameter shrinks by lr * weight_decay) */
-  float scale;         /* factor of the orthogonalised matrix, > 0 */
+  float scale;         /* factor of the orthogonalised matrix, > 0; the same for gate, up and down */
   float eps;           /* added to the norm, > 0 */
   int32_t nesterov;    /* 1: u = g + mu m; 0: u = m */
   int32_t steps;       /* Newton-Schulz steps, 1..16 */

@@ -176,7 +176,8 @@ struct NsArgs {
   float decay, step;       // p <- decay p - step X
 };
 
-// Stores: one tile and its mirror, both orientations, the parameters, or a part of a symmetric product's sums over K.
+// Stores: one tile and its mirror, both orientations, the parameters, or a part of a symmetric product's sums over K. (That of the
+// parameters spills 276 bytes a lane in the 256 x 256 tiles, beside 256 bytes of results a lane that wait in the other registers.)
 enum NsMode { NS_SYMMETRIC, NS_BOTH, NS_LAST, NS_PARTIAL };
 
 // LDS of an epilogue: a wavefront's part transposed, [WTN][WTM] fp16 with rows of PITCH words, or for parameters stored
@@ -563,6 +564,9 @@ hipError_t ns_product(const char* name, const NsArgs& a, bool precise, hipStream
   // Rounds of the chip, each priced by a tile's time: 4 units of the 128 x 128 tile's work at 1.4 times its rate (a last round in
   // quarters 0.4 or 0.8 of that), two such tiles at once, the smaller ones where both cost the same. 48 matrices of 1024 x 2816: A 170
   // and 204 us, P 82 and 94, X 346 and 407; 27 of 1024 x 1536 (A and P cost the same) 74 and 73, 58 and 52, X 122 and 142.
+  // The prices hold for 16 K-tiles and more. Where there are four to six, storing is most of a tile's time, which they leave out: 24
+  // matrices of 384 x 2176 take the larger tiles at 46.5 and 58.4 us for X and the parameters (128 x 128 tiles: 38.0 and 44.5), 24
+  // of 256 x 2560 at 32.2 for the parameters (24.6).
   const int64_t cus = device_cus();
   const double large = rounds_of(ns_tiles<NsLarge, MODE>(a), cus) * 4 / 1.4;
   const int64_t n = ns_tiles<NsSmall, MODE>(a);
