@@ -177,7 +177,7 @@ struct NsArgs {
 };
 
 // Stores: one tile and its mirror, both orientations, the parameters, or a part of a symmetric product's sums over K. (That of the
-// parameters spills 276 bytes a lane in the 256 x 256 tiles, beside 256 bytes of results a lane that wait in the other registers.)
+// parameters spills 276 bytes a lane in the 256 x 256 tiles, whose results take 256 registers meanwhile.)
 enum NsMode { NS_SYMMETRIC, NS_BOTH, NS_LAST, NS_PARTIAL };
 
 // LDS of an epilogue: a wavefront's part transposed, [WTN][WTM] fp16 with rows of PITCH words, or for parameters stored
