@@ -13,7 +13,8 @@ All calls are enqueued on one stream; no per-expert count ever returns to the ho
 """
 from __future__ import annotations
 
-from dataclasses import dataclass, replace
+from copy import copy
+from dataclasses import dataclass
 from typing import Optional
 
 import numpy as np
@@ -383,10 +384,10 @@ class MoEStack:
     """Layers one after the other with norms, gates and the residual stream around them:
         r_0 = x, h_0 = pre(r_0);  y_i = layer_i(h_i);  r_i+1 = alpha r_i + gate_i+1 * post(y_i), h_i+1 = pre(r_i+1)
     with `final` in place of pre at the end. The result is the last h, or the last r where final is "none". layers: MoELayers of
-    one T, d and dtype that host all experts. forward takes the layers' weights (whose x it sets) and len(layers) + 1 NormWeights. The stack's calls
-    read the layers' inputs from its own buffers, never from the weights' x: other stacks may run with the same weights between
-    a forward and its backward, and layers of one stack may share theirs. A backward belongs to the last forward of each of its
-    layers."""
+    one T, d and dtype that host all experts. forward takes the layers' weights (whose x it sets) and len(layers) + 1
+    NormWeights. The stack's calls read the layers' inputs from its own buffers, never from the weights' x: other stacks may run
+    with the same weights between a forward and its backward, and layers of one stack may share theirs. A backward belongs to
+    the last forward of each of its layers."""
 
     def __init__(self, layers, pre="rms", post="none", final="rms", eps=1e-6, residual_scale=1.0, gate_groups=1):
         if not layers:
@@ -419,13 +420,19 @@ class MoEStack:
             raise ValueError(f"{n} layers take {n} weights, {n + 1} norms and, if any, {n} experts: got {len(ws)}, {len(ns)}"
                              + (f" and {len(experts)}" if experts is not None else ""))
 
+    def _of(self, i, w):
+        """Weights w with the input of layer i."""
+        w = copy(w)
+        w.x = self.norms[i].h
+        return w
+
     def forward(self, x, ws, ns, experts=None):
         """experts: a Q4Experts or Q8Experts for each layer, to run the experts from (no backward can follow)."""
         self._check_counts(ws, ns, experts)
         r, h = self.norms[0].forward(ns[0], x)
         for i, (layer, w) in enumerate(zip(self.layers, ws)):
             w.x = h
-            w = replace(w, x=h)
+            w = self._of(i, w)
             if experts is None:
                 y = layer.forward(w)
             else:
@@ -435,8 +442,8 @@ class MoEStack:
         return r if h is None else h
 
     def backward(self, d, ws, ns):
-        """The gradient of x from that of forward's result. Layers leave the gradients of their weights in their buffers, the
-        norms in theirs."""
+        """The gradient of x from that of forward's result (without what passes through the routing of layers built with
+        router_backward=False). Layers leave the gradients of their weights in their buffers, the norms in theirs."""
         self._check_counts(ws, ns)
         if not self.backward_enabled:
             raise RuntimeError("a stack with a layer built with backward=False has no backward")
@@ -449,7 +456,7 @@ class MoEStack:
         dr, dh = (d, None) if self.norms[-1].h is None else (None, d)
         for i in reversed(range(len(self.layers))):
             dr, dy = self.norms[i + 1].backward(ns[i + 1], dr, dh)
-            dh = self.layers[i].backward(replace(ws[i], x=self.norms[i].h), dy)
+            dh = self.layers[i].backward(self._of(i, ws[i]), dy)
         return self.norms[0].backward(ns[0], dr, dh)[0]
 
 
