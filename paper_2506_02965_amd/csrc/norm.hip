@@ -719,11 +719,11 @@ hipError_t launch_residual_norm_bwd(const moe_desc& d, const moe_norm& n, const 
       // whole gate rows of a workgroup: what w_post's gradient has so far is added to in memory, a gate row at a time
       const auto more = [&](auto p, auto most) { with(t, p, most, std::false_type{}); };
       if (a.cpr <= 512) few(std::integral_constant<int, 1>{});
-      else if (a.cpr <= 1024) few(std::integral_constant<int, 2>{});
-      else if (a.cpr <= 1536) more(std::integral_constant<int, 3>{}, half);
-      else if (a.cpr <= 2048) more(std::integral_constant<int, 4>{}, half);
-      else if (a.cpr <= 3072) more(std::integral_constant<int, 3>{}, whole);
-      else if (a.cpr <= 4096) more(std::integral_constant<int, 4>{}, whole);
+      else if (a.cpr <= 2 * 512) few(std::integral_constant<int, 2>{});
+      else if (a.cpr <= 3 * 512) more(std::integral_constant<int, 3>{}, half);
+      else if (a.cpr <= 4 * 512) more(std::integral_constant<int, 4>{}, half);
+      else if (a.cpr <= 3 * 1024) more(std::integral_constant<int, 3>{}, whole);
+      else if (a.cpr <= 4 * 1024) more(std::integral_constant<int, 4>{}, whole);
       else if constexpr (std::is_same<T, float>::value) more(std::integral_constant<int, 6>{}, whole);  // at most 5,760
     };
     if (d.dtype == MOE_BF16) shapes(bf16{});
